@@ -205,6 +205,68 @@ ss_status slide_sparse_gemm_fused_ws(const void* Xq, const float* s_x, const voi
                                      ss_dtype dtype, void* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/* ---- Microscaled 4-bit operands (the OCP MX format with e2m1 elements) and layers of experts -------------------------------------
+ * Beyond the paper: the same quantise - pack - multiply path with the 4-bit type of gfx950's matrix instructions, dense and
+ * grouped by expert, and the router's choice and weighted sum around the grouped product.
+ *
+ * Code rows.  32 consecutive values of a row share a scale 2^(b - 127) (b = 255: not a number); a code is sign, two exponent
+ * bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A row is counted in units of 256 values; the last one is completed with zeros.
+ *   codes[row][mx4_row_bytes(K)]        two codes to a byte, the even value in the low half; 128 bytes a unit
+ *   scales[unit][row][8]                byte j: values 32 j .. 32 j + 31 of the unit; mx4_row_scales(K) bytes a row in all
+ * Limits: 1 <= K <= 2^24, rows <= 2^24, experts <= 1024; codes, scales and packed weights 16-byte aligned; other matrices need
+ * the alignment of an element, whatever their strides. */
+int64_t mx4_row_bytes(int64_t K);       /* 128 ceil(K / 256); -1 on a bad K */
+int64_t mx4_row_scales(int64_t K);      /* 8 ceil(K / 256); -1 on a bad K */
+
+/* Row r of the codes is row rows[r] of X[M,K] (row stride ldx elements; fp32 or bf16), or row r where rows is NULL (then R = M).  An entry of
+ * rows outside 0 .. M - 1 gives a row of zeros.  Per 32 values with a = max|x|: b = max(floor(log2 a) - 2 + 127, 0), codes
+ * rne(x / 2^(b - 127)) with ties to even, at most 6 in magnitude; the sign of zeros is kept.  a = 0: b = 0.  Values with an infinity or
+ * a NaN among them: b = 255, codes 0, and every product with them is a NaN. */
+ss_status mx4_quant(const void* X, ss_act_dtype in_dtype, int64_t M, int64_t K, int64_t ldx, const int32_t* rows, int64_t R,
+                    void* codes, void* scales, void* stream);
+
+/* The values that codes[R] and their scales stand for, as fp32 (exact) or bf16 (exact but for magnitudes below 2^-133), row stride ldy. */
+ss_status mx4_dequant(const void* codes, const void* scales, int64_t R, int64_t K, ss_act_dtype out_dtype, void* Y, int64_t ldy,
+                      void* stream);
+
+/* Weights for the two products, once.  codes and scales of E matrices [O,K] one after the other, as mx4_quant writes them for [E O, K]; gated: of E
+ * matrices [2 O, K], the O rows of gate before the O rows of up.  The packed layout is opaque. */
+ss_status mx4_packed_sizes(int64_t E, int64_t O, int64_t K, int gated, size_t* vals_bytes, size_t* meta_bytes);
+ss_status mx4_pack(const void* codes, const void* scales, int64_t E, int64_t O, int64_t K, int gated, void* w_vals, void* w_meta,
+                   void* stream);
+
+/* Y[M,O] = bf16(X W^T) of 4-bit operands, products exact, sums in fp32, one rounding; gated = 1: bf16(silu(X Wg^T) * (X Wu^T)).
+ * codes, scales: rows of mx4_quant with the same K; w_vals, w_meta: mx4_pack with E = 1 and the same O, K, gated.  Y has row stride ldy
+ * (O <= ldy < 2^22).  workspace as for slide_sparse_gemm_ws: mx4_gemm_workspace_bytes(M, 1, O, K, gated) bytes let few rows use the
+ * whole chip; without it, or with less, the row is not split.  Every call with the same arguments gives the same bits. */
+size_t mx4_gemm_workspace_bytes(int64_t R, int64_t E, int64_t O, int64_t K, int gated);
+ss_status mx4_gemm(const void* codes, const void* scales, const void* w_vals, const void* w_meta, int64_t M, int64_t O, int64_t K,
+                   int gated, void* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same with the weights of E experts: row r of R is multiplied with expert e's where offsets[e] <= r < offsets[e + 1].  offsets[E + 1] lies on the
+ * device, begins with 0 and does not fall; experts may have no row.  Rows from offsets[E] on give zeros.  (Offsets that break these rules are
+ * moved to the nearest that do not: some rows then meet another expert than meant, and nothing else happens.) */
+ss_status mx4_grouped_gemm(const void* codes, const void* scales, const int32_t* offsets, const void* w_vals, const void* w_meta,
+                           int64_t R, int64_t E, int64_t O, int64_t K, int gated, void* Y, int64_t ldy, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* The k experts of largest score of each row of logits[M,E] (row stride ld; fp32 or bf16; 1 <= k <= min(E, 64)), and the order of the M k rows by expert:
+ *   ids[M,k]       largest score first; of equal ones (and -0 and 0 are equal) the lower index; a NaN lies below every number
+ *   weights[M,k]   exp(score) over the sum of the k chosen (renormalise = 1) or of all E; all scores of a row minus infinity: zeros
+ *   offsets[E+1]   where each expert's rows begin, for mx4_grouped_gemm
+ *   slots[M,k]     the row that choice j of token m has in that order: by expert, then by token
+ *   rows[M k]      the token of each row in that order, for mx4_quant
+ * workspace: expert_route_workspace_bytes(M, E, k) bytes (0 for up to 64 tokens), 16-byte aligned, SS_ERR_WORKSPACE if there is less. */
+size_t expert_route_workspace_bytes(int64_t M, int64_t E, int64_t k);
+ss_status expert_route(const void* logits, ss_act_dtype in_dtype, int64_t M, int64_t E, int64_t ld, int k, int renormalise,
+                       int32_t* ids, float* weights, int32_t* slots, int32_t* rows, int32_t* offsets, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* out[m] = bf16(sum over j of weights[m,j] Y[slots[m,j]] + base[m]): sums in fp32 in the order of j, base (bf16 [M,O], may be NULL) last, one
+ * rounding.  Y bf16 [R,O]; a slot outside 0 .. R - 1 adds nothing.  Row strides ldy, ldb, ldo; 1 <= k <= 64. */
+ss_status expert_combine(const void* Y, int64_t R, int64_t O, int64_t ldy, const int32_t* slots, const float* weights, int64_t M,
+                         int k, const void* base, int64_t ldb, void* out, int64_t ldo, void* stream);
+
 /* Library housekeeping (no passage of the paper): a static, human-readable name for a status code ... */
 const char* ss_status_string(ss_status s);
 

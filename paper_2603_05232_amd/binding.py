@@ -28,6 +28,8 @@ EXPORTS = ("slide_lifted_k", "slide_lifted_ld", "slide_packed_sizes", "slide_pru
            "slide_gemm_workspace_bytes", "slide_sparse_gemm_ws", "dense_gemm_ws",
            "slide_packed_sizes_fused", "slide_decompose_fused", "slide_sparse_gemm_fused", "slide_sparse_gemm_fused_ws",
            "slide_static_scratch_bytes", "slide_sparse_gemm_static",
+           "mx4_row_bytes", "mx4_row_scales", "mx4_quant", "mx4_dequant", "mx4_packed_sizes", "mx4_pack", "mx4_gemm_workspace_bytes", "mx4_gemm",
+           "mx4_grouped_gemm", "expert_route_workspace_bytes", "expert_route", "expert_combine",
            "ss_status_string", "slide_format_version")
 # entry points that the extension module calls, at the addresses of the library loaded here (order of its bind())
 _CALLED = ("slide_lifted_ld", "act_lift_quant", "slide_sparse_gemm_ws", "slide_sparse_gemm_fused_ws")
@@ -78,6 +80,19 @@ def load():
                  "act_lift_quant", "slide_sparse_gemm", "dense_gemm", "slide_sparse_gemm_ws", "dense_gemm_ws",
                  "slide_packed_sizes_fused", "slide_decompose_fused", "slide_sparse_gemm_fused"):
         getattr(lib, name).restype = i32
+    for name, args, res in (("mx4_row_bytes", [i64], i64), ("mx4_row_scales", [i64], i64),
+                            ("mx4_quant", [vp, i32, i64, i64, i64, vp, i64, vp, vp, vp], i32),
+                            ("mx4_dequant", [vp, vp, i64, i64, i32, vp, i64, vp], i32),
+                            ("mx4_packed_sizes", [i64, i64, i64, i32, ctypes.POINTER(sz), ctypes.POINTER(sz)], i32),
+                            ("mx4_pack", [vp, vp, i64, i64, i64, i32, vp, vp, vp], i32),
+                            ("mx4_gemm_workspace_bytes", [i64, i64, i64, i64, i32], sz),
+                            ("mx4_gemm", [vp, vp, vp, vp, i64, i64, i64, i32, vp, i64, vp, sz, vp], i32),
+                            ("mx4_grouped_gemm", [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, i64, vp, sz, vp], i32),
+                            ("expert_route_workspace_bytes", [i64, i64, i64], sz),
+                            ("expert_route", [vp, i32, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp], i32),
+                            ("expert_combine", [vp, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp], i32)):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, res
     lib.ss_status_string.argtypes = [i32]
     lib.ss_status_string.restype = ctypes.c_char_p
     lib.slide_format_version.restype = i32
@@ -312,4 +327,161 @@ def slide_sparse_gemm_static(X_lifted, s_x, w_vals, w_meta, s_w, O: int, dtype: 
     assert X_lifted.is_contiguous() and out is not None
     _check(load().slide_sparse_gemm_static(_ptr(X_lifted), _ptr(s_x), _ptr(w_vals), _ptr(w_meta), _ptr(s_w), M, O, Kp,
                                            DTYPE_CODE[dtype], _ptr(out), out.stride(0), _stream()), "slide_sparse_gemm_static")
+    return out
+
+
+# ---- microscaled 4-bit operands and layers of experts -------------------------------------------------------------------------
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements between the rows of a matrix whose rows are dense (of a single row: its width)."""
+    rows, width = t.shape
+    assert t.is_cuda and (width < 2 or t.stride(1) == 1)
+    return t.stride(0) if rows > 1 else width
+
+
+def _dense_i32(t: torch.Tensor, what: str) -> int:
+    if t.dtype != torch.int32:
+        raise TypeError(f"{what} must be int32, got {t.dtype}")
+    assert t.is_cuda and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _mx4_operand(codes: torch.Tensor, scales: torch.Tensor, K: int):
+    """Checks that codes[R, 128 U] and scales[U, R, 8] are rows of K values."""
+    assert codes.is_cuda and codes.is_contiguous() and scales.is_contiguous() and codes.dtype == scales.dtype == torch.uint8
+    assert codes.shape[1] == mx4_row_bytes(K) and scales.shape == (codes.shape[1] // 128, codes.shape[0], 8)
+
+
+@functools.lru_cache(maxsize=4096, typed=True)
+def mx4_row_bytes(K: int) -> int:
+    return int(load().mx4_row_bytes(K))
+
+
+def mx4_row_scales(K: int) -> int:
+    return int(load().mx4_row_scales(K))
+
+
+def mx4_quant(X: torch.Tensor, rows=None, codes=None, scales=None):
+    """X[M,K] fp32/bf16 (row stride allowed) -> (codes[R, 128 U] uint8, scales[U, R, 8] uint8); rows: int32 [R], the row of X that each
+    row of codes is made of."""
+    M, K = X.shape
+    R = M if rows is None else rows.shape[0]
+    width = mx4_row_bytes(K)
+    if width < 0:
+        raise SlideSparseError(3, "mx4_quant")
+    if codes is None:
+        codes = X.new_empty((R, width), dtype=torch.uint8)
+    if scales is None:
+        scales = X.new_empty((width // 128, R, 8), dtype=torch.uint8)
+    assert codes.shape[0] == R
+    _mx4_operand(codes, scales, K)
+    code = load().mx4_quant(X.data_ptr(), _in_code(X), M, K, _row_stride(X), None if rows is None else _dense_i32(rows, "rows"), R, codes.data_ptr(),
+                            scales.data_ptr(), _stream())
+    if code:
+        _check(code, "mx4_quant")
+    return codes, scales
+
+
+def mx4_dequant(codes: torch.Tensor, scales: torch.Tensor, K: int, dtype: torch.dtype = torch.float32, out=None):
+    """codes, scales of mx4_quant -> their values [R,K] as fp32 or bf16."""
+    _mx4_operand(codes, scales, K)
+    if out is None:
+        out = codes.new_empty((codes.shape[0], K), dtype=dtype)
+    assert out.shape == (codes.shape[0], K)
+    code = load().mx4_dequant(codes.data_ptr(), scales.data_ptr(), codes.shape[0], K, _in_code(out), out.data_ptr(), _row_stride(out), _stream())
+    if code:
+        _check(code, "mx4_dequant")
+    return out
+
+
+def mx4_packed_sizes(O: int, K: int, experts: int = 1, gated: bool = False):
+    v, m = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().mx4_packed_sizes(experts, O, K, int(gated), ctypes.byref(v), ctypes.byref(m)), "mx4_packed_sizes")
+    return int(v.value), int(m.value)
+
+
+def mx4_pack(codes: torch.Tensor, scales: torch.Tensor, K: int, experts: int = 1, gated: bool = False):
+    """Codes of experts x [O,K] weights (gated: of experts x [2 O,K], gate's rows before up's) -> (w_vals, w_meta)."""
+    _mx4_operand(codes, scales, K)
+    O, rest = divmod(codes.shape[0], experts * (2 if gated else 1))
+    if rest:
+        raise SlideSparseError(3, "mx4_pack")
+    vb, mb = mx4_packed_sizes(O, K, experts, gated)
+    w_vals = codes.new_empty((vb,))
+    w_meta = codes.new_empty((mb,))
+    _check(load().mx4_pack(codes.data_ptr(), scales.data_ptr(), experts, O, K, int(gated), w_vals.data_ptr(), w_meta.data_ptr(), _stream()), "mx4_pack")
+    return w_vals, w_meta
+
+
+def mx4_gemm_workspace_bytes(R: int, O: int, K: int, experts: int = 1, gated: bool = False) -> int:
+    return int(load().mx4_gemm_workspace_bytes(R, experts, O, K, int(gated)))
+
+
+def _mx4_product(name, offsets, codes, scales, w_vals, w_meta, experts, O, K, gated, out, workspace):
+    _mx4_operand(codes, scales, K)
+    sizes = _mx4_sizes(O, K, experts, gated)
+    assert w_vals.is_contiguous() and w_meta.is_contiguous() and (w_vals.numel(), w_meta.numel()) == sizes
+    R = codes.shape[0]
+    if out is None:
+        out = codes.new_empty((R, O), dtype=torch.bfloat16)
+    assert out.dtype == torch.bfloat16 and out.shape == (R, O)
+    tail = (O, K, int(gated), out.data_ptr(), _row_stride(out), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if offsets is None:
+        code = load().mx4_gemm(codes.data_ptr(), scales.data_ptr(), w_vals.data_ptr(), w_meta.data_ptr(), R, *tail)
+    else:
+        code = load().mx4_grouped_gemm(codes.data_ptr(), scales.data_ptr(), offsets, w_vals.data_ptr(), w_meta.data_ptr(), R, experts, *tail)
+    if code:
+        _check(code, name)
+    return out
+
+
+_mx4_sizes = functools.lru_cache(maxsize=4096, typed=True)(mx4_packed_sizes)
+
+
+def mx4_gemm(codes, scales, w_vals, w_meta, O: int, K: int, gated: bool = False, out=None, workspace=None):
+    """Y[M,O] bf16 = X . W^T of 4-bit operands (gated: silu(X . Wg^T) * (X . Wu^T)); workspace: optional uint8 device tensor."""
+    return _mx4_product("mx4_gemm", None, codes, scales, w_vals, w_meta, 1, O, K, gated, out, workspace)
+
+
+def mx4_grouped_gemm(codes, scales, offsets, w_vals, w_meta, O: int, K: int, gated: bool = False, out=None, workspace=None):
+    """The same with the weights of expert e for the rows offsets[e] .. offsets[e + 1] - 1 (int32, on the device); the others give zeros."""
+    return _mx4_product("mx4_grouped_gemm", _dense_i32(offsets, "offsets"), codes, scales, w_vals, w_meta, offsets.shape[0] - 1, O, K, gated, out, workspace)
+
+
+def expert_route_workspace_bytes(M: int, E: int, k: int) -> int:
+    return int(load().expert_route_workspace_bytes(M, E, k))
+
+
+def expert_route(logits: torch.Tensor, k: int, renormalise: bool = True, workspace=None):
+    """logits[M,E] fp32/bf16 -> (ids[M,k], weights[M,k], slots[M,k], rows[M k], offsets[E + 1]): the k experts of largest score, their softmax
+    weights, and the order of the rows by expert."""
+    M, E = logits.shape
+    if workspace is None:
+        n = expert_route_workspace_bytes(M, E, k)
+        workspace = logits.new_empty((n,), dtype=torch.uint8) if n else None
+    ids, slots = logits.new_empty((2, M, max(k, 0)), dtype=torch.int32)
+    weights = logits.new_empty((M, max(k, 0)), dtype=torch.float32)
+    rows = logits.new_empty((M * max(k, 0),), dtype=torch.int32)
+    offsets = logits.new_empty((E + 1,), dtype=torch.int32)
+    code = load().expert_route(logits.data_ptr(), _in_code(logits), M, E, _row_stride(logits), k, int(renormalise), ids.data_ptr(), weights.data_ptr(),
+                               slots.data_ptr(), rows.data_ptr(), offsets.data_ptr(), _ptr(workspace),
+                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    if code:
+        _check(code, "expert_route")
+    return ids, weights, slots, rows, offsets
+
+
+def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, base=None, out=None):
+    """out[M,O] bf16 = sum over j of weights[m,j] Y[slots[m,j]] (+ base[m]); Y bf16 [R,O], slots int32 [M,k], weights fp32 [M,k]."""
+    R, O = Y.shape
+    M, k = slots.shape
+    assert weights.shape == (M, k) and weights.is_contiguous() and weights.dtype == torch.float32 and Y.dtype == torch.bfloat16
+    assert base is None or (base.shape == (M, O) and base.dtype == torch.bfloat16)
+    if out is None:
+        out = Y.new_empty((M, O))
+    assert out.shape == (M, O) and out.dtype == torch.bfloat16
+    code = load().expert_combine(Y.data_ptr(), R, O, _row_stride(Y), _dense_i32(slots, "slots"), weights.data_ptr(), M, k, _ptr(base),
+                                 0 if base is None else _row_stride(base), out.data_ptr(), _row_stride(out), _stream())
+    if code:
+        _check(code, "expert_combine")
     return out

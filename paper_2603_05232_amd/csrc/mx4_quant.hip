@@ -1,0 +1,221 @@
+// mx4_quant, mx4_dequant, mx4_pack: microscaled 4-bit codes of activations and weights, their values, and the operand order of the products.
+#include "mx4_common.h"
+#include "quant_common.h"
+
+namespace ss {
+
+// loads and stores of 16 bytes at the alignment of an element
+template <typename T> struct Piece;
+template <> struct Piece<float> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Piece<uint16_t> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2))); };
+
+// eight consecutive values of a row from element k on, those at or beyond K zero
+template <typename T> __device__ inline void load8(const T* row, int64_t k, int64_t K, float (&f)[8])
+{
+    if (k + 8 <= K) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const typename Piece<T>::V v = reinterpret_cast<const typename Piece<T>::V*>(row + k)[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[4 * i + j] = __uint_as_float(v[j]);
+            }
+        } else {
+            const typename Piece<T>::V v = *reinterpret_cast<const typename Piece<T>::V*>(row + k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(v[j] << 16); f[2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u); }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = k + j < K ? load_scalar(row + k + j) : 0.0f;
+    }
+}
+
+// the magnitudes' largest bits; a NaN's are above infinity's
+__device__ inline uint32_t largest8(const float (&f)[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+    return m;
+}
+
+__device__ inline uint32_t scale_byte(uint32_t largest) { return largest >= 0x7F800000u ? 255u : max(largest >> 23, 2u) - 2u; }
+
+// code of x r, r the inverse of the scale: nearest, ties to even, at most 6
+__device__ inline uint32_t code_of(float x, float r)
+{
+    const float v = fabsf(x * r);
+    const uint32_t c = (v > 0.25f) + (v >= 0.75f) + (v > 1.25f) + (v >= 1.75f) + (v > 2.5f) + (v >= 3.5f) + (v > 5.0f);
+    return c | (__float_as_uint(x) >> 31 << 3);
+}
+
+// A thread takes eight values, four threads a block, a wavefront two units of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_quant(const T* __restrict__ X, int64_t M, int64_t K, int64_t ldx, const int32_t* __restrict__ rows, int64_t R,
+                                                   int U, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int per_row)
+{
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), r = item / per_row;
+    const int lane = threadIdx.x & 63;
+    if (r >= R) return;
+    const int u = (int)(item - r * per_row) * 2 + (lane >> 5);
+    const int64_t src = rows ? rows[r] : r;
+    float f[8];
+    const bool there = src >= 0 && src < M && u < U;
+    load8(X + (there ? src : 0) * ldx, (int64_t)u * MX_UNIT + (lane & 31) * 8, there ? K : 0, f);
+    uint32_t m = largest8(f);
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1, 64));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2, 64));
+    const uint32_t b = scale_byte(m);
+    const float inv = __uint_as_float((254u - min(b, 253u)) << 23);
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w |= code_of(f[j], inv) << (4 * j);
+    if (u < U) {
+        *reinterpret_cast<uint32_t*>(codes + r * U * MX_UNITB + (int64_t)u * MX_UNITB + (lane & 31) * 4) = b == 255 ? 0u : w;
+        if ((lane & 3) == 0) scales[((int64_t)u * R + r) * MX_UNITS + ((lane & 31) >> 2)] = (uint8_t)b;
+    }
+}
+
+__device__ inline float code_value(uint32_t c)
+{
+    const uint32_t e = (c >> 1) & 3, m = c & 1;
+    const float v = e ? __uint_as_float(((126 + e) << 23) | (m << 22)) : 0.5f * (float)m;
+    return c & 8 ? -v : v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_mx4_dequant(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t R, int64_t K, int U,
+                                                     T* __restrict__ Y, int64_t ldy, int per_row)
+{
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), r = item / per_row;
+    const int lane = threadIdx.x & 63;
+    if (r >= R) return;
+    const int u = (int)(item - r * per_row) * 2 + (lane >> 5);
+    if (u >= U) return;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + r * U * MX_UNITB + (int64_t)u * MX_UNITB + (lane & 31) * 4);
+    const uint32_t b = scales[((int64_t)u * R + r) * MX_UNITS + ((lane & 31) >> 2)];
+    const float s = b == 255 ? __uint_as_float(0x7FC00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = code_value(w >> (4 * j)) * s;
+    const int64_t k = (int64_t)u * MX_UNIT + (lane & 31) * 8;
+    T* const dst = Y + r * ldy + k;
+    typedef typename Piece<T>::V V;
+    if constexpr (sizeof(T) == 4) {
+        if (k + 8 <= K) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                reinterpret_cast<V*>(dst)[i] = V{__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]), __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3])};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < K) dst[j] = f[j];
+        }
+    } else {
+        const uint32_t o[4] = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+        if (k + 8 <= K) *reinterpret_cast<V*>(dst) = V{o[0], o[1], o[2], o[3]};
+        else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < K) dst[j] = (T)(o[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+}
+
+// one workgroup per fragment and unit: thread (step, lane) moves one lane's 16 bytes, the first 64 threads the scale words
+__global__ __launch_bounds__(256) void k_mx4_pack(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t all_rows, int U,
+                                                  bool gated, int64_t frags, uint8_t* __restrict__ w_vals, uint8_t* __restrict__ w_meta)
+{
+    const int u = blockIdx.x % U;
+    const int64_t f = blockIdx.x / U, expert = f / frags;
+    const int s = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+    const int64_t c = (f - expert * frags) * MX_FRAG + mx4_channel(lane & 31);
+    const bool there = c < rows;
+    const int64_t row = expert * rows + (gated ? (c & 1) * (rows >> 1) + (c >> 1) : c);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (there) v = *reinterpret_cast<const uint4*>(codes + (row * U + u) * MX_UNITB + (4 * h + s) * 16);
+    reinterpret_cast<uint4*>(w_vals + (f * U + u) * MX_FRAGB)[threadIdx.x] = v;
+    if (s == 0)
+        reinterpret_cast<uint32_t*>(w_meta + (f * U + u) * MX_FRAGS)[lane] =
+            there ? *reinterpret_cast<const uint32_t*>(scales + ((int64_t)u * all_rows + row) * MX_UNITS + 4 * h) : 0u;
+}
+
+}  // namespace ss
+
+using namespace ss;
+
+static bool valid_in(ss_act_dtype t) { return t == SS_IN_F32 || t == SS_IN_BF16; }
+static int in_size(ss_act_dtype t) { return t == SS_IN_F32 ? 4 : 2; }
+
+extern "C" int64_t mx4_row_bytes(int64_t K) { return K < 1 || K > MX_MAX_K ? -1 : mx4_units(K) * MX_UNITB; }
+extern "C" int64_t mx4_row_scales(int64_t K) { return K < 1 || K > MX_MAX_K ? -1 : mx4_units(K) * MX_UNITS; }
+
+extern "C" ss_status mx4_quant(const void* X, ss_act_dtype in_dtype, int64_t M, int64_t K, int64_t ldx, const int32_t* rows, int64_t R, void* codes,
+                               void* scales, void* stream)
+{
+    if (!valid_in(in_dtype)) return SS_ERR_DTYPE;
+    if (M < 0 || R < 0 || M > MX_MAX_ROWS || R > MX_MAX_ROWS || K < 1 || K > MX_MAX_K || ldx < K || (!rows && R != M)) return SS_ERR_SHAPE;
+    if (R == 0) return SS_OK;
+    if ((!X && M > 0) || !codes || !scales) return SS_ERR_NULL;
+    if (((uintptr_t)X & (in_size(in_dtype) - 1)) || ((uintptr_t)rows & 3) || ((uintptr_t)codes & 15) || ((uintptr_t)scales & 15)) return SS_ERR_SHAPE;
+    const int U = (int)mx4_units(K), per_row = (U + 1) / 2;
+    const int64_t blocks = (R * per_row + 3) / 4;
+    if (blocks > INT32_MAX) return SS_ERR_SHAPE;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (in_dtype == SS_IN_F32)
+        hipLaunchKernelGGL(k_mx4_quant<float>, dim3((uint32_t)blocks), dim3(256), 0, hs, static_cast<const float*>(X), M, K, ldx, rows, R, U,
+                           static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), per_row);
+    else
+        hipLaunchKernelGGL(k_mx4_quant<uint16_t>, dim3((uint32_t)blocks), dim3(256), 0, hs, static_cast<const uint16_t*>(X), M, K, ldx, rows, R, U,
+                           static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), per_row);
+    return launch_status();
+}
+
+extern "C" ss_status mx4_dequant(const void* codes, const void* scales, int64_t R, int64_t K, ss_act_dtype out_dtype, void* Y, int64_t ldy, void* stream)
+{
+    if (!valid_in(out_dtype)) return SS_ERR_DTYPE;
+    if (R < 0 || R > MX_MAX_ROWS || K < 1 || K > MX_MAX_K || ldy < K) return SS_ERR_SHAPE;
+    if (R == 0) return SS_OK;
+    if (!codes || !scales || !Y) return SS_ERR_NULL;
+    if (((uintptr_t)codes & 15) || ((uintptr_t)scales & 15) || ((uintptr_t)Y & (in_size(out_dtype) - 1))) return SS_ERR_SHAPE;
+    const int U = (int)mx4_units(K), per_row = (U + 1) / 2;
+    const int64_t blocks = (R * per_row + 3) / 4;
+    if (blocks > INT32_MAX) return SS_ERR_SHAPE;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (out_dtype == SS_IN_F32)
+        hipLaunchKernelGGL(k_mx4_dequant<float>, dim3((uint32_t)blocks), dim3(256), 0, hs, static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), R, K, U,
+                           static_cast<float*>(Y), ldy, per_row);
+    else
+        hipLaunchKernelGGL(k_mx4_dequant<uint16_t>, dim3((uint32_t)blocks), dim3(256), 0, hs, static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), R, K, U,
+                           static_cast<uint16_t*>(Y), ldy, per_row);
+    return launch_status();
+}
+
+static bool valid_weights(int64_t E, int64_t O, int64_t K, int gated)
+{
+    return E >= 1 && E <= MX_MAX_EXPERTS && O >= 0 && O < (1 << 22) && K >= 1 && K <= MX_MAX_K && (gated == 0 || gated == 1);
+}
+
+extern "C" ss_status mx4_packed_sizes(int64_t E, int64_t O, int64_t K, int gated, size_t* vals_bytes, size_t* meta_bytes)
+{
+    if (!valid_weights(E, O, K, gated)) return SS_ERR_SHAPE;
+    if (!vals_bytes || !meta_bytes) return SS_ERR_NULL;
+    const size_t n = (size_t)(E * mx4_frags(O << gated) * mx4_units(K));
+    *vals_bytes = n * MX_FRAGB;
+    *meta_bytes = n * MX_FRAGS;
+    return SS_OK;
+}
+
+extern "C" ss_status mx4_pack(const void* codes, const void* scales, int64_t E, int64_t O, int64_t K, int gated, void* w_vals, void* w_meta, void* stream)
+{
+    if (!valid_weights(E, O, K, gated)) return SS_ERR_SHAPE;
+    if (O == 0) return SS_OK;
+    if (!codes || !scales || !w_vals || !w_meta) return SS_ERR_NULL;
+    if (((uintptr_t)codes & 15) || ((uintptr_t)scales & 15) || ((uintptr_t)w_vals & 15) || ((uintptr_t)w_meta & 15)) return SS_ERR_SHAPE;
+    const int64_t rows = O << gated, U = mx4_units(K), frags = mx4_frags(rows);
+    if (E * rows > MX_MAX_ROWS * 64 || E * frags * U > INT32_MAX) return SS_ERR_SHAPE;
+    hipLaunchKernelGGL(k_mx4_pack, dim3((uint32_t)(E * frags * U)), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<const uint8_t*>(codes),
+                       static_cast<const uint8_t*>(scales), rows, E * rows, (int)U, gated != 0, frags, static_cast<uint8_t*>(w_vals), static_cast<uint8_t*>(w_meta));
+    return launch_status();
+}
