@@ -104,4 +104,8 @@ struct mx4_call {
     bool gated;
 };
 
+// Tiles of 256 channels x 256 rows (mx4_tile.hip); rows of MX_TILE_UNITS units and more.
+constexpr int MX_TILE_UNITS = 3;
+ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
+
 }  // namespace ss

@@ -141,6 +141,7 @@ static ss_status mx4_product(bool grouped, const void* codes, const void* scales
                   static_cast<const uint8_t*>(w_meta), (int)R, (int)E, (int)O, (int)mx4_units(K), (int)mx4_frags(O << gated),
                   static_cast<uint16_t*>(Y), ldy, gated != 0};
     hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (c.U >= MX_TILE_UNITS && R >= 192 * E) return launch_mx4_tile(c, hs);
     return grouped ? launch_mx4_stream<true>(c, mx4_max_tiles(R, E, 32), hs) : launch_mx4_stream<false>(c, (R + 31) / 32, hs);
 }
 
