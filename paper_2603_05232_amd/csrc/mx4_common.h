@@ -6,12 +6,12 @@
 //   codes[row][unit][128]     two codes to a byte, the even value in the low half; block j of the unit is bytes 16 j .. 16 j + 15
 //   scales[unit][row][8]      byte j: block j of the unit.  The units lie outermost so that a tile's rows of one unit are one run.
 //
-// Operands.  Lane (n, h) = (l & 31, l >> 5) of the 32x32x64 instruction holds 32 values, one block, of row n.  Step s = 0 .. 3 of a unit
-// takes block 4 h + s, so a lane's four blocks are 64 consecutive bytes and their scales one word, whose byte s the instruction selects.
-//   w_vals[expert][fragment of 32 channels][unit][step 4][lane 64][16 B]
-//   w_meta[expert][fragment][unit][lane 64][4 B]
-// Fragment row r holds channel mx4_channel(r), so that a lane's sixteen sums are sixteen consecutive channels.  Gated layers alternate
-// the channels of gate and up: packed channel 2 c is gate's channel c, 2 c + 1 is up's.
+// Operands.  Lane (n, q) = (l & 15, l >> 4) of the 16x16x128 instruction holds 32 values, one block, of row n.  Step t = 0, 1 of a unit takes block
+// 2 q + t, so a lane's two blocks are 32 consecutive bytes and their scales lie side by side; the instruction selects the byte.
+//   w_vals[expert][fragment of 32 channels][unit][step 2][half 2][lane 64][16 B]      lane (n, q): block 2 q + t of fragment row (half, n)
+//   w_meta[expert][fragment][unit][lane 64][4 B]                                      byte 2 half + t: its scale
+// Fragment row (half, r) holds channel mx4_channel(half, r), so that a lane's eight sums (4 half + i) are eight consecutive channels.
+// Gated layers alternate the channels of gate and up: packed channel 2 c is gate's channel c, 2 c + 1 is up's.
 #pragma once
 #include "ss_common.h"
 #include "mma_types.h"
@@ -30,18 +30,44 @@ constexpr int64_t MX_MAX_ROWS = 1 << 24;
 
 __host__ __device__ inline int64_t mx4_units(int64_t K) { return (K + MX_UNIT - 1) / MX_UNIT; }
 __host__ __device__ inline int64_t mx4_frags(int64_t rows) { return (rows + MX_FRAG - 1) / MX_FRAG; }
-// channel of a fragment's row r: sums i of lane half h belong to rows 8 (i >> 2) + 4 h + (i & 3)
-__host__ __device__ inline int mx4_channel(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
+// channel of a fragment's row: sums i of lane group q belong to rows 4 q + i
+__host__ __device__ inline int mx4_channel(int half, int r) { return (r >> 2) * 8 + half * 4 + (r & 3); }
 
-// One 32x32x64 product of 4-bit operands; `S` selects the byte of the scale words.
-template <int S> __device__ __forceinline__ v16f mx4_mma(v4i a, v4i b, v16f c, int sa, int sb)
+// One 16x16x128 product of 4-bit operands; SA, SB select the bytes of the scale words.
+template <int SA, int SB> __device__ __forceinline__ v4f mx4_mma(v4i a, v4i b, v4f c, int sa, int sb)
 {
     const v8i a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, S, sa, S, sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, SA, sa, SB, sb);
 }
+
+typedef uint32_t piece4_t __attribute__((aligned(2)));
 
 // silu(g) u, in 32 bits
 __device__ inline float mx4_gate(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
+// running sum and maximum over the lanes of a wavefront
+template <typename F> __device__ inline int wave_scan(int v, int none, F f)
+{
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x111, 0xF, 0xF, false));      // row_shr:1
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x112, 0xF, 0xF, false));      // 2
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x114, 0xF, 0xF, false));      // 4
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x118, 0xF, 0xF, false));      // 8
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x142, 0xA, 0xF, false));      // row_bcast:15
+    v = f(v, __builtin_amdgcn_update_dpp(none, v, 0x143, 0xC, 0xF, false));      // row_bcast:31
+    return v;
+}
+__device__ inline int wave_scan_add(int v) { return wave_scan(v, 0, [](int a, int b) { return a + b; }); }
+__device__ inline int wave_scan_max(int v) { return wave_scan(v, 0, [](int a, int b) { return a > b ? a : b; }); }      // of values >= 0
+
+// The rows of experts e0 .. e0 + 63, one to a lane (lanes beyond the last expert: those behind its rows).  Offsets outside [0, R] or below one before
+// them are moved to the nearest that is not, so that every row belongs to one expert or to none, whatever they hold.
+struct mx4_span { int first, last; };
+__device__ inline mx4_span mx4_spans(const int32_t* __restrict__ offsets, int E, int R, int e0, int lane, int end)
+{
+    const int e = e0 + lane, last = max(wave_scan_max(e < E ? min(max(offsets[e + 1], 0), R) : R), end);
+    const int before = __builtin_amdgcn_update_dpp(end, last, 0x138, 0xF, 0xF, false);      // wave_shr:1
+    return {before, last};
+}
 
 // A tile of token rows of one expert.
 struct mx4_rows {
@@ -49,41 +75,23 @@ struct mx4_rows {
     int first, count;    // count = 0: there is no such tile
 };
 
-// Tile number `slot` of the tiles of T rows that the experts' rows and the rows behind the last expert's make, in order.  Offsets outside
-// [0, R] or below one before them are moved to the nearest that is not, so that every row belongs to one tile whatever they hold.
-// Called by whole wavefronts.
+// Tile number `slot` of the tiles of T rows that the experts' rows and the rows behind the last expert's make, in order.  Called by whole wavefronts.
 __device__ inline mx4_rows mx4_find(const int32_t* __restrict__ offsets, int E, int R, int T, int slot)
 {
     const int lane = threadIdx.x & 63;
     int before = 0, end = 0;                              // tiles and last row of the experts so far
     for (int e0 = 0; e0 <= E; e0 += 64) {
-        const int e = e0 + lane;
-        int last = e < E ? min(max(offsets[e + 1], 0), R) : R;
-        if (e > E) last = 0;
-        last = max(last, end);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {                // running maximum
-            const int o = __shfl_up(last, d, 64);
-            if (lane >= d) last = max(last, o);
-        }
-        int first = __shfl_up(last, 1, 64);
-        if (lane == 0) first = end;
-        const int tiles = e <= E ? (last - first + T - 1) / T : 0;
-        int sum = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += o;
-        }
+        const mx4_span s = mx4_spans(offsets, E, R, e0, lane, end);
+        const int tiles = (s.last - s.first + T - 1) / T, sum = wave_scan_add(tiles);
         const uint64_t has = __ballot(before + sum > slot);
         if (has) {
             const int at = __ffsll((unsigned long long)has) - 1;
-            const int f = __shfl(first, at, 64), l = __shfl(last, at, 64), in = slot - (before + __shfl(sum - tiles, at, 64));
-            const int start = __builtin_amdgcn_readfirstlane(f + in * T), rest = __builtin_amdgcn_readfirstlane(l) - start;
-            return {__builtin_amdgcn_readfirstlane(e0 + at), start, rest < T ? rest : T};
+            const int f = __builtin_amdgcn_readlane(s.first, at), l = __builtin_amdgcn_readlane(s.last, at);
+            const int start = f + (slot - (before + __builtin_amdgcn_readlane(sum - tiles, at))) * T;
+            return {e0 + at, start, min(l - start, T)};
         }
-        before += __builtin_amdgcn_readfirstlane(__shfl(sum, 63, 64));
-        end = __builtin_amdgcn_readfirstlane(__shfl(last, 63, 64));
+        before += __builtin_amdgcn_readlane(sum, 63);
+        end = __builtin_amdgcn_readlane(s.last, 63);
     }
     return {0, 0, 0};
 }

@@ -4,15 +4,16 @@
 
 namespace ss {
 
-// A workgroup of four wavefronts takes FW fragments of 32 channels and a tile of 32 TB token rows.  The wavefronts share out the units of
+// A workgroup of four wavefronts takes FW fragments of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the units of
 // the row; operands go from global memory straight into registers, DEPTH units ahead.
 template <int FW, int TB, int DEPTH, bool GROUPED>
 __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
 {
-    __shared__ __attribute__((aligned(16))) float part[4][FW * TB][16][64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-    mx4_rows t = {0, (int)blockIdx.y * 32 * TB, min(32 * TB, c.R - (int)blockIdx.y * 32 * TB)};
-    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 32 * TB, blockIdx.y);
+    constexpr int ACC = FW * TB * 2;                     // blocks of 16 x 16
+    __shared__ __attribute__((aligned(16))) float part[4][ACC][4][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    mx4_rows t = {0, (int)blockIdx.y * 16 * TB, min(16 * TB, c.R - (int)blockIdx.y * 16 * TB)};
+    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 16 * TB, blockIdx.y);
     if (t.count <= 0) return;
     const bool none = GROUPED && t.expert == c.E;
     const int f0 = blockIdx.x * FW;
@@ -25,19 +26,19 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
     }
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
-        const int64_t row = t.first + min(32 * b + n, t.count - 1);
-        xv[b] = c.codes + row * c.U * MX_UNITB + h * 64;
-        xm[b] = c.scales + row * MX_UNITS + h * 4;
+        const int64_t row = t.first + min(16 * b + n, t.count - 1);
+        xv[b] = c.codes + row * c.U * MX_UNITB + q * 32;
+        xm[b] = c.scales + row * MX_UNITS + q * 2;
     }
-    struct Unit { v4i w[FW][4], x[TB][4]; int sw[FW], sx[TB]; };
+    struct Unit { v4i w[FW][4], x[TB][2]; int sw[FW], sx[TB]; };
     Unit ring[DEPTH];
-    v16f acc[FW][TB];
+    v4f acc[FW][2][TB];
 #pragma unroll
     for (int f = 0; f < FW; ++f)
 #pragma unroll
-        for (int b = 0; b < TB; ++b)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[f][b][i] = 0.0f;
+            for (int b = 0; b < TB; ++b) acc[f][h][b] = v4f{0, 0, 0, 0};
     auto load = [&](Unit& r, int u) __attribute__((always_inline)) {
 #pragma unroll
         for (int f = 0; f < FW; ++f) {
@@ -48,17 +49,17 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
 #pragma unroll
         for (int b = 0; b < TB; ++b) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) r.x[b][s] = *reinterpret_cast<const v4i*>(xv[b] + (int64_t)u * MX_UNITB + s * 16);
-            r.sx[b] = *reinterpret_cast<const int*>(xm[b] + (int64_t)u * c.R * MX_UNITS);
+            for (int s = 0; s < 2; ++s) r.x[b][s] = *reinterpret_cast<const v4i*>(xv[b] + (int64_t)u * MX_UNITB + s * 16);
+            r.sx[b] = *reinterpret_cast<const uint16_t*>(xm[b] + (int64_t)u * c.R * MX_UNITS);
         }
     };
     auto multiply = [&](const Unit& r) __attribute__((always_inline)) {
         unroll<4>([&](auto s) __attribute__((always_inline)) {
-            constexpr int S = decltype(s)::value;
+            constexpr int T = decltype(s)::value >> 1, H = decltype(s)::value & 1;
 #pragma unroll
             for (int f = 0; f < FW; ++f)
 #pragma unroll
-                for (int b = 0; b < TB; ++b) acc[f][b] = mx4_mma<S>(r.w[f][S], r.x[b][S], acc[f][b], r.sw[f], r.sx[b]);
+                for (int b = 0; b < TB; ++b) acc[f][H][b] = mx4_mma<2 * H + T, T>(r.w[f][2 * T + H], r.x[b][T], acc[f][H][b], r.sw[f], r.sx[b]);
         });
     };
     const int mine = none ? 0 : (c.U - wave + 3) / 4;           // units wave, wave + 4, ...
@@ -74,45 +75,34 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
 #pragma unroll
     for (int f = 0; f < FW; ++f)
 #pragma unroll
-        for (int b = 0; b < TB; ++b)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[wave][f * TB + b][i][lane] = acc[f][b][i];
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[wave][(f * TB + b) * 2 + h][i][lane] = acc[f][h][b][i];
     __syncthreads();
-    // wavefront w adds sums 4 w .. 4 w + 3 of every lane, in the order of the wavefronts
+    // A thread adds two neighbouring channels of a row, in the order of the wavefronts.
+    for (int i = threadIdx.x; i < FW * TB * 256; i += 256) {
+        const int row = (i >> 4) & 15, pair = i & 15, f = i / (256 * TB), b = (i >> 8) % TB, ch = (f0 + f) * MX_FRAG + 2 * pair;
+        if (16 * b + row >= t.count) continue;
+        const int a = (f * TB + b) * 2 + ((pair >> 1) & 1), e = 2 * (pair & 1), l = 16 * (pair >> 2) + row;
+        float v[2];
 #pragma unroll
-    for (int f = 0; f < FW; ++f)
-#pragma unroll
-        for (int b = 0; b < TB; ++b) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float(*p)[FW * TB][16][64] = part;
-                v[e] = ((p[0][f * TB + b][4 * wave + e][lane] + p[1][f * TB + b][4 * wave + e][lane]) + p[2][f * TB + b][4 * wave + e][lane]) +
-                       p[3][f * TB + b][4 * wave + e][lane];
-            }
-            const int tok = 32 * b + n, ch = (f0 + f) * 32 + 16 * h + 4 * wave;      // packed channel
-            if (tok >= t.count || f0 + f >= c.frags) continue;
-            uint16_t* const row = c.Y + (int64_t)(t.first + tok) * c.ldy;
-            if (c.gated) {
-                const uint32_t w = pack_bf16x2(mx4_gate(v[0], v[1]), mx4_gate(v[2], v[3]));
-                const int o = ch >> 1;
-                if (o < c.O) row[o] = (uint16_t)w;
-                if (o + 1 < c.O) row[o + 1] = (uint16_t)(w >> 16);
-            } else {
-                const uint32_t w[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                if (ch + 4 <= c.O) *reinterpret_cast<piece8_t*>(row + ch) = piece8_t{w[0], w[1]};
-                else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (ch + e < c.O) row[ch + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-                }
-            }
+        for (int j = 0; j < 2; ++j) v[j] = ((part[0][a][e + j][l] + part[1][a][e + j][l]) + part[2][a][e + j][l]) + part[3][a][e + j][l];
+        uint16_t* const y = c.Y + (int64_t)(t.first + 16 * b + row) * c.ldy;
+        if (c.gated) {
+            if ((ch >> 1) < c.O) y[ch >> 1] = (uint16_t)pack_bf16x2(mx4_gate(v[0], v[1]), 0.0f);
+        } else {
+            const uint32_t w = pack_bf16x2(v[0], v[1]);
+            if (ch + 2 <= c.O) *reinterpret_cast<piece4_t*>(y + ch) = w;
+            else if (ch < c.O) y[ch] = (uint16_t)w;
         }
+    }
 }
 
 template <bool GROUPED> static ss_status launch_mx4_stream(const mx4_call& c, int64_t tiles, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_mx4_stream<1, 1, 4, GROUPED>), dim3((uint32_t)c.frags, (uint32_t)tiles), dim3(256), 0, stream, c);
+    hipLaunchKernelGGL((k_mx4_stream<1, 2, 4, GROUPED>), dim3((uint32_t)c.frags, (uint32_t)tiles), dim3(256), 0, stream, c);
     return launch_status();
 }
 

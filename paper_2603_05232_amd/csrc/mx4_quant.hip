@@ -123,22 +123,27 @@ __global__ __launch_bounds__(256) void k_mx4_dequant(const uint8_t* __restrict__
     }
 }
 
-// one workgroup per fragment and unit: thread (step, lane) moves one lane's 16 bytes, the first 64 threads the scale words
+// one workgroup per fragment and unit: thread (step, half, lane) moves one lane's 16 bytes, the first 64 threads the scale words
 __global__ __launch_bounds__(256) void k_mx4_pack(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t all_rows, int U,
                                                   bool gated, int64_t frags, uint8_t* __restrict__ w_vals, uint8_t* __restrict__ w_meta)
 {
     const int u = blockIdx.x % U;
-    const int64_t f = blockIdx.x / U, expert = f / frags;
-    const int s = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
-    const int64_t c = (f - expert * frags) * MX_FRAG + mx4_channel(lane & 31);
-    const bool there = c < rows;
-    const int64_t row = expert * rows + (gated ? (c & 1) * (rows >> 1) + (c >> 1) : c);
+    const int64_t f = blockIdx.x / U, expert = f / frags, c0 = (f - expert * frags) * MX_FRAG;
+    const int t = threadIdx.x >> 7, half = (threadIdx.x >> 6) & 1, n = threadIdx.x & 15, q = (threadIdx.x >> 4) & 3;
+    auto row_of = [&](int64_t c) { return expert * rows + (gated ? (c & 1) * (rows >> 1) + (c >> 1) : c); };
+    const int64_t c = c0 + mx4_channel(half, n);
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (there) v = *reinterpret_cast<const uint4*>(codes + (row * U + u) * MX_UNITB + (4 * h + s) * 16);
+    if (c < rows) v = *reinterpret_cast<const uint4*>(codes + (row_of(c) * U + u) * MX_UNITB + (2 * q + t) * 16);
     reinterpret_cast<uint4*>(w_vals + (f * U + u) * MX_FRAGB)[threadIdx.x] = v;
-    if (s == 0)
-        reinterpret_cast<uint32_t*>(w_meta + (f * U + u) * MX_FRAGS)[lane] =
-            there ? *reinterpret_cast<const uint32_t*>(scales + ((int64_t)u * all_rows + row) * MX_UNITS + 4 * h) : 0u;
+    if (threadIdx.x < 64) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t ch = c0 + mx4_channel(h, n);
+            if (ch < rows) w |= (uint32_t)*reinterpret_cast<const uint16_t*>(scales + ((int64_t)u * all_rows + row_of(ch)) * MX_UNITS + 2 * q) << (16 * h);
+        }
+        reinterpret_cast<uint32_t*>(w_meta + (f * U + u) * MX_FRAGS)[threadIdx.x] = w;
+    }
 }
 
 }  // namespace ss

@@ -1,8 +1,7 @@
 // Products of microscaled 4-bit operands on tiles of 256 channels x 256 token rows (mx4_gemm, mx4_grouped_gemm: many rows).
 //
-// Persistent workgroups of eight wavefronts, two per SIMD, of 128 channels x 64 rows = 8 x 4 blocks of the 16x16x128 instruction.  A unit of 256
-// values is two steps; lane (n, q) = (l & 15, l >> 4) takes block 2 q + t of its row in step t, so that its two scales lie side by side
-// in one 16-bit read, whose byte the instruction selects.
+// Persistent workgroups of eight wavefronts, two per SIMD, of 128 channels x 64 rows = 8 x 4 blocks of the 16x16x128 instruction; a unit of 256
+// values is two steps.
 //
 // LDS: weights in three slots of a step (16 KB), token rows in three slots of a unit (32 KB), scales of two units.  Direct loads fill
 // them; those of a step are spread from one meeting of the workgroup to the next.  The workgroup meets once a step, behind
@@ -37,15 +36,9 @@ __device__ inline void xt_load4(const uint8_t* base, uint32_t lane_off, uint32_t
 // time (rows 0 .. 3, 12 .. 15 of the one, 4 .. 11 of the other), whose chunks 2 apart would meet on the same banks
 __device__ inline int xt_place(int c) { return (c & 4) | ((c & 1) << 1) | ((c >> 1) & 1); }      // its own inverse
 
-template <int T> __device__ __forceinline__ v4f mx4_mma16(v4i a, v4i b, v4f c, int sa, int sb)
-{
-    const v8i a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, T, sa, T, sb);
-}
-
-// acc[a][b][i] of lane (n, q), a = 4 hh + f: packed channel 32 f + 16 (q & 1) + 8 hh + 4 (q >> 1) + i, row 16 b + n of a sub-tile of 128 x 64 of which
-// rows_left rows and cols_left columns of Y exist.  Staged 16 rows at a time through the wavefront's own 4 KB, so that every store
-// writes whole pieces of Y's rows.  All loads in flight are waited for before the first store (the wait counter counts both).
+// acc[2 f + hh][b][i] of lane (n, q): packed channel 32 f + 8 q + 4 hh + i, row 16 b + n of a sub-tile of 128 x 64 of which rows_left rows and cols_left
+// columns of Y exist.  Staged 16 rows at a time through the wavefront's own 4 KB, so that every store writes whole pieces of Y's rows.
+// All loads in flight are waited for before the first store (the wait counter counts both).
 template <bool GATED>
 __device__ inline void xt_store(const v4f (&acc)[8][4], bool zeros, uint16_t* __restrict__ Y_sub, uint32_t ldy, int rows_left, int cols_left, uint8_t* stage)
 {
@@ -55,16 +48,14 @@ __device__ inline void xt_store(const v4f (&acc)[8][4], bool zeros, uint16_t* __
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
 #pragma unroll
-        for (int a = 0; a < 8; ++a) {
-            const int f = a & 3, hh = a >> 2;
-            const v4f v = zeros ? v4f{0, 0, 0, 0} : acc[a][b];
-            if constexpr (GATED) {
-                const int chunk = 2 * f + (q & 1);
-                *reinterpret_cast<uint32_t*>(stage + n * ROW + ((chunk ^ (n & 7)) << 4) + 8 * hh + 4 * (q >> 1)) = pack_bf16x2(mx4_gate(v[0], v[1]), mx4_gate(v[2], v[3]));
-            } else {
-                const int chunk = 4 * f + 2 * (q & 1) + hh;
-                *reinterpret_cast<uint2*>(stage + n * ROW + ((chunk ^ n) << 4) + 8 * (q >> 1)) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-            }
+        for (int f = 0; f < 4; ++f) {
+            const v4f v = zeros ? v4f{0, 0, 0, 0} : acc[2 * f][b], w = zeros ? v4f{0, 0, 0, 0} : acc[2 * f + 1][b];
+            if constexpr (GATED)
+                *reinterpret_cast<uint2*>(stage + n * ROW + (((2 * f + (q >> 1)) ^ (n & 7)) << 4) + 8 * (q & 1)) =
+                    make_uint2(pack_bf16x2(mx4_gate(v[0], v[1]), mx4_gate(v[2], v[3])), pack_bf16x2(mx4_gate(w[0], w[1]), mx4_gate(w[2], w[3])));
+            else
+                *reinterpret_cast<uint4*>(stage + n * ROW + (((4 * f + q) ^ n) << 4)) =
+                    make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]));
         }
         if (b == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -107,25 +98,11 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         if (wave == 0) {
             int tiles = 0, end = 0;
             for (int e0 = 0; e0 < c.E; e0 += 64) {
-                const int e = e0 + lane;
-                int last = e < c.E ? min(max(c.offsets[e + 1], 0), c.R) : 0;
-                last = max(last, end);
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(last, d, 64);
-                    if (lane >= d) last = max(last, o);
-                }
-                int first = __shfl_up(last, 1, 64);
-                if (lane == 0) first = end;
-                int sum = (last - first + BT - 1) / BT * tiles_o;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(sum, d, 64);
-                    if (lane >= d) sum += o;
-                }
-                if (e < c.E) { tile_end[e] = tiles + sum; row_end[e] = last; }
-                tiles += __shfl(sum, 63, 64);
-                end = __shfl(last, 63, 64);
+                const mx4_span r = mx4_spans(c.offsets, c.E, c.R, e0, lane, end);
+                const int sum = wave_scan_add((r.last - r.first + BT - 1) / BT * tiles_o);
+                if (e0 + lane < c.E) { tile_end[e0 + lane] = tiles + sum; row_end[e0 + lane] = r.last; }
+                tiles += __builtin_amdgcn_readlane(sum, 63);
+                end = __builtin_amdgcn_readlane(r.last, 63);
             }
         }
         __syncthreads();
@@ -163,81 +140,85 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         return true;
     };
 
-    // Sources of the direct loads: weights of fragment `wave`, token rows 8 (8 i + wave) .. + 7, scales of fragment `wave` and of rows 32 wave .. + 31.
-    const uint8_t *av = nullptr, *am = nullptr, *bv = nullptr, *bm = nullptr;
+    // Sources of the direct loads, at the unit that is requested next: weights and scales of fragment `wave`, token rows 8 (8 i + wave) .. + 7, scales of
+    // rows 64 (wave / 2) + 16 b + 8 (wave % 2) .. + 7, as [row & 15][half of a unit][b 4] words.
+    struct Weights { const uint8_t *v, *m; } pa;
+    struct Rows { const uint8_t *v, *m; } pb;
     uint32_t boff[4], bmoff = 0;
-    auto set_weights = [&](const Tile& t) {
+    auto weights_of = [&](const Tile& t) -> Weights {
         const int64_t at = ((int64_t)(GROUPED && t.expert == c.E ? 0 : t.expert) * c.frags + min(t.o * 8 + wave, c.frags - 1)) * U;
-        av = c.w_vals + at * MX_FRAGB;
-        am = c.w_meta + at * MX_FRAGS;
+        return {c.w_vals + at * MX_FRAGB, c.w_meta + at * MX_FRAGS};
     };
     auto set_rows = [&](const Tile& t) {
         const int ln = fresh_lane();
-        bv = c.codes + (int64_t)t.first * U * MX_UNITB;
-        bm = c.scales + (int64_t)t.first * MX_UNITS;
+        pb = {c.codes + (int64_t)t.first * U * MX_UNITB, c.scales + (int64_t)t.first * MX_UNITS};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 8 * (8 * i + wave) + (ln >> 3);
             boff[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)(U * MX_UNITB) + xt_place((ln & 7) ^ swz(row)) * 16;
         }
-        bmoff = (uint32_t)min(32 * wave + (ln >> 1), t.rows - 1) * MX_UNITS + (ln & 1) * 4;
+        bmoff = (uint32_t)min((wave >> 1) * 64 + 16 * (ln & 3) + (wave & 1) * 8 + (ln >> 3), t.rows - 1) * MX_UNITS + (ln & 4);
     };
+    const int64_t mb_next = (int64_t)c.R * MX_UNITS;
     const uint32_t lane16 = lane * 16, lane4 = lane * 4;
     const uint32_t a_wave = lds0 + wave * 2048, b_wave = lds0 + XT_B_OFF + wave * 1024, ma_wave = lds0 + XT_MA_OFF + wave * 256, mb_wave = lds0 + XT_MB_OFF + wave * 256;
-    auto load_a = [&](int u, int t, int j, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
-        xt_load16(av + ((uint32_t)u * MX_FRAGB + (2 * j + t) * 1024), lane16, a_wave + slot + j * 1024, more);
+    auto load_a = [&](int t, int j, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
+        xt_load16(pa.v + (2 * t + j) * 1024, lane16, a_wave + slot + j * 1024, more);
     };
-    auto load_ma = [&](int u, uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load4(am + (uint32_t)u * MX_FRAGS, lane4, ma_wave + slot, more); };
-    auto load_b = [&](int u, int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
-        xt_load16(bv + (uint32_t)u * MX_UNITB, boff[i], b_wave + slot + i * 8192, more);
-    };
-    auto load_mb = [&](int u, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
-        xt_load4(bm + (int64_t)u * c.R * MX_UNITS, bmoff, mb_wave + slot, more);
-    };
+    auto load_ma = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load4(pa.m, lane4, ma_wave + slot, more); };
+    auto load_b = [&](int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
+    auto load_mb = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load4(pb.m, bmoff, mb_wave + slot, more); };
+    auto next_a = [&]() __attribute__((always_inline)) { pa.v += MX_FRAGB; pa.m += MX_FRAGS; };
+    auto next_b = [&]() __attribute__((always_inline)) { pb.v += MX_UNITB; pb.m += mb_next; };
 
     // LDS offsets of this lane's operand reads
-    const uint32_t ra = wo * 8192 + (q & 1) * 1024 + ((q >> 1) * 32 + n) * 16;
-    const uint32_t rma = XT_MA_OFF + wo * 1024 + ((q >> 1) * 32 + n) * 4 + 2 * (q & 1);
+    const uint32_t ra = wo * 8192 + lane * 16;
+    const uint32_t rma = XT_MA_OFF + wo * 1024 + lane * 4;
     const uint32_t rb = XT_B_OFF + (wt * 64 + n) * ROWB + ((xt_place(2 * q) ^ swz(n)) << 4);
-    const uint32_t rmb = XT_MB_OFF + (wt * 64 + n) * MX_UNITS + 2 * q;
+    const uint32_t rmb = XT_MB_OFF + wt * 512 + n * 32 + (q >> 1) * 16;
+    const uint32_t mb_shift = 16 * (q & 1);               // this lane's two bytes of a word of four scales
 
     uint32_t a0 = 0, a1 = XT_A, a2 = 2 * XT_A;            // slots of this step's weights and the next two's
     uint32_t b0 = 0, b1 = XT_B, b2 = 2 * XT_B;            // of this unit's token rows and the next two's
     uint32_t m0 = 0, m1 = XT_M;                           // of this unit's scales and the next one's
     Tile now, next;
     if (!tile_of(0, now)) return;
-    set_weights(now);
+    pa = weights_of(now);
     set_rows(now);
     constexpr uint32_t ALL = ~0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_b(0, i, b0, ALL);
-    load_ma(0, m0, ALL);
-    load_mb(0, m0, ALL);
-    load_a(0, 0, 0, a0, ALL);
-    load_a(0, 0, 1, a0, ALL);
-    load_a(0, 1, 0, a1, ALL);
-    load_a(0, 1, 1, a1, ALL);
+    for (int i = 0; i < 4; ++i) load_b(i, b0, ALL);
+    load_ma(m0, ALL);
+    load_mb(m0, ALL);
+    load_a(0, 0, a0, ALL);
+    load_a(0, 1, a0, ALL);
+    load_a(1, 0, a1, ALL);
+    load_a(1, 1, a1, ALL);
+    next_a();
+    next_b();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_b(1, i, b1, ALL);
-    load_ma(1, m1, ALL);
-    load_mb(1, m1, ALL);
-    load_a(1, 0, 0, a2, ALL);
-    load_a(1, 0, 1, a2, ALL);
+    for (int i = 0; i < 4; ++i) load_b(i, b1, ALL);
+    load_ma(m1, ALL);
+    load_mb(m1, ALL);
+    load_a(0, 0, a2, ALL);
+    load_a(0, 1, a2, ALL);
+    next_b();
     wait_vmcnt<10>();
     wg_barrier();
 
-    int ua = 1, ub = 2;                                   // units that the next requests of weights and of token rows are for
-    uint32_t more_a = ALL, more_b = ALL;                // none where there is no next tile
+    uint32_t more_a = ALL, more_b = ALL;                  // none where there is no next tile
+    Weights then = pa;                                    // of the next tile
     int have = 1;
     v4f acc[8][4];
     v4i va[8], vb[4];
-    int sa[8], sb[4];
+    int sa[4], sb[4];
+    v4i wb;                                               // the next unit's token scales as they were read
     auto rd = [&](uint32_t off) __attribute__((always_inline)) -> v4i { return *reinterpret_cast<const v4i*>(smem + off); };
-    auto rd2 = [&](uint32_t off) __attribute__((always_inline)) -> int { return *reinterpret_cast<const uint16_t*>(smem + off); };
-    auto read_a = [&](int a, uint32_t slot) __attribute__((always_inline)) { va[a] = rd(ra + slot + (a & 3) * 2048 + (a >> 2) * 256); };
-    auto read_sa = [&](int a, uint32_t slot) __attribute__((always_inline)) { sa[a] = rd2(rma + slot + (a & 3) * 256 + (a >> 2) * 64); };
+    auto read_a = [&](int a, uint32_t slot) __attribute__((always_inline)) { va[a] = rd(ra + slot + a * 1024); };
+    auto read_sa = [&](int f, uint32_t slot) __attribute__((always_inline)) { sa[f] = *reinterpret_cast<const int*>(smem + rma + slot + f * 256); };
     auto read_b = [&](int b, int t, uint32_t slot) __attribute__((always_inline)) { vb[b] = rd(((rb + slot) ^ (t * 32)) + b * 2048); };
-    auto read_sb = [&](int b, uint32_t slot) __attribute__((always_inline)) { sb[b] = rd2(rmb + slot + b * 128); };
+    auto read_sb = [&](uint32_t slot) __attribute__((always_inline)) { wb = rd(rmb + slot); };
+    auto set_sb = [&](int b) __attribute__((always_inline)) { sb[b] = (int)((uint32_t)wb[b] >> mb_shift); };
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int a = 0; a < 8; ++a)
@@ -252,11 +233,11 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         unroll<32>([&](auto i_c) __attribute__((always_inline)) {
             constexpr int i = decltype(i_c)::value;
             constexpr int a = (i >> 1) & 7, b = 2 * (i >> 4) + (i & 1);
-            acc[a][b] = mx4_mma16<T>(va[a], vb[b], acc[a][b], sa[a], sb[b]);
+            acc[a][b] = mx4_mma<2 * (a & 1) + T, T>(va[a], vb[b], acc[a][b], sa[a >> 1], sb[b]);
             __builtin_amdgcn_sched_barrier(0);
             if (i == 0 || i == 2) {                       // these registers were in use until the end of the last step
                 read_b(2 + i / 2, T, b0);
-                if (T == 0) read_sb(2 + i / 2, m0);
+                if (T == 0) set_sb(2 + i / 2);
             }
             if (i == 1) __builtin_amdgcn_s_setprio(0);
             if (i == 16) __builtin_amdgcn_s_setprio(1);
@@ -266,27 +247,28 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
                 wg_barrier();
             }
             if constexpr (T == 1) {
-                if (i == 4) load_b(ub, 2, b2, more_b);
-                if (i == 9) load_b(ub, 3, b2, more_b);
+                if (i == 4) load_b(2, b2, more_b);
+                if (i == 9) load_b(3, b2, more_b);
             }
-            if (i == 15) load_a(ua, 1 - T, 0, a0, more_a);
-            if (i == (T == 0 ? 18 : 20)) load_a(ua, 1 - T, 1, a0, more_a);
+            if (i == 15) load_a(1 - T, 0, a0, more_a);
+            if (i == (T == 0 ? 18 : 20)) load_a(1 - T, 1, a0, more_a);
             if (i == (T == 0 ? 21 : 25)) {
-                if (T == 0) load_mb(ub, m0, more_b);
-                else load_ma(ua, m0, more_a);
+                if (T == 0) load_mb(m0, more_b);
+                else load_ma(m0, more_a);
             }
             if constexpr (T == 0) {
-                if (i == 24) load_b(ub, 0, b2, more_b);
-                if (i == 27) load_b(ub, 1, b2, more_b);
+                if (i == 24) load_b(0, b2, more_b);
+                if (i == 27) load_b(1, b2, more_b);
             }
             if (i >= 17 && (i & 1)) {
                 read_a((i - 17) >> 1, a1);
-                if (T == 1) read_sa((i - 17) >> 1, m1);
+                if (T == 1 && (i & 2)) read_sa((i - 19) >> 2, m1);
             }
             if (i == 18 || i == 22) {
                 read_b((i - 18) >> 2, 1 - T, T == 0 ? b0 : b1);
-                if (T == 1) read_sb((i - 18) >> 2, m1);
+                if (T == 1 && i == 18) read_sb(m1);
             }
+            if (T == 1 && i == 31) { set_sb(0); set_sb(1); }
             __builtin_amdgcn_sched_barrier(0);
         });
         const uint32_t w = a0;
@@ -298,26 +280,30 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         }
     };
 #pragma unroll
-    for (int a = 0; a < 8; ++a) { read_a(a, a0); read_sa(a, m0); }
+    for (int a = 0; a < 8; ++a) read_a(a, a0);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) { read_b(b, 0, b0); read_sb(b, m0); }
+    for (int f = 0; f < 4; ++f) read_sa(f, m0);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) read_b(b, 0, b0);
+    read_sb(m0);
+    set_sb(0);
+    set_sb(1);
     clear();
     int round = 0, u = 0, waits = 1;
     for (;;) {
-        if (u == U - 2) {                                 // the token rows' requests go on to the next tile
+        if (u == U - 2) {                                 // the token rows' requests go on to the next tile, the weights' in the second step
             have = __builtin_amdgcn_readfirstlane(tile_of(++round, next) ? 1 : 0);
-            ub = 0;
-            if (have) set_rows(next);
+            if (have) { set_rows(next); then = weights_of(next); }
             more_b = -have;
         }
         step(std::integral_constant<int, 0>{}, waits);
-        if (++ua == U) {                                  // and the weights'
-            ua = 0;
-            if (have) set_weights(next);
-            more_a = -have;
-        }
+        next_a();                                         // without a branch: the products of a step would sink below it
+        const bool wrap = u == U - 2;
+        pa.v = wrap ? then.v : pa.v;
+        pa.m = wrap ? then.m : pa.m;
+        more_a = wrap ? (uint32_t)-have : more_a;
         step(std::integral_constant<int, 1>{}, waits);
-        ++ub;
+        next_b();
         waits = 1;
         if (++u < U) continue;
         // The tile's results.  b2 is free, nothing is requested into it before the next meeting.
