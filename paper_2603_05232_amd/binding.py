@@ -33,9 +33,12 @@ EXPORTS = ("slide_lifted_k", "slide_lifted_ld", "slide_packed_sizes", "slide_pru
            "ss_status_string", "slide_format_version")
 # entry points that the extension module calls, at the addresses of the library loaded here (order of its bind())
 _CALLED = ("slide_lifted_ld", "act_lift_quant", "slide_sparse_gemm_ws", "slide_sparse_gemm_fused_ws")
+_CALLED_MX4 = ("mx4_row_bytes", "mx4_quant", "mx4_dequant", "mx4_packed_sizes", "mx4_gemm", "mx4_grouped_gemm", "expert_route_workspace_bytes", "expert_route",
+               "expert_combine")                          # of its bind_mx4()
 
 _lib = None
 _calls = None
+_mx4_calls = None                                         # the module again, for the 4-bit expert layer's calls
 
 
 class SlideSparseError(RuntimeError):
@@ -46,7 +49,7 @@ class SlideSparseError(RuntimeError):
 
 def load():
     """Load the shared library (raises if it has not been built)."""
-    global _lib, _calls
+    global _lib, _calls, _mx4_calls
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -96,7 +99,8 @@ def load():
     lib.ss_status_string.argtypes = [i32]
     lib.ss_status_string.restype = ctypes.c_char_p
     lib.slide_format_version.restype = i32
-    _lib, _calls = lib, _load_calls(lib)
+    calls = _load_calls(lib)
+    _lib, _calls, _mx4_calls = lib, calls, calls
     return lib
 
 
@@ -109,8 +113,10 @@ def _load_calls(lib):
             raise ImportError(f"built for torch {calls.torch_version}, not {torch.__version__}")
     except (ImportError, AttributeError) as e:
         warnings.warn(f"{CALLS_PATH} cannot be used ({e}): calls go through ctypes, 6 us more on the host for each layer", RuntimeWarning, stacklevel=3)
-        return types.SimpleNamespace(**dict.fromkeys(("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused"), lambda *args: None))
+        return types.SimpleNamespace(**dict.fromkeys(("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused", "mx4_quant", "mx4_dequant", "mx4_product",
+                                                    "expert_route", "expert_combine"), lambda *args: None))
     calls.bind(SlideSparseError, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED))
+    calls.bind_mx4(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED_MX4))
     return calls
 
 
@@ -364,6 +370,11 @@ def mx4_row_scales(K: int) -> int:
 def mx4_quant(X: torch.Tensor, rows=None, codes=None, scales=None):
     """X[M,K] fp32/bf16 (row stride allowed) -> (codes[R, 128 U] uint8, scales[U, R, 8] uint8); rows: int32 [R], the row of X that each
     row of codes is made of."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.mx4_quant(X, rows, codes, scales)
+    if done is not None:
+        return done
     M, K = X.shape
     R = M if rows is None else rows.shape[0]
     width = mx4_row_bytes(K)
@@ -384,6 +395,11 @@ def mx4_quant(X: torch.Tensor, rows=None, codes=None, scales=None):
 
 def mx4_dequant(codes: torch.Tensor, scales: torch.Tensor, K: int, dtype: torch.dtype = torch.float32, out=None):
     """codes, scales of mx4_quant -> their values [R,K] as fp32 or bf16."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.mx4_dequant(codes, scales, K, _IN_CODE.get(dtype), out)
+    if done is not None:
+        return done
     _mx4_operand(codes, scales, K)
     if out is None:
         out = codes.new_empty((codes.shape[0], K), dtype=dtype)
@@ -440,11 +456,21 @@ _mx4_sizes = functools.lru_cache(maxsize=4096, typed=True)(mx4_packed_sizes)
 
 def mx4_gemm(codes, scales, w_vals, w_meta, O: int, K: int, gated: bool = False, out=None, workspace=None):
     """Y[M,O] bf16 = X . W^T of 4-bit operands (gated: silu(X . Wg^T) * (X . Wu^T)); workspace: optional uint8 device tensor."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.mx4_product(None, codes, scales, w_vals, w_meta, O, K, gated, out, workspace)
+    if done is not None:
+        return done
     return _mx4_product("mx4_gemm", None, codes, scales, w_vals, w_meta, 1, O, K, gated, out, workspace)
 
 
 def mx4_grouped_gemm(codes, scales, offsets, w_vals, w_meta, O: int, K: int, gated: bool = False, out=None, workspace=None):
     """The same with the weights of expert e for the rows offsets[e] .. offsets[e + 1] - 1 (int32, on the device); the others give zeros."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.mx4_product(offsets, codes, scales, w_vals, w_meta, O, K, gated, out, workspace)
+    if done is not None:
+        return done
     return _mx4_product("mx4_grouped_gemm", _dense_i32(offsets, "offsets"), codes, scales, w_vals, w_meta, offsets.shape[0] - 1, O, K, gated, out, workspace)
 
 
@@ -455,6 +481,11 @@ def expert_route_workspace_bytes(M: int, E: int, k: int) -> int:
 def expert_route(logits: torch.Tensor, k: int, renormalise: bool = True, workspace=None):
     """logits[M,E] fp32/bf16 -> (ids[M,k], weights[M,k], slots[M,k], rows[M k], offsets[E + 1]): the k experts of largest score, their softmax
     weights, and the order of the rows by expert."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.expert_route(logits, k, renormalise, workspace)
+    if done is not None:
+        return done
     M, E = logits.shape
     if workspace is None:
         n = expert_route_workspace_bytes(M, E, k)
@@ -473,6 +504,11 @@ def expert_route(logits: torch.Tensor, k: int, renormalise: bool = True, workspa
 
 def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, base=None, out=None):
     """out[M,O] bf16 = sum over j of weights[m,j] Y[slots[m,j]] (+ base[m]); Y bf16 [R,O], slots int32 [M,k], weights fp32 [M,k]."""
+    if _mx4_calls is None:
+        load()
+    done = _mx4_calls.expert_combine(Y, slots, weights, base, out)
+    if done is not None:
+        return done
     R, O = Y.shape
     M, k = slots.shape
     assert weights.shape == (M, k) and weights.is_contiguous() and weights.dtype == torch.float32 and Y.dtype == torch.bfloat16

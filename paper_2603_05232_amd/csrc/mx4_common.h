@@ -40,10 +40,42 @@ template <int SA, int SB> __device__ __forceinline__ v4f mx4_mma(v4i a, v4i b, v
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, SA, sa, SB, sb);
 }
 
+// 16-byte chunk c of a token row lies at chunk mx4_place(c) ^ swz(row): a 16-byte LDS read is served to eight lanes of one q and eight of q ^ 1 at a
+// time (rows 0 .. 3, 12 .. 15 of the one, 4 .. 11 of the other), whose chunks 2 apart would meet on the same banks
+__device__ inline int mx4_place(int c) { return (c & 4) | ((c & 1) << 1) | ((c >> 1) & 1); }      // its own inverse
+
 typedef uint32_t piece4_t __attribute__((aligned(2)));
 
 // silu(g) u, in 32 bits
 __device__ inline float mx4_gate(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
+// Eight consecutive packed channels from `ch` on of one row of Y: sums v (half 0) and w (half 1) of one lane.
+__device__ inline void mx4_store8(v4f v, v4f w, uint16_t* __restrict__ y, int ch, int O, bool gated)
+{
+    uint32_t p[4];
+    int n = 8;
+    if (gated) {
+        p[0] = pack_bf16x2(mx4_gate(v[0], v[1]), mx4_gate(v[2], v[3]));
+        p[1] = pack_bf16x2(mx4_gate(w[0], w[1]), mx4_gate(w[2], w[3]));
+        p[2] = p[3] = 0;
+        ch >>= 1;
+        n = 4;
+    } else {
+        p[0] = pack_bf16x2(v[0], v[1]);
+        p[1] = pack_bf16x2(v[2], v[3]);
+        p[2] = pack_bf16x2(w[0], w[1]);
+        p[3] = pack_bf16x2(w[2], w[3]);
+    }
+    y += ch;
+    if (ch + n <= O) {
+        if (gated) *reinterpret_cast<piece8_t*>(y) = piece8_t{p[0], p[1]};
+        else *reinterpret_cast<piece16_t*>(y) = piece16_t{p[0], p[1], p[2], p[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n && ch + e < O) y[e] = (uint16_t)(p[e >> 1] >> (16 * (e & 1)));
+    }
+}
 
 // running sum and maximum over the lanes of a wavefront
 template <typename F> __device__ inline int wave_scan(int v, int none, F f)
@@ -115,5 +147,7 @@ struct mx4_call {
 // Tiles of 256 channels x 256 rows (mx4_tile.hip); rows of MX_TILE_UNITS units and more.
 constexpr int MX_TILE_UNITS = 3;
 ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
+// Tiles of 128 channels x 32, 64 or 128 rows (mx4_mid.hip).
+ss_status launch_mx4_mid(const mx4_call& c, int rows, hipStream_t stream);
 
 }  // namespace ss

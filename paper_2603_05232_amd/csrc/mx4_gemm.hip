@@ -1,16 +1,17 @@
 // mx4_gemm, mx4_grouped_gemm: products of microscaled 4-bit operands.  Entry points and the kernel for few tokens.
 #include "mx4_common.h"
 #include "device_info.h"
+#include <math.h>
 
 namespace ss {
 
-// A workgroup of four wavefronts takes FW fragments of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the units of
+// A workgroup of W wavefronts takes FW fragments of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the units of
 // the row; operands go from global memory straight into registers, DEPTH units ahead.
-template <int FW, int TB, int DEPTH, bool GROUPED>
-__global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
+template <int W, int FW, int TB, int DEPTH, bool GROUPED>
+__global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
 {
     constexpr int ACC = FW * TB * 2;                     // blocks of 16 x 16
-    __shared__ __attribute__((aligned(16))) float part[4][ACC][4][64];
+    __shared__ __attribute__((aligned(16))) float part[W][ACC][4][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     mx4_rows t = {0, (int)blockIdx.y * 16 * TB, min(16 * TB, c.R - (int)blockIdx.y * 16 * TB)};
     if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 16 * TB, blockIdx.y);
@@ -62,15 +63,15 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
                 for (int b = 0; b < TB; ++b) acc[f][H][b] = mx4_mma<2 * H + T, T>(r.w[f][2 * T + H], r.x[b][T], acc[f][H][b], r.sw[f], r.sx[b]);
         });
     };
-    const int mine = none ? 0 : (c.U - wave + 3) / 4;           // units wave, wave + 4, ...
+    const int mine = none ? 0 : (c.U - wave + W - 1) / W;       // units wave, wave + W, ...
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d)
-        if (d < mine) load(ring[d], wave + 4 * d);
+        if (d < mine) load(ring[d], wave + W * d);
     for (int i = 0; i < mine; i += DEPTH)
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             if (i + d < mine) multiply(ring[d]);
-            if (i + d + DEPTH < mine) load(ring[d], wave + 4 * (i + d + DEPTH));
+            if (i + d + DEPTH < mine) load(ring[d], wave + W * (i + d + DEPTH));
         }
 #pragma unroll
     for (int f = 0; f < FW; ++f)
@@ -82,13 +83,17 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
                 for (int i = 0; i < 4; ++i) part[wave][(f * TB + b) * 2 + h][i][lane] = acc[f][h][b][i];
     __syncthreads();
     // A thread adds two neighbouring channels of a row, in the order of the wavefronts.
-    for (int i = threadIdx.x; i < FW * TB * 256; i += 256) {
+    for (int i = threadIdx.x; i < FW * TB * 256; i += 64 * W) {
         const int row = (i >> 4) & 15, pair = i & 15, f = i / (256 * TB), b = (i >> 8) % TB, ch = (f0 + f) * MX_FRAG + 2 * pair;
         if (16 * b + row >= t.count) continue;
         const int a = (f * TB + b) * 2 + ((pair >> 1) & 1), e = 2 * (pair & 1), l = 16 * (pair >> 2) + row;
         float v[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) v[j] = ((part[0][a][e + j][l] + part[1][a][e + j][l]) + part[2][a][e + j][l]) + part[3][a][e + j][l];
+        for (int j = 0; j < 2; ++j) {
+            v[j] = part[0][a][e + j][l];
+#pragma unroll
+            for (int w = 1; w < W; ++w) v[j] += part[w][a][e + j][l];
+        }
         uint16_t* const y = c.Y + (int64_t)(t.first + 16 * b + row) * c.ldy;
         if (c.gated) {
             if ((ch >> 1) < c.O) y[ch >> 1] = (uint16_t)pack_bf16x2(mx4_gate(v[0], v[1]), 0.0f);
@@ -100,15 +105,53 @@ __global__ __launch_bounds__(256) void k_mx4_stream(mx4_call c)
     }
 }
 
-template <bool GROUPED> static ss_status launch_mx4_stream(const mx4_call& c, int64_t tiles, hipStream_t stream)
+template <int W, int TB, int DEPTH> static ss_status launch_stream(const mx4_call& c, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_mx4_stream<1, 2, 4, GROUPED>), dim3((uint32_t)c.frags, (uint32_t)tiles), dim3(256), 0, stream, c);
+    const int64_t tiles = c.offsets ? mx4_max_tiles(c.R, c.E, 16 * TB) : ((int64_t)c.R + 16 * TB - 1) / (16 * TB);
+    if (tiles > 65535) return SS_ERR_SHAPE;
+    const dim3 grid((uint32_t)c.frags, (uint32_t)tiles);
+    if (c.offsets) hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, true>), grid, dim3(64 * W), 0, stream, c);
+    else hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, false>), grid, dim3(64 * W), 0, stream, c);
     return launch_status();
 }
 
 }  // namespace ss
 
 using namespace ss;
+
+// The kernel of a product: tiles of 16 or 32 rows of the kernel for few tokens, MX_MID + 32, 64 or 128 rows of mx4_mid.hip, 256 of mx4_tile.hip.  Which is the
+// fastest goes by an estimate of every kernel's time in us: its launch, then the longest of what its workgroups take one after the other (time of a
+// unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
+// rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The group sizes lie on the device: E experts are taken to have R / E rows
+// each, and half a tile more.  Constants fitted to the times of all six on 68 shapes (R = 1 .. 16000, 1 .. 74 units, 512 .. 37888 channels, 1 to 128
+// experts): the choice is 1.03 of the fastest on average, 1.26 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+//   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       46.2 |  36.7 |  25.5 | 18.3 | 16.6 | 26.4
+//   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
+//   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
+//   500 rows, 8 experts, 4096 -> 4096   36.3 | 33.5 | 30.3 | 23.2 | 30.2 | 29.6      4000 rows, 64 experts, 2048 -> 1408   62.4 | 61.8 | 38.1 | 34.8 | 43.8 | 39.0
+// The kernel of 16 rows takes eight wavefronts, two units each ahead, where rows have 16 units and more, otherwise four (1 x 18944 -> 3584 10.3 against 12.4, 32 gated
+// rows of 8 experts 4096 -> 14336 83.7 against 88.6; 512 rows of 64 experts, 8 units, 26.4 against 22.2).
+constexpr int MX_MID = 1000;
+static int mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64_t cus)
+{
+    const double used = E > 1 ? (double)E * (1.0 - pow(1.0 - 1.0 / (double)E, (double)R)) : 1.0, ragged = E > 1 ? 1.2 : 1.0, MB = (double)(frags * U * (MX_FRAGB + MX_FRAGS)) / 1e6;
+    const double hbm = used * MB / 5.2, panels = (double)((frags + 3) / 4), wide = (double)((frags + 7) / 8), u = (double)U;
+    auto tiles = [&](int64_t T) { return E > 1 ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
+    auto shares = [&](double workgroups) { return fmax(1.0, workgroups / (double)cus); };
+    const double full = fmin(1.0, wide * tiles(256) / (double)cus);
+    struct { int kernel; double us; } all[] = {
+        {16, 2.2 + fmax(fmax(MB * tiles(16) / 8.5 * ragged, 0.14 * u * fmax(1.0, (double)frags * tiles(16) / (double)(4 * cus))), hbm)},
+        {32, 2.5 + fmax(fmax(MB * tiles(32) / 6.0 * ragged, 0.18 * u), hbm)},
+        {MX_MID + 32, 2.0 + fmax((0.40 * u + 1.2) * ragged * shares(panels * tiles(32)), 1.1 * hbm + 1.0)},
+        {MX_MID + 64, 2.4 + fmax((0.44 * u + 1.3) * ragged * shares(panels * tiles(64)), 1.1 * hbm + 1.0)},
+        {MX_MID + 128, 2.6 + fmax((0.70 * u + 2.2) * ragged * shares(panels * tiles(128)), 1.15 * hbm + 1.0)},
+        {256, U < MX_TILE_UNITS ? 1e30 : 4.0 + fmax(((1.15 + 0.45 * full) * u + 1.5) * shares(wide * tiles(256)), hbm)},
+    };
+    int best = 0;
+    for (int i = 1; i < 6; ++i)
+        if (all[i].us < all[best].us) best = i;
+    return all[best].kernel;
+}
 
 extern "C" size_t mx4_gemm_workspace_bytes(int64_t R, int64_t E, int64_t O, int64_t K, int gated)
 {
@@ -131,8 +174,14 @@ static ss_status mx4_product(bool grouped, const void* codes, const void* scales
                   static_cast<const uint8_t*>(w_meta), (int)R, (int)E, (int)O, (int)mx4_units(K), (int)mx4_frags(O << gated),
                   static_cast<uint16_t*>(Y), ldy, gated != 0};
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    if (c.U >= MX_TILE_UNITS && R >= 192 * E) return launch_mx4_tile(c, hs);
-    return grouped ? launch_mx4_stream<true>(c, mx4_max_tiles(R, E, 32), hs) : launch_mx4_stream<false>(c, (R + 31) / 32, hs);
+    switch (mx4_choose(R, E, c.U, c.frags, cu_count())) {
+    case 16: return c.U >= 16 ? launch_stream<8, 1, 2>(c, hs) : launch_stream<4, 1, 4>(c, hs);
+    case 32: return launch_stream<4, 2, 4>(c, hs);
+    case 256: return launch_mx4_tile(c, hs);
+    case MX_MID + 32: return launch_mx4_mid(c, 32, hs);
+    case MX_MID + 64: return launch_mx4_mid(c, 64, hs);
+    }
+    return launch_mx4_mid(c, 128, hs);
 }
 
 extern "C" ss_status mx4_gemm(const void* codes, const void* scales, const void* w_vals, const void* w_meta, int64_t M, int64_t O, int64_t K, int gated,

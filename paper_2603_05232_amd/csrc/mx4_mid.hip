@@ -1,0 +1,214 @@
+// Products of microscaled 4-bit operands on tiles of 128 channels x 32, 64 or 128 token rows (mx4_gemm, mx4_grouped_gemm).
+//
+// A workgroup of eight wavefronts takes one tile, in two groups of four that share the tile out alike: group g multiplies step g of every unit, and
+// the groups' sums meet in LDS at the end.  (A group per half of the tile would read the operands of the other half's rows or channels
+// once more: 96 instead of 64 KB of LDS reads a unit.)  Operands go through a ring of D units in LDS, filled by direct loads.  The wavefronts meet
+// once a unit, when each of them holds its operands: the unit's slot is then free for unit u + D, and unit u + 1 has landed, whose
+// operands are read while unit u multiplies.
+#include "mx4_common.h"
+#include "mx4_loads.h"
+#include "device_info.h"
+
+namespace ss {
+
+// a group is WO x WT wavefronts of FW fragments of 32 channels x TW blocks of 16 rows
+template <int FW, int TW, int WO, int WT, int KG, int D> struct MidShape {
+    static constexpr int ROWS = 16 * TW * WT, A = 4 * MX_FRAGB, B = ROWS * MX_UNITB, MA = 4 * MX_FRAGS, MB = ROWS * MX_UNITS;
+    static constexpr int B_OFF = A, MA_OFF = A + B, MB_OFF = MA_OFF + MA, UNIT = MB_OFF + MB, LDS = D * UNIT;
+    static constexpr int NB = ROWS >= 64 ? ROWS / 64 : 1;         // loads of token rows of a wavefront for a unit
+    static constexpr int LOADS = 2 + NB;                          // all its loads, without those of the scales, which some have
+    static constexpr int SUMS = 4 * FW * TW * 1024;               // bytes of the sums that a group hands over
+    static_assert(FW * WO == 4 && WO * WT * KG == 8 && (KG == 1 || (KG == 2 && TW % 2 == 0 && SUMS * 2 <= LDS)) && LDS <= 160 * 1024, "whole shares");
+};
+
+// Waits until the wavefront has at most A (with = 1) or B loads in flight.
+template <int A, int B> __device__ inline void mid_wait(int with)
+{
+    with = __builtin_amdgcn_readfirstlane(with);
+    asm volatile("s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n\ts_branch 2f\n1:\n\ts_waitcnt vmcnt(%2)\n2:" ::"s"(with), "n"(A), "n"(B) : "memory", "scc");
+}
+
+template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
+__global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int tiles, Div by)
+{
+    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    constexpr int TS = 2 / KG;                           // steps of a unit that a wavefront multiplies
+    const int group = KG == 2 ? wave >> 2 : 0, wo = wave % WO, wt = wave / WO % WT, U = c.U;
+    const uint32_t lds0 = lds_address(smem);
+    // Neighbouring workgroups of an XCD share a panel's weights (dense) or a tile's rows (grouped).
+    const int item = xcd_run(blockIdx.x, panels * tiles), at = quot(item, by);
+    const int panel = GROUPED ? item - at * panels : at, slot = GROUPED ? at : item - at * tiles;
+    mx4_rows t = {0, slot * S::ROWS, min(S::ROWS, c.R - slot * S::ROWS)};
+    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, S::ROWS, slot);
+    if (t.count <= 0) return;
+    const bool none = GROUPED && t.expert == c.E;
+
+    // Sources of a unit: half of fragment wave / 2, token rows 8 (8 i + wave) .. + 7 (32 rows: of wavefronts 0 .. 3), and by some wavefronts
+    // scales: all weights' by wavefront 0, 32 rows' by wavefronts 4 .. 7.
+    const int64_t first_frag = (int64_t)(none ? 0 : t.expert) * c.frags;
+    const uint8_t* av = c.w_vals + (first_frag + min(panel * 4 + wave / 2, c.frags - 1)) * U * MX_FRAGB + (wave & 1) * 2048;
+    const uint8_t* am = c.w_meta + (first_frag + panel * 4) * U * MX_FRAGS;
+    const uint8_t *bv = c.codes + (int64_t)t.first * U * MX_UNITB, *bm = c.scales + (int64_t)t.first * MX_UNITS;
+    uint32_t boff[S::NB];
+#pragma unroll
+    for (int i = 0; i < S::NB; ++i) {
+        const int row = 8 * (8 * i + wave) + (lane >> 3);
+        boff[i] = (uint32_t)min(row, t.count - 1) * (uint32_t)(U * MX_UNITB) + mx4_place((lane & 7) ^ swz(row)) * 16;
+    }
+    const uint32_t moff = wave == 0 ? (uint32_t)min(lane >> 4, c.frags - 1 - panel * 4) * (uint32_t)(U * MX_FRAGS) + (lane & 15) * 16
+                                    : (uint32_t)min((wave & 3) * 32 + (lane >> 1), t.count - 1) * MX_UNITS + (lane & 1) * 4;
+    const int with = __builtin_amdgcn_readfirstlane(wave == 0 || (wave >= 4 && (wave & 3) * 32 < S::ROWS) ? 1 : 0);
+    const uint32_t lane16 = lane * 16, rows_here = S::ROWS >= 64 || wave < 4 ? ~0u : 0u;
+    const int64_t bm_next = (int64_t)c.R * MX_UNITS;
+    const uint32_t a_dst = lds0 + wave * 2048, b_dst = lds0 + S::B_OFF + wave * 1024, ma_dst = lds0 + S::MA_OFF, mb_dst = lds0 + S::MB_OFF + (wave & 3) * 256;
+    // Load number `piece` of the next unit, into `slot_off`; without `more` by no lane, so that every unit counts the same.
+    auto load = [&](auto piece_c, uint32_t slot_off, bool more) __attribute__((always_inline)) {
+        constexpr int P = decltype(piece_c)::value;
+        const uint32_t all = __builtin_amdgcn_readfirstlane(more ? ~0u : 0u), some = __builtin_amdgcn_readfirstlane(all & rows_here);
+        if constexpr (P < 2) mx4_load16(av + P * 1024, lane16, a_dst + slot_off + P * 1024, all);
+        else if constexpr (P < S::LOADS) mx4_load16(bv, boff[P - 2], b_dst + slot_off + (P - 2) * 8192, some);
+        else {
+            if (wave == 0) mx4_load16(am, moff, ma_dst + slot_off, all);
+            else if (with) mx4_load4(bm, moff, mb_dst + slot_off, all, all);
+            av += MX_FRAGB;
+            am += MX_FRAGS;
+            bv += MX_UNITB;
+            bm += bm_next;
+        }
+    };
+    // this wavefront's operands: step `group` of its fragments and rows
+    const uint32_t ra = wo * FW * MX_FRAGB + group * 2048 + lane * 16, rma = S::MA_OFF + wo * FW * MX_FRAGS + lane * 4;
+    const uint32_t rb = S::B_OFF + (wt * TW * 16 + n) * ROWB + ((mx4_place(2 * q + group) ^ swz(n)) << 4), rmb = S::MB_OFF + (wt * TW * 16 + n) * MX_UNITS + 2 * q + group;
+
+    const int units = none ? 0 : U;
+#pragma unroll
+    for (int d = 0; d < D; ++d) unroll<S::LOADS + 1>([&](auto p) __attribute__((always_inline)) { load(p, d * S::UNIT, d < units); });
+    v4f acc[FW][2][TW];
+#pragma unroll
+    for (int f = 0; f < FW; ++f)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < TW; ++b) acc[f][h][b] = v4f{0, 0, 0, 0};
+    struct Operands { v4i a[TS][FW][2], b[TS][TW]; int sa[FW], sb[TW]; };
+    // operand read number `piece` of READS: a step's rows and weights, the next step's, the scales
+    constexpr int SR = 2 * FW + TW, READS = TS * SR + FW + TW, SN = FW * TW * 2, N = TS * SN;
+    auto read = [&](auto piece_c, Operands& r, uint32_t slot_off) __attribute__((always_inline)) {
+        constexpr int P = decltype(piece_c)::value, T = P / SR, Q = P % SR, Z = P - TS * SR;
+        if constexpr (Z >= FW) {
+            const uint8_t* const at = smem + rmb + slot_off + (Z - FW) * 128;
+            r.sb[Z - FW] = KG == 2 ? *at : *reinterpret_cast<const uint16_t*>(at);
+        } else if constexpr (Z >= 0) r.sa[Z] = *reinterpret_cast<const int*>(smem + rma + slot_off + Z * MX_FRAGS);
+        else if constexpr (Q < TW) r.b[T][Q] = *reinterpret_cast<const v4i*>(smem + ((rb + slot_off) ^ (T * 32)) + Q * 2048);
+        else r.a[T][(Q - TW) >> 1][(Q - TW) & 1] = *reinterpret_cast<const v4i*>(smem + ra + slot_off + T * 2048 + ((Q - TW) >> 1) * MX_FRAGB + ((Q - TW) & 1) * 1024);
+    };
+    uint32_t here = 0;
+    // One by one between the products: a wavefront issues in order, and a read or a load that has to wait for room in its queue keeps the
+    // products behind it from issuing.
+    auto unit = [&](Operands& now, Operands& next, int u) __attribute__((always_inline)) {
+        mid_wait<(D - 2) * (S::LOADS + 1), (D - 2) * S::LOADS>(with);      // unit u + 1 has landed, and this one's operands have arrived
+        wait_lgkm0();
+        wg_barrier();
+        const uint32_t freed = here;
+        here = here + S::UNIT == D * S::UNIT ? 0 : here + S::UNIT;       // behind the last unit what an older one left is read, for nothing
+#pragma unroll
+        for (int f = 0; f < FW; ++f)
+            if constexpr (KG == 2) now.sa[f] = (uint32_t)now.sa[f] >> (8 * group);
+        __builtin_amdgcn_sched_barrier(0);
+        unroll<N>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value, T = i / SN, j = i % SN, b = j / (2 * FW), f = (j >> 1) % FW, h = j & 1;
+            constexpr int r0 = i * READS / N, r1 = (i + 1) * READS / N, l0 = i * (S::LOADS + 1) / N, l1 = (i + 1) * (S::LOADS + 1) / N;
+            acc[f][h][b] = mx4_mma<2 * h + T, T>(now.a[T][f][h], now.b[T][b], acc[f][h][b], now.sa[f], now.sb[b]);
+            __builtin_amdgcn_sched_barrier(0);
+            unroll<r1 - r0>([&](auto p) __attribute__((always_inline)) { read(std::integral_constant<int, r0 + decltype(p)::value>{}, next, here); });
+            unroll<l1 - l0>([&](auto p) __attribute__((always_inline)) { load(std::integral_constant<int, l0 + decltype(p)::value>{}, freed, u + D < U); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    mid_wait<(D - 1) * (S::LOADS + 1), (D - 1) * S::LOADS>(with);
+    wg_barrier();
+    Operands r0, r1;
+    unroll<READS>([&](auto p) __attribute__((always_inline)) { read(p, r0, 0); });
+    int u = 0;
+    for (; u + 2 <= units; u += 2) {
+        unit(r0, r1, u);
+        unit(r1, r0, u + 1);
+    }
+    if (u < units) unit(r0, r1, u);
+    if constexpr (KG == 1) {
+#pragma unroll
+        for (int b = 0; b < TW; ++b) {
+            const int row = 16 * (wt * TW + b) + n;
+            if (row >= t.count) continue;
+            uint16_t* const y = c.Y + (int64_t)(t.first + row) * c.ldy;
+#pragma unroll
+            for (int f = 0; f < FW; ++f) mx4_store8(acc[f][0][b], acc[f][1][b], y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
+        }
+    } else {
+    // The groups' sums: each hands half of its blocks of rows to the other and finishes the rest.
+    wait_lgkm0();
+    wg_barrier();
+    v4f* const mine = reinterpret_cast<v4f*>(smem + group * S::SUMS) + (wave & 3) * (FW * TW * 64) + lane;
+    const v4f* const theirs = reinterpret_cast<const v4f*>(smem + (1 - group) * S::SUMS) + (wave & 3) * (FW * TW * 64) + lane;
+    auto give = [&](auto other) __attribute__((always_inline)) {
+        constexpr int B0 = decltype(other)::value * (TW / 2);
+#pragma unroll
+        for (int b = 0; b < TW / 2; ++b)
+#pragma unroll
+            for (int f = 0; f < FW; ++f)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) mine[((b * FW + f) * 2 + h) * 64] = acc[f][h][B0 + b];
+    };
+    auto finish = [&](auto own) __attribute__((always_inline)) {
+        constexpr int G = decltype(own)::value, B0 = G * (TW / 2);
+        // lane (n, q): channels 8 q .. + 7 of each fragment, row n of each block; group 0's sums first
+#pragma unroll
+        for (int b = 0; b < TW / 2; ++b) {
+            const int row = 16 * (wt * TW + B0 + b) + n;
+            uint16_t* const y = c.Y + (int64_t)(t.first + min(row, t.count - 1)) * c.ldy;
+#pragma unroll
+            for (int f = 0; f < FW; ++f) {
+                const v4f v = theirs[((b * FW + f) * 2) * 64], w = theirs[((b * FW + f) * 2 + 1) * 64];
+                const v4f x = acc[f][0][B0 + b], z = acc[f][1][B0 + b];
+                if (row < t.count) mx4_store8(G == 0 ? x + v : v + x, G == 0 ? z + w : w + z, y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
+            }
+        }
+    };
+    if (group == 0) give(std::integral_constant<int, 1>{});
+    else give(std::integral_constant<int, 0>{});
+    wait_lgkm0();
+    wg_barrier();
+    if (group == 0) finish(std::integral_constant<int, 0>{});
+    else finish(std::integral_constant<int, 1>{});
+    }
+}
+
+template <int FW, int TW, int WO, int WT, int KG, int D> static ss_status launch(const mx4_call& c, hipStream_t stream)
+{
+    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    const int64_t panels = (c.frags + 3) / 4, tiles = c.offsets ? mx4_max_tiles(c.R, c.E, S::ROWS) : ((int64_t)c.R + S::ROWS - 1) / S::ROWS;
+    if (panels * tiles > INT32_MAX) return SS_ERR_SHAPE;
+    const dim3 grid((uint32_t)(panels * tiles));
+    if (c.offsets) {
+        if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, true>>(S::LDS) != SS_OK) return SS_ERR_HIP;
+        hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, true>), grid, dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, make_div(panels));
+    } else {
+        if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, false>>(S::LDS) != SS_OK) return SS_ERR_HIP;
+        hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, false>), grid, dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, make_div(tiles));
+    }
+    return launch_status();
+}
+
+ss_status launch_mx4_mid(const mx4_call& c, int rows, hipStream_t stream)
+{
+    switch (rows) {
+    case 32: return launch<1, 2, 4, 1, 2, 3>(c, stream);
+    case 64: return launch<2, 2, 2, 2, 2, 3>(c, stream);
+    case 128: return launch<2, 2, 2, 4, 1, 4>(c, stream);
+    }
+    return SS_ERR_SHAPE;
+}
+
+}  // namespace ss

@@ -9,7 +9,7 @@
 // behind the meeting need was requested two steps before or earlier.  The requests run on across tiles; between two there is only
 // the epilogue, which stages in the token slot that is free then.
 #include "mx4_common.h"
-#include "lds_pipe.h"
+#include "mx4_loads.h"
 #include "tile_common.h"
 #include "device_info.h"
 
@@ -19,22 +19,6 @@ constexpr int XT_A = 16 * 1024, XT_B = 32 * 1024, XT_M = 2048;
 constexpr int XT_B_OFF = 3 * XT_A, XT_MA_OFF = XT_B_OFF + 3 * XT_B, XT_MB_OFF = XT_MA_OFF + 2 * XT_M, XT_LDS = XT_MB_OFF + 2 * XT_M;      // 152 KB
 constexpr int XT_ENDS = 2 * MX_MAX_EXPERTS * 4;          // last tile and last row of every expert
 static_assert(XT_LDS + XT_ENDS <= 160 * 1024, "LDS budget");
-
-// direct loads by all lanes (more = ~0) or none (0), in a wavefront whose lanes are all active
-__device__ inline void xt_load16(const uint8_t* base, uint32_t lane_off, uint32_t lds, uint32_t more)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
-                 ::"s"(lds), "v"(lane_off), "s"(base), "s"(more) : "memory", "m0");
-}
-__device__ inline void xt_load4(const uint8_t* base, uint32_t lane_off, uint32_t lds, uint32_t more)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
-                 ::"s"(lds), "v"(lane_off), "s"(base), "s"(more) : "memory", "m0");
-}
-
-// 16-byte chunk c of a token row lies at chunk xt_place(c) ^ swz(row): a 16-byte LDS read is served to eight lanes of one q and eight of q ^ 1 at a
-// time (rows 0 .. 3, 12 .. 15 of the one, 4 .. 11 of the other), whose chunks 2 apart would meet on the same banks
-__device__ inline int xt_place(int c) { return (c & 4) | ((c & 1) << 1) | ((c >> 1) & 1); }      // its own inverse
 
 // acc[2 f + hh][b][i] of lane (n, q): packed channel 32 f + 8 q + 4 hh + i, row 16 b + n of a sub-tile of 128 x 64 of which rows_left rows and cols_left
 // columns of Y exist.  Staged 16 rows at a time through the wavefront's own 4 KB, so that every store writes whole pieces of Y's rows.
@@ -155,7 +139,7 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 8 * (8 * i + wave) + (ln >> 3);
-            boff[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)(U * MX_UNITB) + xt_place((ln & 7) ^ swz(row)) * 16;
+            boff[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)(U * MX_UNITB) + mx4_place((ln & 7) ^ swz(row)) * 16;
         }
         bmoff = (uint32_t)min((wave >> 1) * 64 + 16 * (ln & 3) + (wave & 1) * 8 + (ln >> 3), t.rows - 1) * MX_UNITS + (ln & 4);
     };
@@ -163,18 +147,18 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     const uint32_t lane16 = lane * 16, lane4 = lane * 4;
     const uint32_t a_wave = lds0 + wave * 2048, b_wave = lds0 + XT_B_OFF + wave * 1024, ma_wave = lds0 + XT_MA_OFF + wave * 256, mb_wave = lds0 + XT_MB_OFF + wave * 256;
     auto load_a = [&](int t, int j, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
-        xt_load16(pa.v + (2 * t + j) * 1024, lane16, a_wave + slot + j * 1024, more);
+        mx4_load16(pa.v + (2 * t + j) * 1024, lane16, a_wave + slot + j * 1024, more);
     };
-    auto load_ma = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load4(pa.m, lane4, ma_wave + slot, more); };
-    auto load_b = [&](int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
-    auto load_mb = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { xt_load4(pb.m, bmoff, mb_wave + slot, more); };
+    auto load_ma = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pa.m, lane4, ma_wave + slot, more, more); };
+    auto load_b = [&](int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
+    auto load_mb = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pb.m, bmoff, mb_wave + slot, more, more); };
     auto next_a = [&]() __attribute__((always_inline)) { pa.v += MX_FRAGB; pa.m += MX_FRAGS; };
     auto next_b = [&]() __attribute__((always_inline)) { pb.v += MX_UNITB; pb.m += mb_next; };
 
     // LDS offsets of this lane's operand reads
     const uint32_t ra = wo * 8192 + lane * 16;
     const uint32_t rma = XT_MA_OFF + wo * 1024 + lane * 4;
-    const uint32_t rb = XT_B_OFF + (wt * 64 + n) * ROWB + ((xt_place(2 * q) ^ swz(n)) << 4);
+    const uint32_t rb = XT_B_OFF + (wt * 64 + n) * ROWB + ((mx4_place(2 * q) ^ swz(n)) << 4);
     const uint32_t rmb = XT_MB_OFF + wt * 512 + n * 32 + (q >> 1) * 16;
     const uint32_t mb_shift = 16 * (q & 1);               // this lane's two bytes of a word of four scales
 

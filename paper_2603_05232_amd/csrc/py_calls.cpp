@@ -1,4 +1,4 @@
-// The calls of a model's forward pass (quantisation, sparse GEMMs) as CPython functions: argument reading, output
+// The calls of a model's forward pass (quantisation, sparse GEMMs, the 4-bit expert layer) as CPython functions: argument reading, output
 // allocation and the C call without going through ctypes and torch's Python layer.  Layers of few tokens are bound by the time
 // between launches, most of which was spent there (quantisation + GEMM of 16 x 512 x 512: see binding.py).
 //
@@ -187,6 +187,195 @@ PyObject* py_slide_sparse_gemm_fused(PyObject*, PyObject* const* a, Py_ssize_t n
     END_HANDLE_TH_ERRORS
 }
 
+// ---- microscaled 4-bit operands and layers of experts ----
+struct Mx4 {
+    decltype(&::mx4_row_bytes) row_bytes;
+    decltype(&::mx4_quant) quant;
+    decltype(&::mx4_dequant) dequant;
+    decltype(&::mx4_packed_sizes) packed_sizes;
+    decltype(&::mx4_gemm) gemm;
+    decltype(&::mx4_grouped_gemm) grouped_gemm;
+    decltype(&::expert_route_workspace_bytes) route_workspace;
+    decltype(&::expert_route) route;
+    decltype(&::expert_combine) combine;
+} mx4;                                                // zeros until bind_mx4()
+
+bool float_or_bf16(const at::Tensor& t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+ss_act_dtype in_code(const at::Tensor& t) { return t.scalar_type() == at::kFloat ? SS_IN_F32 : SS_IN_BF16; }
+// a matrix on the GPU whose rows are dense, and the elements between its rows
+bool matrix(const at::Tensor& t) { return t.is_cuda() && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1); }
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+bool dense(const at::Tensor& t, at::ScalarType type) { return t.is_cuda() && t.scalar_type() == type && t.is_contiguous(); }
+// codes[R, 128 U] and scales[U, R, 8] of rows of K values
+bool code_rows(const at::Tensor& codes, const at::Tensor& scales, int64_t K)
+{
+    const int64_t width = mx4.row_bytes(K);
+    return width > 0 && dense(codes, at::kByte) && dense(scales, at::kByte) && codes.dim() == 2 && scales.dim() == 3 && codes.size(1) == width &&
+           scales.size(0) == width / 128 && scales.size(1) == codes.size(0) && scales.size(2) == 8;
+}
+PyObject* wrap(at::Tensor& made, PyObject* given) { return made.defined() ? THPVariable_Wrap(std::move(made)) : Py_NewRef(given); }
+
+// mx4_quant(X, rows, codes, scales)
+PyObject* py_mx4_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (!mx4.quant || n != 4 || !plain(a[0]) || !plain_or_none(a[1]) || !plain_or_none(a[2]) || !plain_or_none(a[3]) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[0]);
+    if (!matrix(X) || !float_or_bf16(X)) Py_RETURN_NONE;
+    const int64_t M = X.size(0), K = X.size(1), width = mx4.row_bytes(K);
+    if (width < 0 || (a[1] != Py_None && (THPVariable_Unpack(a[1]).dim() != 1 || !dense(THPVariable_Unpack(a[1]), at::kInt)))) Py_RETURN_NONE;
+    const int64_t R = a[1] == Py_None ? M : THPVariable_Unpack(a[1]).size(0);
+    at::Tensor codes, scales;
+    ss_status st;
+    {
+        Unlocked u;
+        if (a[2] == Py_None) codes = at::empty({R, width}, X.options().dtype(at::kByte));
+        if (a[3] == Py_None) scales = at::empty({width / 128, R, 8}, X.options().dtype(at::kByte));
+        const at::Tensor &c = codes.defined() ? codes : THPVariable_Unpack(a[2]), &s = scales.defined() ? scales : THPVariable_Unpack(a[3]);
+        st = code_rows(c, s, K) && c.size(0) == R
+                 ? mx4.quant(X.data_ptr(), in_code(X), M, K, row_stride(X), static_cast<const int32_t*>(address(a[1])), R, c.data_ptr(), s.data_ptr(), current_stream())
+                 : SS_ERR_SHAPE;
+    }
+    if (st != SS_OK) return refused(st, "mx4_quant");
+    PyObject *pc = wrap(codes, a[2]), *ps = wrap(scales, a[3]);
+    PyObject* r = pc && ps ? PyTuple_Pack(2, pc, ps) : nullptr;
+    Py_XDECREF(pc);
+    Py_XDECREF(ps);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_dequant(codes, scales, K, fp32 or bf16 as ss_act_dtype, out)
+PyObject* py_mx4_dequant(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t K, type;
+    if (!mx4.dequant || n != 5 || !plain(a[0]) || !plain(a[1]) || !integer(a[2], 1, INT64_MAX, K) || !integer(a[3], 0, 1, type) || !plain_or_none(a[4]) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor &codes = THPVariable_Unpack(a[0]), &scales = THPVariable_Unpack(a[1]);
+    if (!code_rows(codes, scales, K)) Py_RETURN_NONE;
+    at::Tensor made;
+    ss_status st;
+    {
+        Unlocked u;
+        if (a[4] == Py_None) made = at::empty({codes.size(0), K}, codes.options().dtype(type == SS_IN_F32 ? at::kFloat : at::kBFloat16));
+        const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[4]);
+        st = matrix(y) && float_or_bf16(y) && y.size(0) == codes.size(0) && y.size(1) == K
+                 ? mx4.dequant(codes.data_ptr(), scales.data_ptr(), codes.size(0), K, in_code(y), y.data_ptr(), row_stride(y), current_stream())
+                 : SS_ERR_SHAPE;
+    }
+    if (st != SS_OK) return refused(st, "mx4_dequant");
+    return wrap(made, a[4]);
+    END_HANDLE_TH_ERRORS
+}
+
+// mx4_product(offsets or None, codes, scales, w_vals, w_meta, O, K, gated, out, workspace)
+PyObject* py_mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t O, K;
+    if (!mx4.gemm || n != 10 || !plain_or_none(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain(a[3]) || !plain(a[4]) || !integer(a[5], 0, INT_MAX, O) || !integer(a[6], 1, INT64_MAX, K) ||
+        !PyBool_Check(a[7]) || !plain_or_none(a[8]) || !plain_or_none(a[9]) || modes_active())
+        Py_RETURN_NONE;
+    const bool grouped = a[0] != Py_None;
+    const int gated = a[7] == Py_True;
+    const at::Tensor &codes = THPVariable_Unpack(a[1]), &scales = THPVariable_Unpack(a[2]), &wv = THPVariable_Unpack(a[3]), &wm = THPVariable_Unpack(a[4]);
+    if (!code_rows(codes, scales, K) || (grouped && (THPVariable_Unpack(a[0]).dim() != 1 || !dense(THPVariable_Unpack(a[0]), at::kInt)))) Py_RETURN_NONE;
+    const int64_t R = codes.size(0), E = grouped ? THPVariable_Unpack(a[0]).size(0) - 1 : 1;
+    size_t vb, mb;
+    if (mx4.packed_sizes(E, O, K, gated, &vb, &mb) != SS_OK || !dense(wv, at::kByte) || !dense(wm, at::kByte) || (size_t)wv.numel() != vb || (size_t)wm.numel() != mb) Py_RETURN_NONE;
+    void* const ws = address(a[9]);
+    const size_t ws_bytes = a[9] == Py_None ? 0 : THPVariable_Unpack(a[9]).nbytes();
+    at::Tensor made;
+    ss_status st;
+    {
+        Unlocked u;
+        if (a[8] == Py_None) made = at::empty({R, O}, codes.options().dtype(at::kBFloat16));
+        const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[8]);
+        if (!matrix(y) || y.scalar_type() != at::kBFloat16 || y.size(0) != R || y.size(1) != O) st = SS_ERR_SHAPE;
+        else if (grouped)
+            st = mx4.grouped_gemm(codes.data_ptr(), scales.data_ptr(), static_cast<const int32_t*>(address(a[0])), wv.data_ptr(), wm.data_ptr(), R, E, O, K, gated, y.data_ptr(),
+                                  row_stride(y), ws, ws_bytes, current_stream());
+        else st = mx4.gemm(codes.data_ptr(), scales.data_ptr(), wv.data_ptr(), wm.data_ptr(), R, O, K, gated, y.data_ptr(), row_stride(y), ws, ws_bytes, current_stream());
+    }
+    if (st != SS_OK) return refused(st, grouped ? "mx4_grouped_gemm" : "mx4_gemm");
+    return wrap(made, a[8]);
+    END_HANDLE_TH_ERRORS
+}
+
+// expert_route(logits, k, renormalise, workspace)
+PyObject* py_expert_route(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t k;
+    if (!mx4.route || n != 4 || !plain(a[0]) || !integer(a[1], 1, 64, k) || !PyBool_Check(a[2]) || !plain_or_none(a[3]) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor& x = THPVariable_Unpack(a[0]);
+    if (!matrix(x) || !float_or_bf16(x) || k > x.size(1)) Py_RETURN_NONE;
+    const int64_t M = x.size(0), E = x.size(1);
+    at::Tensor ids, weights, slots, rows, offsets, scratch;
+    ss_status st;
+    {
+        Unlocked u;
+        const auto i32 = x.options().dtype(at::kInt);
+        ids = at::empty({M, k}, i32);
+        weights = at::empty({M, k}, x.options().dtype(at::kFloat));
+        slots = at::empty({M, k}, i32);
+        rows = at::empty({M * k}, i32);
+        offsets = at::empty({E + 1}, i32);
+        void* ws = address(a[3]);
+        size_t ws_bytes = a[3] == Py_None ? 0 : THPVariable_Unpack(a[3]).nbytes();
+        if (a[3] == Py_None && (ws_bytes = mx4.route_workspace(M, E, k)) > 0) { scratch = at::empty({(int64_t)ws_bytes}, x.options().dtype(at::kByte)); ws = scratch.data_ptr(); }
+        st = mx4.route(x.data_ptr(), in_code(x), M, E, row_stride(x), (int)k, a[2] == Py_True, static_cast<int32_t*>(ids.data_ptr()), static_cast<float*>(weights.data_ptr()),
+                       static_cast<int32_t*>(slots.data_ptr()), static_cast<int32_t*>(rows.data_ptr()), static_cast<int32_t*>(offsets.data_ptr()), ws, ws_bytes, current_stream());
+    }
+    if (st != SS_OK) return refused(st, "expert_route");
+    PyObject* r = PyTuple_New(5);
+    at::Tensor* const all[5] = {&ids, &weights, &slots, &rows, &offsets};
+    for (int i = 0; r && i < 5; ++i) {
+        PyObject* const o = THPVariable_Wrap(std::move(*all[i]));
+        if (o) PyTuple_SET_ITEM(r, i, o);
+        else Py_CLEAR(r);
+    }
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// expert_combine(Y, slots, weights, base, out)
+PyObject* py_expert_combine(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (!mx4.combine || n != 5 || !plain(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain_or_none(a[3]) || !plain_or_none(a[4]) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor &Y = THPVariable_Unpack(a[0]), &slots = THPVariable_Unpack(a[1]), &weights = THPVariable_Unpack(a[2]);
+    if (!matrix(Y) || Y.scalar_type() != at::kBFloat16 || slots.dim() != 2 || !dense(slots, at::kInt) || !dense(weights, at::kFloat) || weights.sizes() != slots.sizes()) Py_RETURN_NONE;
+    const int64_t M = slots.size(0), k = slots.size(1), O = Y.size(1);
+    if (k > INT_MAX) Py_RETURN_NONE;
+    auto fits = [&](const at::Tensor& t) { return matrix(t) && t.scalar_type() == at::kBFloat16 && t.size(0) == M && t.size(1) == O; };
+    if (a[3] != Py_None && !fits(THPVariable_Unpack(a[3]))) Py_RETURN_NONE;
+    at::Tensor made;
+    ss_status st;
+    {
+        Unlocked u;
+        if (a[4] == Py_None) made = at::empty({M, O}, Y.options());
+        const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[4]);
+        st = fits(y) ? mx4.combine(Y.data_ptr(), Y.size(0), O, row_stride(Y), static_cast<const int32_t*>(slots.data_ptr()), static_cast<const float*>(weights.data_ptr()), M, (int)k, address(a[3]),
+                                   a[3] == Py_None ? 0 : row_stride(THPVariable_Unpack(a[3])), y.data_ptr(), row_stride(y), current_stream())
+                     : SS_ERR_SHAPE;
+    }
+    if (st != SS_OK) return refused(st, "expert_combine");
+    return wrap(made, a[4]);
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_mx4(the addresses of Mx4's functions in their order), behind bind()
+PyObject* py_bind_mx4(PyObject*, PyObject* args)
+{
+    unsigned long long f[9];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8])) return nullptr;
+    mx4 = {reinterpret_cast<decltype(mx4.row_bytes)>(f[0]), reinterpret_cast<decltype(mx4.quant)>(f[1]), reinterpret_cast<decltype(mx4.dequant)>(f[2]),
+           reinterpret_cast<decltype(mx4.packed_sizes)>(f[3]), reinterpret_cast<decltype(mx4.gemm)>(f[4]), reinterpret_cast<decltype(mx4.grouped_gemm)>(f[5]),
+           reinterpret_cast<decltype(mx4.route_workspace)>(f[6]), reinterpret_cast<decltype(mx4.route)>(f[7]), reinterpret_cast<decltype(mx4.combine)>(f[8])};
+    Py_RETURN_NONE;
+}
+
 // bind(SlideSparseError, slide_lifted_ld, act_lift_quant, slide_sparse_gemm_ws, slide_sparse_gemm_fused_ws), the last four as
 // addresses; library() tells these
 PyObject* py_bind(PyObject*, PyObject* args)
@@ -211,6 +400,12 @@ PyObject* py_library(PyObject*, PyObject*)
 PyMethodDef methods[] = {{"act_lift_quant", SS_PY(py_act_lift_quant), nullptr},
                          {"slide_sparse_gemm", SS_PY(py_slide_sparse_gemm), nullptr},
                          {"slide_sparse_gemm_fused", SS_PY(py_slide_sparse_gemm_fused), nullptr},
+                         {"mx4_quant", SS_PY(py_mx4_quant), nullptr},
+                         {"mx4_dequant", SS_PY(py_mx4_dequant), nullptr},
+                         {"mx4_product", SS_PY(py_mx4_product), nullptr},
+                         {"expert_route", SS_PY(py_expert_route), nullptr},
+                         {"expert_combine", SS_PY(py_expert_combine), nullptr},
+                         {"bind_mx4", py_bind_mx4, METH_VARARGS, nullptr},
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {"library", py_library, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -1,5 +1,7 @@
 """The choice of experts and the weighted sum against the oracle (64 bits).  Choices and order are equal; weights may be off by the 32-bit exponential's
 argument and the sums: 2^-23 (|largest difference of scores| + summands + 8) of the weight."""
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -87,3 +89,38 @@ def test_combine_refuses():
         binding.expert_combine(Y, s, w, base=Y)
     with pytest.raises(binding.SlideSparseError):
         binding.expert_route(torch.zeros((2, 3), device=DEV), 4)
+
+
+def test_calls_through_the_module_and_without_it(monkeypatch):
+    """The extension module takes plain calls, the general path gives the same."""
+    binding.load()
+    X = torch.randn((70, 600), device=DEV).to(torch.bfloat16)
+    w = binding.mx4_pack(*binding.mx4_quant(torch.randn((4 * 96, 600), device=DEV)), 600, experts=4)
+    w1 = binding.mx4_pack(*binding.mx4_quant(torch.randn((96, 600), device=DEV)), 600)
+    logits = torch.randn((70, 4), device=DEV)
+
+    def calls():
+        ids, weights, slots, rows, offsets = binding.expert_route(logits, 2)
+        codes, scales = binding.mx4_quant(X, rows=rows)
+        Y = binding.mx4_grouped_gemm(codes, scales, offsets, *w, 96, 600)
+        Z = binding.mx4_gemm(codes, scales, *w1, 96, 600, out=torch.zeros((140, 100), dtype=torch.bfloat16, device=DEV)[:, :96])
+        return [ids, weights, slots, rows, offsets, codes, scales, Y, Z, binding.mx4_dequant(codes, scales, 600), binding.mx4_dequant(codes, scales, 600, torch.bfloat16),
+                binding.expert_combine(Y, slots, weights), binding.expert_combine(Y, slots, weights, base=Z[:70])]
+
+    taken = []
+    names = ("mx4_quant", "mx4_dequant", "mx4_product", "expert_route", "expert_combine")
+    real = binding._mx4_calls
+
+    def spy(name):
+        def call(*args):
+            r = getattr(real, name)(*args)
+            taken.append(r is not None)
+            return r
+        return call
+
+    monkeypatch.setattr(binding, "_mx4_calls", types.SimpleNamespace(**{n: spy(n) for n in names}))
+    a = calls()
+    assert taken and all(taken)
+    monkeypatch.setattr(binding, "_mx4_calls", types.SimpleNamespace(**dict.fromkeys(names, lambda *args: None)))
+    for x, y in zip(a, calls()):
+        assert x.shape == y.shape and x.dtype == y.dtype and x.device == y.device and torch.equal(x, y)
