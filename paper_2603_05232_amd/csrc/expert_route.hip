@@ -7,8 +7,7 @@
 namespace ss {
 
 constexpr int RT_TOKENS = 64;            // tokens of a workgroup: one bit each in the experts' masks
-constexpr int RT_WAVES = 16;
-constexpr int RT_THREADS = 64 * RT_WAVES;
+constexpr int RT_THREADS = 16 * RT_TOKENS;
 constexpr int RT_MAX_K = 64;
 
 // Scores as unsigned keys in their order; a NaN lies below every number, 0 is none at all.
@@ -20,139 +19,124 @@ __device__ inline uint32_t score_key(float x)
 }
 __device__ inline float key_score(uint32_t k) { return k == 1 ? __uint_as_float(0x7FC00000u) : __uint_as_float(k >> 31 ? k & 0x7FFFFFFFu : ~k); }
 
-// largest key of a wavefront, in every lane
-__device__ inline uint32_t wave_max(uint32_t v)
+// over a row of sixteen lanes, in every lane: rotations by 8, 4, 2 and 1
+template <typename F> __device__ inline int row_all(int v, F f)
 {
-    auto step = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x111, 0xF, 0xF, false));      // row_shr:1
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x112, 0xF, 0xF, false));      // 2
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x114, 0xF, 0xF, false));      // 4
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x118, 0xF, 0xF, false));      // 8
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x142, 0xA, 0xF, false));      // row_bcast:15
-    v = step(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x143, 0xC, 0xF, false));      // row_bcast:31
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, true));
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, true));
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, true));
+    return f(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, true));
 }
+__device__ inline uint32_t row_max(uint32_t v) { return (uint32_t)row_all((int)v, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); }); }
+__device__ inline int row_min(int v) { return row_all(v, [](int a, int b) { return min(a, b); }); }
+__device__ inline float row_sum(float v) { return __int_as_float(row_all(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); })); }
 
-__device__ inline float wave_sum(float v)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
-// The experts of 64 tokens: a wavefront per token, EL scores to a lane (expert 64 j + lane).  Which tokens of the workgroup take an expert
-// is a mask of 64 bits in LDS; the place of a row among the workgroup's rows for its expert is the number of bits below its own,
-// whatever the order in which they were set.
-// ONE: the only workgroup, which then knows the order; otherwise slots gets the places and counts[expert][workgroup] the numbers of rows.
-template <typename T, int EL, bool ONE>
+// The experts of 64 tokens: sixteen lanes to a token, four tokens to a wavefront, EL scores to a lane (expert 16 j + lane).  Which tokens of the
+// workgroup take an expert is a mask of 64 bits in LDS; the place of a row among the workgroup's rows for its expert is the number of bits
+// below its own, whatever the order in which they were set.
+// A lane keeps KL choices, number 16 c + l.
+// ONE: the only workgroup, which then knows the order; otherwise slots gets the places and counts[workgroup][expert] the numbers of rows.
+// Bound by instructions: a choice is about 8 EL + 30 of them, for four tokens at once (a wavefront for each token, 8192 x 128 bf16, k = 8: 14.4 us).
+template <typename T, int EL, int KL, bool ONE>
 __global__ __launch_bounds__(RT_THREADS) void k_route_choose(const T* __restrict__ logits, int64_t M, int E, int64_t ld, int k, bool renormalise,
                                                              int32_t* __restrict__ ids, float* __restrict__ weights, int32_t* __restrict__ slots,
                                                              int32_t* __restrict__ rows, int32_t* __restrict__ offsets, int32_t* __restrict__ counts)
 {
-    __shared__ unsigned long long mask[64 * EL];
-    __shared__ int32_t start[ONE ? 64 * EL + 1 : 1];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int e = threadIdx.x; e < 64 * EL; e += RT_THREADS) mask[e] = 0;
+    constexpr int ALL = 16 * EL;
+    __shared__ unsigned long long mask[ALL];
+    __shared__ int32_t start[ONE ? ALL : 1];
+    const int lane = threadIdx.x & 63, l = lane & 15;
+    for (int e = threadIdx.x; e < ALL; e += RT_THREADS) mask[e] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * RT_TOKENS;
-    const int tokens = (int)min((int64_t)RT_TOKENS, M - first);
-    constexpr int PER = RT_TOKENS / RT_WAVES;
-    int mine[PER];                                       // lane j < k: the j-th expert of the wavefront's tokens
+    const int t = threadIdx.x >> 4;                      // this lane's token of the workgroup's
+    const bool there = first + t < M;
+    const T* const row = logits + (there ? first + t : 0) * ld;
+    uint32_t key[EL];
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
-        const int t = wave + RT_WAVES * p;
-        mine[p] = 0;
-        if (t >= tokens) continue;
-        const T* const row = logits + (first + t) * ld;
-        uint32_t key[EL];
+    for (int j = 0; j < EL; ++j) key[j] = there && 16 * j + l < E ? score_key(load_scalar(row + 16 * j + l)) : 0;
+    uint32_t chosen[KL];
+    int mine[KL];
 #pragma unroll
-        for (int j = 0; j < EL; ++j) key[j] = 64 * j + lane < E ? score_key(load_scalar(row + 64 * j + lane)) : 0;
-        uint32_t chosen = 0;
-        float top = 0.0f, total = 0.0f;
-        for (int i = 0; i < k; ++i) {
-            uint32_t best = key[0];
+    for (int c = 0; c < KL; ++c) { chosen[c] = 0; mine[c] = 0; }
+    float top = 0.0f, total = 0.0f;
+    for (int i = 0; i < k; ++i) {
+        uint32_t best = key[0];
+        int at = l;
 #pragma unroll
-            for (int j = 1; j < EL; ++j) best = max(best, key[j]);
-            best = wave_max(best);
-            if (i == 0) {
-                top = key_score(best);
-                if (!renormalise) {                      // the sum over all experts, before any is taken out
-                    float part = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < EL; ++j)
-                        if (key[j]) part += expf(key_score(key[j]) - top);
-                    total = wave_sum(part);
-                }
-            }
-            int at = -1;
-#pragma unroll
-            for (int j = 0; j < EL; ++j) {
-                const uint64_t has = __ballot(key[j] == best);
-                if (at < 0 && has) {
-                    at = 64 * j + __ffsll((unsigned long long)has) - 1;
-                    if (lane == (at & 63)) key[j] = 0;
-                }
-            }
-            if (lane == i) { chosen = best; mine[p] = at; }
+        for (int j = 1; j < EL; ++j) {
+            at = key[j] > best ? 16 * j + l : at;        // of equal ones the first
+            best = max(best, key[j]);
         }
-        float w = lane < k ? expf(key_score(chosen) - top) : 0.0f;
-        if (renormalise) total = wave_sum(w);
-        w = top == -INFINITY ? 0.0f : w / total;         // all scores of a row at minus infinity: no expert has a weight
-        if (lane < k) {
-            ids[(first + t) * k + lane] = mine[p];
-            weights[(first + t) * k + lane] = w;
-            atomicOr(&mask[mine[p]], 1ull << t);
+        const uint32_t most = row_max(best);
+        at = row_min(best == most ? at : INT32_MAX);
+        if (i == 0) {
+            top = key_score(most);
+            if (!renormalise) {                          // the sum over all experts, before any is taken out
+                float part = 0.0f;
+#pragma unroll
+                for (int j = 0; j < EL; ++j) part += key[j] ? expf(key_score(key[j]) - top) : 0.0f;
+                total = row_sum(part);
+            }
         }
+#pragma unroll
+        for (int j = 0; j < EL; ++j) key[j] = 16 * j + l == at ? 0 : key[j];
+#pragma unroll
+        for (int c = 0; c < KL; ++c)
+            if (i == 16 * c + l) { chosen[c] = most; mine[c] = at; }
     }
+    float w[KL];
+#pragma unroll
+    for (int c = 0; c < KL; ++c) w[c] = there && 16 * c + l < k ? expf(key_score(chosen[c]) - top) : 0.0f;
+    if (renormalise) {
+        total = w[0];
+#pragma unroll
+        for (int c = 1; c < KL; ++c) total += w[c];
+        total = row_sum(total);
+    }
+#pragma unroll
+    for (int c = 0; c < KL; ++c)
+        if (there && 16 * c + l < k) {
+            ids[(first + t) * k + 16 * c + l] = mine[c];
+            weights[(first + t) * k + 16 * c + l] = top == -INFINITY ? 0.0f : w[c] / total;      // all scores of a row at minus infinity: no expert has a weight
+            atomicOr(&mask[mine[c]], 1ull << t);
+        }
     __syncthreads();
     if constexpr (ONE) {
-        if (wave == 0) {                                 // first place of each expert
+        if (threadIdx.x < 64) {                          // first place of each expert
             int before = 0;
             for (int e0 = 0; e0 < E; e0 += 64) {
-                const int c = __popcll(mask[e0 + lane]);
-                int sum = c;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(sum, d, 64);
-                    if (lane >= d) sum += o;
-                }
-                start[e0 + lane] = before + sum - c;
-                if (e0 + lane < E) offsets[e0 + lane] = before + sum - c;
-                before += __shfl(sum, 63, 64);
+                const int c = __popcll(mask[e0 + lane]), sum = wave_scan_add(c), at = before + sum - c;
+                start[e0 + lane] = at;
+                if (e0 + lane < E) offsets[e0 + lane] = at;
+                before += __builtin_amdgcn_readlane(sum, 63);
             }
             if (lane == 0) offsets[E] = before;
         }
         __syncthreads();
     } else {
-        for (int e = threadIdx.x; e < E; e += RT_THREADS) counts[(int64_t)e * gridDim.x + blockIdx.x] = __popcll(mask[e]);
+        for (int e = threadIdx.x; e < E; e += RT_THREADS) counts[(int64_t)blockIdx.x * E + e] = __popcll(mask[e]);
     }
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
-        const int t = wave + RT_WAVES * p;
-        if (t >= tokens || lane >= k) continue;
-        const int place = __popcll(mask[mine[p]] & ((1ull << t) - 1));
-        if constexpr (ONE) {
-            slots[t * k + lane] = start[mine[p]] + place;
-            rows[start[mine[p]] + place] = t;
-        } else slots[(first + t) * k + lane] = place;
-    }
+    for (int c = 0; c < KL; ++c)
+        if (there && 16 * c + l < k) {
+            const int place = __popcll(mask[mine[c]] & ((1ull << t) - 1));
+            if constexpr (ONE) {
+                slots[t * k + 16 * c + l] = start[mine[c]] + place;
+                rows[start[mine[c]] + place] = t;
+            } else slots[(first + t) * k + 16 * c + l] = place;
+        }
 }
 
-// counts[expert][workgroup] -> rows of the expert before the workgroup's; totals[expert].  A workgroup per expert.
-__global__ __launch_bounds__(256) void k_route_scan(int32_t* __restrict__ counts, int B, int32_t* __restrict__ totals)
+// counts[workgroup][expert] -> rows of the expert in the workgroups before; totals[expert].  A workgroup per expert.
+__global__ __launch_bounds__(256) void k_route_scan(int32_t* __restrict__ counts, int E, int B, int32_t* __restrict__ totals)
 {
     __shared__ int part[4];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int32_t* const c = counts + (int64_t)blockIdx.x * B;
+    int32_t* const c = counts + blockIdx.x;
     int before = 0;
     for (int b0 = 0; b0 < B; b0 += 256) {
-        const int b = b0 + threadIdx.x, v = b < B ? c[b] : 0;
-        int sum = v;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += o;
-        }
+        const int b = b0 + threadIdx.x, v = b < B ? c[(int64_t)b * E] : 0, sum = wave_scan_add(v);
         if (lane == 63) part[wave] = sum;
         __syncthreads();
         int add = before, all = 0;
@@ -161,42 +145,61 @@ __global__ __launch_bounds__(256) void k_route_scan(int32_t* __restrict__ counts
             if (w < wave) add += part[w];
             all += part[w];
         }
-        if (b < B) c[b] = add + sum - v;
+        if (b < B) c[(int64_t)b * E] = add + sum - v;
         before += all;
         __syncthreads();
     }
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-// places within the workgroups -> places in the order of the experts
-__global__ __launch_bounds__(256) void k_route_place(const int32_t* __restrict__ ids, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
-                                                     int64_t M, int E, int k, int B, int32_t* __restrict__ slots, int32_t* __restrict__ rows,
-                                                     int32_t* __restrict__ offsets)
+// Places within the workgroups -> places in the order of the experts.  SCANNED: k_route_scan has added the counts up; otherwise every workgroup adds
+// up all of them itself, which with few workgroups costs less than the launch in between (8192 tokens, 128 experts: 5.0 us against 3.9 and 4.3).
+constexpr int RT_OWN_SUMS = 256;         // workgroups up to which they do
+template <bool SCANNED>
+__global__ __launch_bounds__(RT_THREADS) void k_route_place(const int32_t* __restrict__ ids, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
+                                                            int64_t M, int E, int k, int B, int32_t* __restrict__ slots, int32_t* __restrict__ rows,
+                                                            int32_t* __restrict__ offsets)
 {
-    __shared__ int32_t start[MX_MAX_EXPERTS + 64];
+    __shared__ int32_t before[MX_MAX_EXPERTS + 64], total[MX_MAX_EXPERTS + 64];
     const int lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        int before = 0;
-        for (int e0 = 0; e0 < E; e0 += 64) {
-            const int c = e0 + lane < E ? totals[e0 + lane] : 0;
-            int sum = c;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int o = __shfl_up(sum, d, 64);
-                if (lane >= d) sum += o;
+    for (int e = threadIdx.x; e < MX_MAX_EXPERTS + 64; e += RT_THREADS) {
+        before[e] = SCANNED && e < E ? counts[(int64_t)blockIdx.x * E + e] : 0;
+        total[e] = SCANNED && e < E ? totals[e] : 0;
+    }
+    __syncthreads();
+    if constexpr (!SCANNED) {
+        // a thread for each expert and part of the workgroups
+        const int width = E <= 64 ? 64 : E <= 128 ? 128 : E <= 256 ? 256 : E <= 512 ? 512 : 1024, parts = RT_THREADS / width;
+        const int e = threadIdx.x & (width - 1), per = (B + parts - 1) / parts, b0 = threadIdx.x / width * per, b1 = min(B, b0 + per);
+        if (e < E) {
+            int n = 0, all = 0;
+#pragma unroll 8
+            for (int b = b0; b < b1; ++b) {
+                const int v = counts[(int64_t)b * E + e];
+                all += v;
+                n += b < (int)blockIdx.x ? v : 0;
             }
-            start[e0 + lane] = before + sum - c;
-            if (blockIdx.x == 0 && e0 + lane < E) offsets[e0 + lane] = before + sum - c;
-            before += __shfl(sum, 63, 64);
+            if (n) atomicAdd(&before[e], n);              // whole numbers: the order does not matter
+            if (all) atomicAdd(&total[e], all);
         }
-        if (blockIdx.x == 0 && lane == 0) offsets[E] = before;
+        __syncthreads();
+    }
+    if (threadIdx.x < 64) {
+        int start = 0;
+        for (int e0 = 0; e0 < E; e0 += 64) {
+            const int c = total[e0 + lane], sum = wave_scan_add(c), at = start + sum - c;
+            before[e0 + lane] += at;
+            if (blockIdx.x == 0 && e0 + lane < E) offsets[e0 + lane] = at;
+            start += __builtin_amdgcn_readlane(sum, 63);
+        }
+        if (blockIdx.x == 0 && lane == 0) offsets[E] = start;
     }
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * RT_TOKENS * k, end = min(first + (int64_t)RT_TOKENS * k, M * k);
-    for (int64_t i = first + threadIdx.x; i < end; i += 256) {
-        const int e = ids[i], s = start[e] + counts[(int64_t)e * B + blockIdx.x] + slots[i];
+    for (int64_t i = first + threadIdx.x; i < end; i += RT_THREADS) {
+        const int s = before[ids[i]] + slots[i];
         slots[i] = s;
-        rows[s] = (int32_t)(i / k);
+        rows[s] = (int32_t)(blockIdx.x * RT_TOKENS + (int)(i - first) / k);
     }
 }
 
@@ -248,22 +251,26 @@ __global__ __launch_bounds__(256) void k_combine(const uint16_t* __restrict__ Y,
     }
 }
 
-template <typename T, int EL>
+template <typename T, int EL, int KL>
 static ss_status launch_route(const void* logits, int64_t M, int64_t E, int64_t ld, int k, bool renormalise, int32_t* ids, float* weights, int32_t* slots,
                               int32_t* rows, int32_t* offsets, int32_t* counts, hipStream_t hs)
 {
     const int64_t B = M == 0 ? 1 : (M + RT_TOKENS - 1) / RT_TOKENS;       // without tokens the offsets are written all the same
     const T* const x = static_cast<const T*>(logits);
     if (B == 1) {
-        hipLaunchKernelGGL((k_route_choose<T, EL, true>), dim3(1), dim3(RT_THREADS), 0, hs, x, M, (int)E, ld, k, renormalise, ids, weights, slots, rows, offsets, counts);
+        hipLaunchKernelGGL((k_route_choose<T, EL, KL, true>), dim3(1), dim3(RT_THREADS), 0, hs, x, M, (int)E, ld, k, renormalise, ids, weights, slots, rows, offsets, counts);
         return launch_status();
     }
-    hipLaunchKernelGGL((k_route_choose<T, EL, false>), dim3((uint32_t)B), dim3(RT_THREADS), 0, hs, x, M, (int)E, ld, k, renormalise, ids, weights, slots, rows, offsets, counts);
+    hipLaunchKernelGGL((k_route_choose<T, EL, KL, false>), dim3((uint32_t)B), dim3(RT_THREADS), 0, hs, x, M, (int)E, ld, k, renormalise, ids, weights, slots, rows, offsets, counts);
     if (launch_status() != SS_OK) return SS_ERR_HIP;
     int32_t* const totals = counts + E * B;
-    hipLaunchKernelGGL(k_route_scan, dim3((uint32_t)E), dim3(256), 0, hs, counts, (int)B, totals);
+    if (B <= RT_OWN_SUMS) {
+        hipLaunchKernelGGL(k_route_place<false>, dim3((uint32_t)B), dim3(RT_THREADS), 0, hs, ids, counts, totals, M, (int)E, k, (int)B, slots, rows, offsets);
+        return launch_status();
+    }
+    hipLaunchKernelGGL(k_route_scan, dim3((uint32_t)E), dim3(256), 0, hs, counts, (int)E, (int)B, totals);
     if (launch_status() != SS_OK) return SS_ERR_HIP;
-    hipLaunchKernelGGL(k_route_place, dim3((uint32_t)B), dim3(256), 0, hs, ids, counts, totals, M, (int)E, k, (int)B, slots, rows, offsets);
+    hipLaunchKernelGGL(k_route_place<true>, dim3((uint32_t)B), dim3(RT_THREADS), 0, hs, ids, counts, totals, M, (int)E, k, (int)B, slots, rows, offsets);
     return launch_status();
 }
 
@@ -291,8 +298,8 @@ extern "C" ss_status expert_route(const void* logits, ss_act_dtype in_dtype, int
     if (((uintptr_t)logits & (in_dtype == SS_IN_F32 ? 3 : 1)) || (((uintptr_t)ids | (uintptr_t)weights | (uintptr_t)slots | (uintptr_t)rows | (uintptr_t)offsets) & 3))
         return SS_ERR_SHAPE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-#define SS_RT(T, EL) launch_route<T, EL>(logits, M, E, ld, k, renormalise != 0, ids, weights, slots, rows, offsets, static_cast<int32_t*>(workspace), hs)
-#define SS_RE(T) (E <= 64 ? SS_RT(T, 1) : E <= 128 ? SS_RT(T, 2) : E <= 256 ? SS_RT(T, 4) : E <= 512 ? SS_RT(T, 8) : SS_RT(T, 16))
+#define SS_RT(T, EL) (k <= 16 ? launch_route<T, EL, 1> : launch_route<T, EL, RT_MAX_K / 16>)(logits, M, E, ld, k, renormalise != 0, ids, weights, slots, rows, offsets, static_cast<int32_t*>(workspace), hs)
+#define SS_RE(T) (E <= 64 ? SS_RT(T, 4) : E <= 128 ? SS_RT(T, 8) : E <= 256 ? SS_RT(T, 16) : SS_RT(T, 64))
     return in_dtype == SS_IN_F32 ? SS_RE(float) : SS_RE(uint16_t);
 #undef SS_RE
 #undef SS_RT
