@@ -147,7 +147,12 @@ struct mx4_call {
 // Tiles of 256 channels x 256 rows (mx4_tile.hip); rows of MX_TILE_UNITS units and more.
 constexpr int MX_TILE_UNITS = 3;
 ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
-// Tiles of 128 channels x 32, 64 or 128 rows (mx4_mid.hip).
-ss_status launch_mx4_mid(const mx4_call& c, int rows, hipStream_t stream);
+// Tiles of 128 channels x 32, 64 or 128 rows (mx4_mid.hip); more than one range of units: with a workspace of mx4_mid_bytes.
+ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream);
+inline size_t mx4_mid_bytes(int64_t R, int64_t E, int64_t frags, int rows, int ranges)
+{
+    const int64_t tiles = E > 1 ? mx4_max_tiles(R, E, rows) : (R + rows - 1) / rows;
+    return ranges > 1 ? (size_t)((frags + 3) / 4 * tiles * ranges) * 512 * rows : 0;
+}
 
 }  // namespace ss

@@ -129,34 +129,43 @@ using namespace ss;
 //   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
 //   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
 //   500 rows, 8 experts, 4096 -> 4096   36.3 | 33.5 | 30.3 | 23.2 | 30.2 | 29.6      4000 rows, 64 experts, 2048 -> 1408   62.4 | 61.8 | 38.1 | 34.8 | 43.8 | 39.0
+// Ranges of units (the second kernel, its launch and MB of sums: 3.5 us + 0.36 a MB), split over unsplit: 256 x 18944 -> 3584 25.5 | 33.8, 777 x 18944 -> 512 18.9 | 29.4,
+// 100 x 14336 -> 4096 16.3 | 22.7; 64 x 4096 -> 4096, whose estimate is against it, 9.5 | 6.2.
 // The kernel of 16 rows takes eight wavefronts, two units each ahead, where rows have 16 units and more, otherwise four (1 x 18944 -> 3584 10.3 against 12.4, 32 gated
 // rows of 8 experts 4096 -> 14336 83.7 against 88.6; 512 rows of 64 experts, 8 units, 26.4 against 22.2).
 constexpr int MX_MID = 1000;
-static int mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64_t cus)
+struct mx4_plan { int kernel, ranges; };
+static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64_t cus, size_t ws_bytes)
 {
     const double used = E > 1 ? (double)E * (1.0 - pow(1.0 - 1.0 / (double)E, (double)R)) : 1.0, ragged = E > 1 ? 1.2 : 1.0, MB = (double)(frags * U * (MX_FRAGB + MX_FRAGS)) / 1e6;
     const double hbm = used * MB / 5.2, panels = (double)((frags + 3) / 4), wide = (double)((frags + 7) / 8), u = (double)U;
     auto tiles = [&](int64_t T) { return E > 1 ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
     auto shares = [&](double workgroups) { return fmax(1.0, workgroups / (double)cus); };
-    const double full = fmin(1.0, wide * tiles(256) / (double)cus);
-    struct { int kernel; double us; } all[] = {
-        {16, 2.2 + fmax(fmax(MB * tiles(16) / 8.5 * ragged, 0.14 * u * fmax(1.0, (double)frags * tiles(16) / (double)(4 * cus))), hbm)},
-        {32, 2.5 + fmax(fmax(MB * tiles(32) / 6.0 * ragged, 0.18 * u), hbm)},
-        {MX_MID + 32, 2.0 + fmax((0.40 * u + 1.2) * ragged * shares(panels * tiles(32)), 1.1 * hbm + 1.0)},
-        {MX_MID + 64, 2.4 + fmax((0.44 * u + 1.3) * ragged * shares(panels * tiles(64)), 1.1 * hbm + 1.0)},
-        {MX_MID + 128, 2.6 + fmax((0.70 * u + 2.2) * ragged * shares(panels * tiles(128)), 1.15 * hbm + 1.0)},
-        {256, U < MX_TILE_UNITS ? 1e30 : 4.0 + fmax(((1.15 + 0.45 * full) * u + 1.5) * shares(wide * tiles(256)), hbm)},
+    mx4_plan best = {16, 1};
+    double time = 2.2 + fmax(fmax(MB * tiles(16) / 8.5 * ragged, 0.14 * u * fmax(1.0, (double)frags * tiles(16) / (double)(4 * cus))), hbm);
+    auto offer = [&](mx4_plan p, double us) {
+        if (us < time) { best = p; time = us; }
     };
-    int best = 0;
-    for (int i = 1; i < 6; ++i)
-        if (all[i].us < all[best].us) best = i;
-    return all[best].kernel;
+    offer({32, 1}, 2.5 + fmax(fmax(MB * tiles(32) / 6.0 * ragged, 0.18 * u), hbm));
+    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.3, 1.1}, {128, 2.6, 0.70, 2.2, 1.15}};
+    for (const auto& m : mid) {
+        const double w = panels * tiles(m.rows);
+        for (int r = 1; r <= 16 && r <= U; ++r) {
+            if (r > 1 && (mx4_mid_bytes(R, E, frags, m.rows, r) > ws_bytes || w * r > 2.0 * (double)cus)) break;
+            const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0;
+            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * ragged * shares(w * r), m.hbm * hbm + 1.0) + add);
+        }
+    }
+    if (U >= MX_TILE_UNITS) offer({256, 1}, 4.0 + fmax(((1.15 + 0.45 * fmin(1.0, wide * tiles(256) / (double)cus)) * u + 1.5) * shares(wide * tiles(256)), hbm));
+    return best;
 }
 
 extern "C" size_t mx4_gemm_workspace_bytes(int64_t R, int64_t E, int64_t O, int64_t K, int gated)
 {
-    (void)R; (void)E; (void)O; (void)K; (void)gated;
-    return 0;
+    if (R < 1 || R > MX_MAX_ROWS || E < 1 || E > MX_MAX_EXPERTS || O < 1 || O >= (1 << 22) || K < 1 || K > MX_MAX_K || (gated != 0 && gated != 1)) return 0;
+    const int64_t frags = mx4_frags(O << gated);
+    const mx4_plan p = mx4_choose(R, E, mx4_units(K), frags, cu_count(), SIZE_MAX);
+    return p.kernel > MX_MID ? mx4_mid_bytes(R, E, frags, p.kernel - MX_MID, p.ranges) : 0;
 }
 
 static ss_status mx4_product(bool grouped, const void* codes, const void* scales, const int32_t* offsets, const void* w_vals, const void* w_meta, int64_t R,
@@ -174,14 +183,13 @@ static ss_status mx4_product(bool grouped, const void* codes, const void* scales
                   static_cast<const uint8_t*>(w_meta), (int)R, (int)E, (int)O, (int)mx4_units(K), (int)mx4_frags(O << gated),
                   static_cast<uint16_t*>(Y), ldy, gated != 0};
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    switch (mx4_choose(R, E, c.U, c.frags, cu_count())) {
+    const mx4_plan p = mx4_choose(R, E, c.U, c.frags, cu_count(), workspace_bytes);
+    switch (p.kernel) {
     case 16: return c.U >= 16 ? launch_stream<8, 1, 2>(c, hs) : launch_stream<4, 1, 4>(c, hs);
     case 32: return launch_stream<4, 2, 4>(c, hs);
     case 256: return launch_mx4_tile(c, hs);
-    case MX_MID + 32: return launch_mx4_mid(c, 32, hs);
-    case MX_MID + 64: return launch_mx4_mid(c, 64, hs);
     }
-    return launch_mx4_mid(c, 128, hs);
+    return launch_mx4_mid(c, p.kernel - MX_MID, p.ranges, workspace, hs);
 }
 
 extern "C" ss_status mx4_gemm(const void* codes, const void* scales, const void* w_vals, const void* w_meta, int64_t M, int64_t O, int64_t K, int gated,

@@ -5,6 +5,9 @@
 // once more: 96 instead of 64 KB of LDS reads a unit.)  Operands go through a ring of D units in LDS, filled by direct loads.  The wavefronts meet
 // once a unit, when each of them holds its operands: the unit's slot is then free for unit u + D, and unit u + 1 has landed, whose
 // operands are read while unit u multiplies.
+//
+// With few tiles and long rows the units of a row are split into ranges, a workgroup each; their sums go through the workspace and a second kernel
+// adds them in the order of the ranges.
 #include "mx4_common.h"
 #include "mx4_loads.h"
 #include "device_info.h"
@@ -18,6 +21,7 @@ template <int FW, int TW, int WO, int WT, int KG, int D> struct MidShape {
     static constexpr int NB = ROWS >= 64 ? ROWS / 64 : 1;         // loads of token rows of a wavefront for a unit
     static constexpr int LOADS = 2 + NB;                          // all its loads, without those of the scales, which some have
     static constexpr int SUMS = 4 * FW * TW * 1024;               // bytes of the sums that a group hands over
+    static constexpr int BLOCKS = TW / KG, NV = 2 * FW * BLOCKS;  // blocks of rows that a wavefront finishes, vectors of four sums of them
     static_assert(FW * WO == 4 && WO * WT * KG == 8 && (KG == 1 || (KG == 2 && TW % 2 == 0 && SUMS * 2 <= LDS)) && LDS <= 160 * 1024, "whole shares");
 };
 
@@ -29,7 +33,7 @@ template <int A, int B> __device__ inline void mid_wait(int with)
 }
 
 template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
-__global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int tiles, Div by)
+__global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int tiles, Div by, Div by_items, KRanges ranges, int S_ranges, v4f* __restrict__ ws)
 {
     typedef MidShape<FW, TW, WO, WT, KG, D> S;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -38,7 +42,7 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     const int group = KG == 2 ? wave >> 2 : 0, wo = wave % WO, wt = wave / WO % WT, U = c.U;
     const uint32_t lds0 = lds_address(smem);
     // Neighbouring workgroups of an XCD share a panel's weights (dense) or a tile's rows (grouped).
-    const int item = xcd_run(blockIdx.x, panels * tiles), at = quot(item, by);
+    const int id = xcd_run(blockIdx.x, panels * tiles * S_ranges), range = quot(id, by_items), item = id - range * panels * tiles, at = quot(item, by);
     const int panel = GROUPED ? item - at * panels : at, slot = GROUPED ? at : item - at * tiles;
     mx4_rows t = {0, slot * S::ROWS, min(S::ROWS, c.R - slot * S::ROWS)};
     if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, S::ROWS, slot);
@@ -51,6 +55,11 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     const uint8_t* av = c.w_vals + (first_frag + min(panel * 4 + wave / 2, c.frags - 1)) * U * MX_FRAGB + (wave & 1) * 2048;
     const uint8_t* am = c.w_meta + (first_frag + panel * 4) * U * MX_FRAGS;
     const uint8_t *bv = c.codes + (int64_t)t.first * U * MX_UNITB, *bm = c.scales + (int64_t)t.first * MX_UNITS;
+    const int64_t begin = range_first(ranges, range);
+    av += begin * MX_FRAGB;
+    am += begin * MX_FRAGS;
+    bv += begin * MX_UNITB;
+    bm += begin * c.R * MX_UNITS;
     uint32_t boff[S::NB];
 #pragma unroll
     for (int i = 0; i < S::NB; ++i) {
@@ -82,7 +91,7 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     const uint32_t ra = wo * FW * MX_FRAGB + group * 2048 + lane * 16, rma = S::MA_OFF + wo * FW * MX_FRAGS + lane * 4;
     const uint32_t rb = S::B_OFF + (wt * TW * 16 + n) * ROWB + ((mx4_place(2 * q + group) ^ swz(n)) << 4), rmb = S::MB_OFF + (wt * TW * 16 + n) * MX_UNITS + 2 * q + group;
 
-    const int units = none ? 0 : U;
+    const int units = none ? 0 : range_units(ranges, range);
 #pragma unroll
     for (int d = 0; d < D; ++d) unroll<S::LOADS + 1>([&](auto p) __attribute__((always_inline)) { load(p, d * S::UNIT, d < units); });
     v4f acc[FW][2][TW];
@@ -123,7 +132,7 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
             acc[f][h][b] = mx4_mma<2 * h + T, T>(now.a[T][f][h], now.b[T][b], acc[f][h][b], now.sa[f], now.sb[b]);
             __builtin_amdgcn_sched_barrier(0);
             unroll<r1 - r0>([&](auto p) __attribute__((always_inline)) { read(std::integral_constant<int, r0 + decltype(p)::value>{}, next, here); });
-            unroll<l1 - l0>([&](auto p) __attribute__((always_inline)) { load(std::integral_constant<int, l0 + decltype(p)::value>{}, freed, u + D < U); });
+            unroll<l1 - l0>([&](auto p) __attribute__((always_inline)) { load(std::integral_constant<int, l0 + decltype(p)::value>{}, freed, u + D < units); });
             __builtin_amdgcn_sched_barrier(0);
         });
     };
@@ -137,7 +146,17 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
         unit(r1, r0, u + 1);
     }
     if (u < units) unit(r0, r1, u);
+    v4f* const partial = ws + ((((int64_t)range * panels * tiles + item) * 8 + wave) * S::NV) * 64 + lane;
     if constexpr (KG == 1) {
+        if (S_ranges > 1) {
+#pragma unroll
+            for (int b = 0; b < TW; ++b)
+#pragma unroll
+                for (int f = 0; f < FW; ++f)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) partial[((b * FW + f) * 2 + h) * 64] = acc[f][h][b];
+            return;
+        }
 #pragma unroll
         for (int b = 0; b < TW; ++b) {
             const int row = 16 * (wt * TW + b) + n;
@@ -172,7 +191,10 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
             for (int f = 0; f < FW; ++f) {
                 const v4f v = theirs[((b * FW + f) * 2) * 64], w = theirs[((b * FW + f) * 2 + 1) * 64];
                 const v4f x = acc[f][0][B0 + b], z = acc[f][1][B0 + b];
-                if (row < t.count) mx4_store8(G == 0 ? x + v : v + x, G == 0 ? z + w : w + z, y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
+                if (S_ranges > 1) {
+                    partial[((b * FW + f) * 2) * 64] = G == 0 ? x + v : v + x;
+                    partial[((b * FW + f) * 2 + 1) * 64] = G == 0 ? z + w : w + z;
+                } else if (row < t.count) mx4_store8(G == 0 ? x + v : v + x, G == 0 ? z + w : w + z, y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
             }
         }
     };
@@ -185,30 +207,60 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     }
 }
 
-template <int FW, int TW, int WO, int WT, int KG, int D> static ss_status launch(const mx4_call& c, hipStream_t stream)
+// adds the sums of the ranges, a thread what one lane of the workgroups before had
+template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
+__global__ __launch_bounds__(512) void k_mx4_mid_add(mx4_call c, int panels, int tiles, Div by, int S_ranges, const v4f* __restrict__ ws)
 {
     typedef MidShape<FW, TW, WO, WT, KG, D> S;
-    const int64_t panels = (c.frags + 3) / 4, tiles = c.offsets ? mx4_max_tiles(c.R, c.E, S::ROWS) : ((int64_t)c.R + S::ROWS - 1) / S::ROWS;
-    if (panels * tiles > INT32_MAX) return SS_ERR_SHAPE;
-    const dim3 grid((uint32_t)(panels * tiles));
-    if (c.offsets) {
-        if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, true>>(S::LDS) != SS_OK) return SS_ERR_HIP;
-        hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, true>), grid, dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, make_div(panels));
-    } else {
-        if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, false>>(S::LDS) != SS_OK) return SS_ERR_HIP;
-        hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, false>), grid, dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, make_div(tiles));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    const int group = KG == 2 ? wave >> 2 : 0, wo = wave % WO, wt = wave / WO % WT;
+    const int item = blockIdx.x, at = quot(item, by);
+    const int panel = GROUPED ? item - at * panels : at, slot = GROUPED ? at : item - at * tiles;
+    mx4_rows t = {0, slot * S::ROWS, min(S::ROWS, c.R - slot * S::ROWS)};
+    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, S::ROWS, slot);
+    if (t.count <= 0) return;
+    const v4f* from = ws + (((int64_t)item * 8 + wave) * S::NV) * 64 + lane;
+    const int64_t next = (int64_t)panels * tiles * 8 * S::NV * 64;
+    v4f sum[S::NV];
+#pragma unroll
+    for (int i = 0; i < S::NV; ++i) sum[i] = from[i * 64];
+    for (int r = 1; r < S_ranges; ++r) {
+        from += next;
+#pragma unroll
+        for (int i = 0; i < S::NV; ++i) sum[i] += from[i * 64];
     }
-    return launch_status();
+#pragma unroll
+    for (int b = 0; b < S::BLOCKS; ++b) {
+        const int row = 16 * (wt * TW + group * S::BLOCKS + b) + n;
+        if (row >= t.count) continue;
+        uint16_t* const y = c.Y + (int64_t)(t.first + row) * c.ldy;
+#pragma unroll
+        for (int f = 0; f < FW; ++f) mx4_store8(sum[(b * FW + f) * 2], sum[(b * FW + f) * 2 + 1], y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
+    }
 }
 
-ss_status launch_mx4_mid(const mx4_call& c, int rows, hipStream_t stream)
+template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED> static ss_status launch_kind(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
 {
-    switch (rows) {
-    case 32: return launch<1, 2, 4, 1, 2, 3>(c, stream);
-    case 64: return launch<2, 2, 2, 2, 2, 3>(c, stream);
-    case 128: return launch<2, 2, 2, 4, 1, 4>(c, stream);
-    }
-    return SS_ERR_SHAPE;
+    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    const int64_t panels = (c.frags + 3) / 4, tiles = GROUPED ? mx4_max_tiles(c.R, c.E, S::ROWS) : ((int64_t)c.R + S::ROWS - 1) / S::ROWS, items = panels * tiles;
+    if (items * ranges > INT32_MAX) return SS_ERR_SHAPE;
+    if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>>(S::LDS) != SS_OK) return SS_ERR_HIP;
+    const Div by = make_div(GROUPED ? panels : tiles);
+    hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>), dim3((uint32_t)(items * ranges)), dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, by, make_div(items),
+                       k_ranges(c.U, ranges), ranges, static_cast<v4f*>(ws));
+    if (launch_status() != SS_OK) return SS_ERR_HIP;
+    if (ranges == 1) return SS_OK;
+    hipLaunchKernelGGL((k_mx4_mid_add<FW, TW, WO, WT, KG, D, GROUPED>), dim3((uint32_t)items), dim3(512), 0, stream, c, (int)panels, (int)tiles, by, ranges, static_cast<const v4f*>(ws));
+    return launch_status();
+}
+template <int FW, int TW, int WO, int WT, int KG, int D> static ss_status launch(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
+{
+    return c.offsets ? launch_kind<FW, TW, WO, WT, KG, D, true>(c, ranges, ws, stream) : launch_kind<FW, TW, WO, WT, KG, D, false>(c, ranges, ws, stream);
+}
+
+ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream)
+{
+    return rows == 32 ? launch<1, 2, 4, 1, 2, 3>(c, ranges, ws, stream) : rows == 64 ? launch<2, 2, 2, 2, 2, 3>(c, ranges, ws, stream) : launch<2, 2, 2, 4, 1, 4>(c, ranges, ws, stream);
 }
 
 }  // namespace ss

@@ -214,3 +214,111 @@ def test_refused_tensors():
         binding.mx4_gemm(codes, scales, *w, 64, 300, out=torch.empty((4, 64), device=DEV))
     with pytest.raises(TypeError):
         binding.mx4_grouped_gemm(codes, scales, torch.tensor([0, 4], device=DEV), *w, 64, 300)
+
+
+def _sampled(rows, cols, codes, scales, w_codes, w_scales, gated, dev=DEV):
+    """The products of some rows and columns of Y in 64 bits, from codes on the GPU, and the bound of 32-bit sums."""
+    def values(c, s):
+        c = c.cpu().numpy()
+        code = np.stack([c & 15, c >> 4], axis=-1).reshape(c.shape[0], -1, 256)
+        return mo.values(code, s.cpu().numpy().transpose(1, 0, 2))
+
+    xv = values(codes[rows], scales[:, rows].contiguous())
+    n = w_codes.shape[0] // 2
+    wi = torch.cat([cols, cols + n]) if gated else cols
+    return mo.product(xv, values(w_codes[wi], w_scales[:, wi].contiguous()), gated)
+
+
+# every kernel and several rounds of each: tiles of 256 x 256 (more of them than compute units, an odd last tile, rows of three units and of many), of 128 channels
+# with 32, 64 and 128 rows, ranges of units, few tokens on long rows
+FULL = [(4099, 800, 9001, False), (2100, 5120, 4224, False), (1500, 3584, 8200, True), (2304, 768, 16384, False), (777, 5003, 4099, False), (600, 4096, 4096, True),
+        (200, 4096, 14336, False), (100, 4096, 14336, False), (256, 18944, 3584, False), (100, 14336, 4096, True), (777, 18944, 512, False), (48, 3584, 37888, False),
+        (1, 18944, 3584, False), (17, 3584, 18944, True), (40, 600, 600, False)]
+
+
+@pytest.mark.parametrize("M,K,O,gated", FULL)
+def test_gemm_of_full_size(M, K, O, gated):
+    g = torch.Generator(device=DEV).manual_seed(M + K + O)
+    codes, scales = binding.mx4_quant(torch.randn((M, K), generator=g, device=DEV))
+    wc, ws_ = binding.mx4_quant(0.02 * torch.randn((O << gated, K), generator=g, device=DEV))
+    w = binding.mx4_pack(wc, ws_, K, gated=gated)
+    rng = np.random.default_rng(M)
+    rows = torch.from_numpy(np.unique(np.concatenate([rng.integers(0, M, 40), [0, M - 1]]))).to(DEV)
+    cols = torch.from_numpy(np.unique(np.concatenate([rng.integers(0, O, 60), [0, O - 1]]))).to(DEV)
+    ref, off = _sampled(rows, cols, codes, scales, wc, ws_, gated)
+    n = binding.mx4_gemm_workspace_bytes(M, O, K, gated=gated)
+    for ws in [None] + ([torch.full((n,), 0x5A, dtype=torch.uint8, device=DEV)] if n else []):
+        Y = binding.mx4_gemm(codes, scales, *w, O, K, gated=gated, workspace=ws)
+        check_product(Y[rows][:, cols], ref, off)
+        if ws is not None:
+            assert bool((ws != 0x5A).any())
+    assert not bool(Y.isnan().any())
+
+
+def test_long_rows_ask_for_a_workspace():
+    assert binding.mx4_gemm_workspace_bytes(256, 3584, 18944) > 0 and binding.mx4_gemm_workspace_bytes(8192, 37888, 3584) == 0
+    assert binding.mx4_gemm_workspace_bytes(0, 64, 64) == binding.mx4_gemm_workspace_bytes(4, 64, 64, experts=1025) == 0
+
+
+GROUPED_FULL = [(8192, 8, 4096, 2048, False), (3000, 5, 2304, 1500, True), (2000, 64, 2048, 1408, False), (500, 8, 4096, 4096, False), (32, 8, 4096, 1024, True), (1200, 4, 8192, 512, False)]
+
+
+@pytest.mark.parametrize("R,E,K,O,gated", GROUPED_FULL)
+def test_grouped_of_full_size(R, E, K, O, gated):
+    g = torch.Generator(device=DEV).manual_seed(R + E)
+    off = groups("skewed", R, E, np.random.default_rng(R))
+    codes, scales = binding.mx4_quant(torch.randn((R, K), generator=g, device=DEV))
+    rows_e = O << gated
+    wc, ws_ = binding.mx4_quant(0.02 * torch.randn((E * rows_e, K), generator=g, device=DEV))
+    w = binding.mx4_pack(wc, ws_, K, experts=E, gated=gated)
+    n = binding.mx4_gemm_workspace_bytes(R, O, K, experts=E, gated=gated)
+    offsets = torch.from_numpy(off.astype(np.int32)).to(DEV)
+    rng = np.random.default_rng(E)
+    cols = torch.from_numpy(np.unique(np.concatenate([rng.integers(0, O, 40), [0, O - 1]]))).to(DEV)
+    for ws in [None] + ([torch.full((n,), 0x5A, dtype=torch.uint8, device=DEV)] if n else []):
+        Y = binding.mx4_grouped_gemm(codes, scales, offsets, *w, O, K, gated=gated, workspace=ws)
+        for e in range(E):
+            if off[e + 1] > off[e]:
+                rows = torch.from_numpy(np.unique(np.concatenate([rng.integers(off[e], off[e + 1], 8), [off[e], off[e + 1] - 1]]))).to(DEV)
+                part = slice(e * rows_e, (e + 1) * rows_e)
+                ref, tol = _sampled(rows, cols, codes, scales, wc[part], ws_[:, part], gated)
+                check_product(Y[rows][:, cols], ref, tol)
+        assert not bool(Y[off[-1]:].any())
+
+
+def test_replayed_graph():
+    """Captured calls, replayed several times with eager work between: the results of eager calls each time."""
+    K, O, E = 1024, 256, 4
+    X = torch.randn((300, K), device=DEV).to(torch.bfloat16)
+    logits = torch.randn((300, E), device=DEV)
+    w = binding.mx4_pack(*binding.mx4_quant(torch.randn((E * 2 * O, K), device=DEV)), K, experts=E, gated=True)
+    ws = torch.empty((max(16, binding.mx4_gemm_workspace_bytes(600, O, K, experts=E, gated=True)),), dtype=torch.uint8, device=DEV)
+
+    def step():
+        ids, weights, slots, rows, offsets = binding.expert_route(logits, 2)
+        codes, scales = binding.mx4_quant(X, rows=rows)
+        return binding.expert_combine(binding.mx4_grouped_gemm(codes, scales, offsets, *w, O, K, gated=True, workspace=ws), slots, weights)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(4):
+        X.copy_(torch.randn((300, K), device=DEV))
+        logits.copy_(torch.randn((300, E), device=DEV))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, step())
+
+
+def test_another_stream():
+    X, W = torch.randn((40, 512), device=DEV), torch.randn((64, 512), device=DEV)
+    want = binding.mx4_gemm(*binding.mx4_quant(X), *binding.mx4_pack(*binding.mx4_quant(W), 512), 64, 512)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        got = binding.mx4_gemm(*binding.mx4_quant(X), *binding.mx4_pack(*binding.mx4_quant(W), 512), 64, 512)
+    stream.synchronize()
+    assert torch.equal(got, want)
