@@ -203,41 +203,58 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_place(const int32_t* __res
     }
 }
 
+// sixteen bytes at the alignment of an element
 typedef uint32_t row16_t __attribute__((ext_vector_type(4), aligned(2)));
 
-// A thread takes eight columns of a token.
+// eight columns of a row, `have` of which exist
+__device__ inline void get8(const uint16_t* p, int have, float (&f)[8])
+{
+    if (have == 8) {
+        const row16_t v = __builtin_nontemporal_load(reinterpret_cast<const row16_t*>(p));      // read once
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(v[j] << 16); f[2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = j < have ? bf16_bits_to_f32(p[j]) : 0.0f;
+    }
+}
+
+// A thread takes eight columns of a token; with a known number of rows (K > 0) it asks for all of them before it adds the first.
+template <int K>
 __global__ __launch_bounds__(256) void k_combine(const uint16_t* __restrict__ Y, int64_t R, int64_t O, int64_t ldy, const int32_t* __restrict__ slots,
                                                  const float* __restrict__ weights, int64_t M, int k, const uint16_t* __restrict__ base, int64_t ldb,
                                                  uint16_t* __restrict__ out, int64_t ldo, int64_t per_row)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per_row, o = (i - m * per_row) * 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = per_row == 1 ? i : i / per_row, o = (i - m * per_row) * 8;
     if (m >= M) return;
     const int have = (int)min((int64_t)8, O - o);
     float a[8];
-    auto get = [&](const uint16_t* p, float (&f)[8]) {
-        if (have == 8) {
-            const row16_t v = *reinterpret_cast<const row16_t*>(p);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(v[j] << 16); f[2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u); }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = j < have ? bf16_bits_to_f32(p[j]) : 0.0f;
-        }
-    };
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = 0.0f;
-    for (int q = 0; q < k; ++q) {
-        const int64_t s = slots[m * k + q];
-        if (s < 0 || s >= R) continue;
-        const float w = weights[m * k + q];
-        float f[8];
-        get(Y + s * ldy + o, f);
+    if constexpr (K > 0) {
+        int s[K];
+        float w[K], f[K][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a[j] = fmaf(w, f[j], a[j]);
+        for (int q = 0; q < K; ++q) { s[q] = slots[m * K + q]; w[q] = weights[m * K + q]; }
+#pragma unroll
+        for (int q = 0; q < K; ++q) get8(Y + (s[q] >= 0 && s[q] < R ? s[q] : 0) * ldy + o, R > 0 ? have : 0, f[q]);
+#pragma unroll
+        for (int q = 0; q < K; ++q)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = s[q] >= 0 && s[q] < R ? fmaf(w[q], f[q][j], a[j]) : a[j];
+    } else {
+        for (int q = 0; q < k; ++q) {
+            const int64_t s = slots[m * k + q];
+            if (s < 0 || s >= R) continue;
+            float f[8];
+            get8(Y + s * ldy + o, have, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = fmaf(weights[m * k + q], f[j], a[j]);
+        }
     }
     if (base) {
         float f[8];
-        get(base + m * ldb + o, f);
+        get8(base + m * ldb + o, have, f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) a[j] += f[j];
     }
@@ -314,7 +331,16 @@ extern "C" ss_status expert_combine(const void* Y, int64_t R, int64_t O, int64_t
     if ((((uintptr_t)Y | (uintptr_t)base | (uintptr_t)out) & 1) || (((uintptr_t)slots | (uintptr_t)weights) & 3)) return SS_ERR_SHAPE;
     const int64_t per_row = (O + 7) / 8, blocks = (M * per_row + 255) / 256;
     if (blocks > INT32_MAX) return SS_ERR_SHAPE;
-    hipLaunchKernelGGL(k_combine, dim3((uint32_t)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(Y), R, O, ldy, slots, weights, M, k,
-                       static_cast<const uint16_t*>(base), ldb, static_cast<uint16_t*>(out), ldo, per_row);
-    return launch_status();
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(Y), R, O, ldy, slots, weights, M, k,
+                           static_cast<const uint16_t*>(base), ldb, static_cast<uint16_t*>(out), ldo, per_row);
+        return launch_status();
+    };
+    switch (k) {
+    case 1: return launch(k_combine<1>);
+    case 2: return launch(k_combine<2>);
+    case 4: return launch(k_combine<4>);
+    case 8: return launch(k_combine<8>);
+    }
+    return launch(k_combine<0>);
 }

@@ -151,8 +151,7 @@ ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
 ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream);
 inline size_t mx4_mid_bytes(int64_t R, int64_t E, int64_t frags, int rows, int ranges)
 {
-    const int64_t tiles = E > 1 ? mx4_max_tiles(R, E, rows) : (R + rows - 1) / rows;
-    return ranges > 1 ? (size_t)((frags + 3) / 4 * tiles * ranges) * 512 * rows : 0;
+    return ranges > 1 ? (size_t)((frags + 3) / 4 * mx4_max_tiles(R, E, rows) * ranges) * 512 * rows : 0;      // a grouped call of one expert has more tiles than a dense one
 }
 
 }  // namespace ss

@@ -13,8 +13,9 @@ __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
     constexpr int ACC = FW * TB * 2;                     // blocks of 16 x 16
     __shared__ __attribute__((aligned(16))) float part[W][ACC][4][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    mx4_rows t = {0, (int)blockIdx.y * 16 * TB, min(16 * TB, c.R - (int)blockIdx.y * 16 * TB)};
-    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 16 * TB, blockIdx.y);
+    const int slot = blockIdx.z * gridDim.y + blockIdx.y;
+    mx4_rows t = {0, slot * 16 * TB, min(16 * TB, c.R - slot * 16 * TB)};
+    if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 16 * TB, slot);
     if (t.count <= 0) return;
     const bool none = GROUPED && t.expert == c.E;
     const int f0 = blockIdx.x * FW;
@@ -108,8 +109,8 @@ __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
 template <int W, int TB, int DEPTH> static ss_status launch_stream(const mx4_call& c, hipStream_t stream)
 {
     const int64_t tiles = c.offsets ? mx4_max_tiles(c.R, c.E, 16 * TB) : ((int64_t)c.R + 16 * TB - 1) / (16 * TB);
-    if (tiles > 65535) return SS_ERR_SHAPE;
-    const dim3 grid((uint32_t)c.frags, (uint32_t)tiles);
+    const int64_t layers = (tiles + 65534) / 65535;      // of the grid's third dimension
+    const dim3 grid((uint32_t)c.frags, (uint32_t)((tiles + layers - 1) / layers), (uint32_t)layers);
     if (c.offsets) hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, true>), grid, dim3(64 * W), 0, stream, c);
     else hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, false>), grid, dim3(64 * W), 0, stream, c);
     return launch_status();

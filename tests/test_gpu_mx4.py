@@ -260,7 +260,8 @@ def test_long_rows_ask_for_a_workspace():
     assert binding.mx4_gemm_workspace_bytes(0, 64, 64) == binding.mx4_gemm_workspace_bytes(4, 64, 64, experts=1025) == 0
 
 
-GROUPED_FULL = [(8192, 8, 4096, 2048, False), (3000, 5, 2304, 1500, True), (2000, 64, 2048, 1408, False), (500, 8, 4096, 4096, False), (32, 8, 4096, 1024, True), (1200, 4, 8192, 512, False)]
+GROUPED_FULL = [(8192, 8, 4096, 2048, False), (3000, 5, 2304, 1500, True), (2000, 64, 2048, 1408, False), (500, 8, 4096, 4096, False), (32, 8, 4096, 1024, True), (1200, 4, 8192, 512, False),
+                (256, 1, 18944, 512, False)]
 
 
 @pytest.mark.parametrize("R,E,K,O,gated", GROUPED_FULL)
@@ -322,3 +323,14 @@ def test_another_stream():
         got = binding.mx4_gemm(*binding.mx4_quant(X), *binding.mx4_pack(*binding.mx4_quant(W), 512), 64, 512)
     stream.synchronize()
     assert torch.equal(got, want)
+
+
+def test_more_tiles_than_a_grid_is_high():
+    M, K, O = 1100000, 64, 16
+    g = torch.Generator(device=DEV).manual_seed(1)
+    codes, scales = binding.mx4_quant(torch.randn((M, K), generator=g, device=DEV))
+    wc, ws_ = binding.mx4_quant(torch.randn((O, K), generator=g, device=DEV))
+    Y = binding.mx4_gemm(codes, scales, *binding.mx4_pack(wc, ws_, K), O, K)
+    rows = torch.cat([torch.arange(0, M, 9999), torch.tensor([M - 1, 65535 * 16, 65535 * 16 + 1, 65535 * 16 - 1])]).to(DEV)
+    ref, off = _sampled(rows, torch.arange(O, device=DEV), codes, scales, wc, ws_, False)
+    check_product(Y[rows], ref, off)
