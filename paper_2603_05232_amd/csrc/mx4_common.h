@@ -144,8 +144,7 @@ struct mx4_call {
     bool gated;
 };
 
-// Tiles of 256 channels x 256 rows (mx4_tile.hip); rows of MX_TILE_UNITS units and more.
-constexpr int MX_TILE_UNITS = 3;
+// Tiles of 256 channels x 256 rows (mx4_tile.hip).
 ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
 // Tiles of 128 channels x 32, 64 or 128 rows (mx4_mid.hip); more than one range of units: with a workspace of mx4_mid_bytes.
 ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream);

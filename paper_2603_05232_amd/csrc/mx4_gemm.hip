@@ -123,12 +123,14 @@ using namespace ss;
 // The kernel of a product: tiles of 16 or 32 rows of the kernel for few tokens, MX_MID + 32, 64 or 128 rows of mx4_mid.hip, 256 of mx4_tile.hip.  Which is the
 // fastest goes by an estimate of every kernel's time in us: its launch, then the longest of what its workgroups take one after the other (time of a
 // unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
-// rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The group sizes lie on the device: E experts are taken to have R / E rows
-// each, and half a tile more.  Constants fitted to the times of all six on 68 shapes (R = 1 .. 16000, 1 .. 74 units, 512 .. 37888 channels, 1 to 128
-// experts): the choice is 1.03 of the fastest on average, 1.26 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+// rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The tiles of 256 rows go in rounds of one for each compute unit; the last
+// round, where most stand still, is shorter, the less of them it has.  The group sizes lie on the device: E experts are taken to have R / E rows
+// each, and half a tile more.  Constants fitted to the times of all six on 92 shapes (R = 1 .. 54000, 1 .. 74 units, 360 .. 37888 channels, 1 to 128
+// experts): the choice is 1.03 of the fastest on average, 1.45 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
 //   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       46.2 |  36.7 |  25.5 | 18.3 | 16.6 | 26.4
 //   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
 //   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
+//   8192 x 256 -> 512          17.4 |  17.8 |   8.9 |   6.7 |   5.9 | 10.1      4000 x 256 -> 4096        56.6 |  59.5 |  26.4 | 18.5 | 16.5 | 13.7
 //   500 rows, 8 experts, 4096 -> 4096   36.3 | 33.5 | 30.3 | 23.2 | 30.2 | 29.6      4000 rows, 64 experts, 2048 -> 1408   62.4 | 61.8 | 38.1 | 34.8 | 43.8 | 39.0
 // Ranges of units (the second kernel, its launch and MB of sums: 3.5 us + 0.36 a MB), split over unsplit: 256 x 18944 -> 3584 25.5 | 33.8, 777 x 18944 -> 512 18.9 | 29.4,
 // 100 x 14336 -> 4096 16.3 | 22.7; 64 x 4096 -> 4096, whose estimate is against it, 9.5 | 6.2.
@@ -138,26 +140,32 @@ constexpr int MX_MID = 1000;
 struct mx4_plan { int kernel, ranges; };
 static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64_t cus, size_t ws_bytes)
 {
-    const double used = E > 1 ? (double)E * (1.0 - pow(1.0 - 1.0 / (double)E, (double)R)) : 1.0, ragged = E > 1 ? 1.2 : 1.0, MB = (double)(frags * U * (MX_FRAGB + MX_FRAGS)) / 1e6;
+    const bool many = E > 1;
+    const double used = many ? (double)E * (1.0 - pow(1.0 - 1.0 / (double)E, (double)R)) : 1.0, MB = (double)(frags * U * (MX_FRAGB + MX_FRAGS)) / 1e6;
     const double hbm = used * MB / 5.2, panels = (double)((frags + 3) / 4), wide = (double)((frags + 7) / 8), u = (double)U;
-    auto tiles = [&](int64_t T) { return E > 1 ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
-    auto shares = [&](double workgroups) { return fmax(1.0, workgroups / (double)cus); };
-    mx4_plan best = {16, 1};
-    double time = 2.2 + fmax(fmax(MB * tiles(16) / 8.5 * ragged, 0.14 * u * fmax(1.0, (double)frags * tiles(16) / (double)(4 * cus))), hbm);
+    auto tiles = [&](int64_t T) { return many ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
+    mx4_plan best = {};
+    double time = INFINITY;
     auto offer = [&](mx4_plan p, double us) {
         if (us < time) { best = p; time = us; }
     };
-    offer({32, 1}, 2.5 + fmax(fmax(MB * tiles(32) / 6.0 * ragged, 0.18 * u), hbm));
-    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.3, 1.1}, {128, 2.6, 0.70, 2.2, 1.15}};
+    const struct { int rows; double launch, rate, row, start, unit; } few[] = {{16, 2.2, 8.5, 0.14, 0.40, 0.045}, {32, 2.5, 6.0, 0.18, 0.82, 0.08}};
+    for (const auto& f : few) {
+        const double t = tiles(f.rows), shares = (double)frags * t / (double)cus;
+        offer({f.rows, 1}, f.launch + fmax(fmax(MB * t / f.rate * (many ? 1.2 : 1.0), f.row * u), fmax((f.start + f.unit * u) * (many ? 1.4 : 1.0) * shares, hbm)));
+    }
+    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.4, 1.1}, {128, 2.6, 0.70, 2.4, 1.15}};
     for (const auto& m : mid) {
         const double w = panels * tiles(m.rows);
         for (int r = 1; r <= 16 && r <= U; ++r) {
             if (r > 1 && (mx4_mid_bytes(R, E, frags, m.rows, r) > ws_bytes || w * r > 2.0 * (double)cus)) break;
-            const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0;
-            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * ragged * shares(w * r), m.hbm * hbm + 1.0) + add);
+            const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0, shares = fmax(1.0, w * r / (double)cus);
+            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * (many ? 1.5 : 1.0) * shares, m.hbm * hbm + 1.0) + add);
         }
     }
-    if (U >= MX_TILE_UNITS) offer({256, 1}, 4.0 + fmax(((1.15 + 0.45 * fmin(1.0, wide * tiles(256) / (double)cus)) * u + 1.5) * shares(wide * tiles(256)), hbm));
+    const double all = wide * tiles(256) / (double)cus, part = all - floor(all), full = fmin(1.0, all);
+    const double rounds = all <= 1.0 ? 1.0 : floor(all) + (part > 0.0 ? fmin(1.0, 0.5 + part) : 0.0);
+    offer({256, 1}, 4.8 + fmax(rounds * (fmax(u, 3.0) * (1.15 + 0.45 * full) + (1.5 + 2.3 * full) * (many ? 1.6 : 1.0)), hbm));
     return best;
 }
 

@@ -64,15 +64,18 @@ __device__ inline void xt_store(const v4f (&acc)[8][4], bool zeros, uint16_t* __
     }
 }
 
-// Rows of at least three units.
-template <bool GROUPED>
+__device__ const uint4 mx4_zeros[256] = {};            // a fragment's codes of a unit that rows lack, and the scales of anything
+
+// The requests run up to three units ahead and into the next tile only, so a tile has at least three.  SHORT: rows have fewer; the units that they lack are
+// zeros times what lies in the first unit, with zeros as scale bytes on both sides.
+template <bool GROUPED, bool SHORT>
 __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wo = wave & 1, wt = wave >> 1, n = lane & 15, q = lane >> 4;
     const uint32_t lds0 = lds_address(smem);
-    const int U = c.U;
+    const int U = SHORT ? 3 : c.U;
     int32_t* const tile_end = reinterpret_cast<int32_t*>(smem + XT_LDS);
     int32_t* const row_end = tile_end + MX_MAX_EXPERTS;
 
@@ -128,18 +131,20 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     // rows 64 (wave / 2) + 16 b + 8 (wave % 2) .. + 7, as [row & 15][half of a unit][b 4] words.
     struct Weights { const uint8_t *v, *m; } pa;
     struct Rows { const uint8_t *v, *m; } pb;
+    int ua = 0, ub = 0;                                  // SHORT: the units that the requests are at
     uint32_t boff[4], bmoff = 0;
     auto weights_of = [&](const Tile& t) -> Weights {
-        const int64_t at = ((int64_t)(GROUPED && t.expert == c.E ? 0 : t.expert) * c.frags + min(t.o * 8 + wave, c.frags - 1)) * U;
+        const int64_t at = ((int64_t)(GROUPED && t.expert == c.E ? 0 : t.expert) * c.frags + min(t.o * 8 + wave, c.frags - 1)) * c.U;
         return {c.w_vals + at * MX_FRAGB, c.w_meta + at * MX_FRAGS};
     };
     auto set_rows = [&](const Tile& t) {
         const int ln = fresh_lane();
-        pb = {c.codes + (int64_t)t.first * U * MX_UNITB, c.scales + (int64_t)t.first * MX_UNITS};
+        pb = {c.codes + (int64_t)t.first * c.U * MX_UNITB, c.scales + (int64_t)t.first * MX_UNITS};
+        ub = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = 8 * (8 * i + wave) + (ln >> 3);
-            boff[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)(U * MX_UNITB) + mx4_place((ln & 7) ^ swz(row)) * 16;
+            boff[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)(c.U * MX_UNITB) + mx4_place((ln & 7) ^ swz(row)) * 16;
         }
         bmoff = (uint32_t)min((wave >> 1) * 64 + 16 * (ln & 3) + (wave & 1) * 8 + (ln >> 3), t.rows - 1) * MX_UNITS + (ln & 4);
     };
@@ -152,8 +157,17 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     auto load_ma = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pa.m, lane4, ma_wave + slot, more, more); };
     auto load_b = [&](int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
     auto load_mb = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pb.m, bmoff, mb_wave + slot, more, more); };
-    auto next_a = [&]() __attribute__((always_inline)) { pa.v += MX_FRAGB; pa.m += MX_FRAGS; };
-    auto next_b = [&]() __attribute__((always_inline)) { pb.v += MX_UNITB; pb.m += mb_next; };
+    const uint8_t* const zeros_at = reinterpret_cast<const uint8_t*>(mx4_zeros);
+    auto next_a = [&]() __attribute__((always_inline)) {
+        const bool none = SHORT && ++ua >= c.U;
+        pa.v = none ? zeros_at : pa.v + MX_FRAGB;
+        pa.m = none ? zeros_at : pa.m + MX_FRAGS;
+    };
+    auto next_b = [&]() __attribute__((always_inline)) {
+        const bool none = SHORT && ++ub >= c.U;
+        pb.v += none ? 0 : MX_UNITB;                     // anything that is there
+        pb.m = none ? zeros_at : pb.m + mb_next;
+    };
 
     // LDS offsets of this lane's operand reads
     const uint32_t ra = wo * 8192 + lane * 16;
@@ -285,6 +299,7 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         const bool wrap = u == U - 2;
         pa.v = wrap ? then.v : pa.v;
         pa.m = wrap ? then.m : pa.m;
+        if (SHORT) ua = wrap ? 0 : ua;
         more_a = wrap ? (uint32_t)-have : more_a;
         step(std::integral_constant<int, 1>{}, waits);
         next_b();
@@ -311,15 +326,16 @@ ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream)
 {
     const int64_t tiles_o = (c.frags + 7) / 8, most = tiles_o * (c.offsets ? mx4_max_tiles(c.R, c.E, BT) : ((int64_t)c.R + BT - 1) / BT);
     if (most > INT32_MAX / 2) return SS_ERR_SHAPE;
-    const int cus = cu_count(), grid = (int)(most < cus ? most : cus);
-    if (c.offsets) {
-        if (allow_dynamic_lds<k_mx4_tile<true>>(XT_LDS + XT_ENDS) != SS_OK) return SS_ERR_HIP;
-        hipLaunchKernelGGL(k_mx4_tile<true>, dim3(grid), dim3(512), XT_LDS + XT_ENDS, stream, c, (int)tiles_o);
-    } else {
-        if (allow_dynamic_lds<k_mx4_tile<false>>(XT_LDS) != SS_OK) return SS_ERR_HIP;
-        hipLaunchKernelGGL(k_mx4_tile<false>, dim3(grid), dim3(512), XT_LDS, stream, c, (int)tiles_o);
-    }
-    return launch_status();
+    const int cus = cu_count(), grid = (int)(most < cus ? most : cus), lds = XT_LDS + (c.offsets ? XT_ENDS : 0);
+    auto launch = [&](auto allow, auto kernel) {
+        if (allow != SS_OK) return SS_ERR_HIP;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(512), lds, stream, c, (int)tiles_o);
+        return launch_status();
+    };
+#define SS_XT(G, S) launch(allow_dynamic_lds<k_mx4_tile<G, S>>(lds), k_mx4_tile<G, S>)
+    if (c.offsets) return c.U < 3 ? SS_XT(true, true) : SS_XT(true, false);
+    return c.U < 3 ? SS_XT(false, true) : SS_XT(false, false);
+#undef SS_XT
 }
 
 }  // namespace ss

@@ -230,10 +230,11 @@ def _sampled(rows, cols, codes, scales, w_codes, w_scales, gated, dev=DEV):
 
 
 # every kernel and several rounds of each: tiles of 256 x 256 (more of them than compute units, an odd last tile, rows of three units and of many), of 128 channels
-# with 32, 64 and 128 rows, ranges of units, few tokens on long rows
+# with 32, 64 and 128 rows, ranges of units, few tokens on long rows, rows of one and two units by enough tiles that those of 256 x 256 take them
 FULL = [(4099, 800, 9001, False), (2100, 5120, 4224, False), (1500, 3584, 8200, True), (2304, 768, 16384, False), (777, 5003, 4099, False), (600, 4096, 4096, True),
         (200, 4096, 14336, False), (100, 4096, 14336, False), (256, 18944, 3584, False), (100, 14336, 4096, True), (777, 18944, 512, False), (48, 3584, 37888, False),
-        (1, 18944, 3584, False), (17, 3584, 18944, True), (40, 600, 600, False)]
+        (1, 18944, 3584, False), (17, 3584, 18944, True), (40, 600, 600, False),
+        (4000, 256, 4096, False), (1000, 512, 16384, True), (1030, 31, 16450, False), (8200, 300, 4100, True), (2500, 512, 33, False)]
 
 
 @pytest.mark.parametrize("M,K,O,gated", FULL)
@@ -261,7 +262,7 @@ def test_long_rows_ask_for_a_workspace():
 
 
 GROUPED_FULL = [(8192, 8, 4096, 2048, False), (3000, 5, 2304, 1500, True), (2000, 64, 2048, 1408, False), (500, 8, 4096, 4096, False), (32, 8, 4096, 1024, True), (1200, 4, 8192, 512, False),
-                (256, 1, 18944, 512, False)]
+                (256, 1, 18944, 512, False), (8000, 16, 512, 2048, False), (16000, 5, 256, 1030, True), (3000, 128, 200, 400, False)]
 
 
 @pytest.mark.parametrize("R,E,K,O,gated", GROUPED_FULL)
