@@ -146,6 +146,9 @@ struct mx4_call {
 
 // Tiles of 256 channels x 256 rows (mx4_tile.hip).
 ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
+// Tiles of 128 channels x 16 or 32 rows (mx4_short.hip); rows of at most MX_SHORT_UNITS units.
+constexpr int MX_SHORT_UNITS = 4;
+ss_status launch_mx4_short(const mx4_call& c, int rows, hipStream_t stream);
 // Tiles of 128 channels x 32, 64 or 128 rows (mx4_mid.hip); more than one range of units: with a workspace of mx4_mid_bytes.
 ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream);
 inline size_t mx4_mid_bytes(int64_t R, int64_t E, int64_t frags, int rows, int ranges)

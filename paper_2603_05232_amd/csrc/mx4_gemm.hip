@@ -120,23 +120,28 @@ template <int W, int TB, int DEPTH> static ss_status launch_stream(const mx4_cal
 
 using namespace ss;
 
-// The kernel of a product: tiles of 16 or 32 rows of the kernel for few tokens, MX_MID + 32, 64 or 128 rows of mx4_mid.hip, 256 of mx4_tile.hip.  Which is the
-// fastest goes by an estimate of every kernel's time in us: its launch, then the longest of what its workgroups take one after the other (time of a
+// The kernel of a product: tiles of 16 or 32 rows of the kernel for few tokens, MX_SHORT + 16 or 32 of mx4_short.hip (rows of MX_SHORT_UNITS and fewer), MX_MID + 32,
+// 64 or 128 of mx4_mid.hip, 256 of mx4_tile.hip.  Which is the fastest goes by an estimate of every kernel's time in us: its launch, then the longest of what its workgroups take one after the other (time of a
 // unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
 // rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The tiles of 256 rows go in rounds of one for each compute unit; the last
 // round, where most stand still, is shorter, the less of them it has.  The group sizes lie on the device: E experts are taken to have R / E rows
-// each, and half a tile more.  Constants fitted to the times of all six on 92 shapes (R = 1 .. 54000, 1 .. 74 units, 360 .. 37888 channels, 1 to 128
-// experts): the choice is 1.03 of the fastest on average, 1.45 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+// each, and half a tile more.  Constants fitted to the times of all on 104 shapes (R = 1 .. 54000, 1 .. 74 units, 360 .. 37888 channels, 1 to 128
+// experts): the choice is 1.03 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
 //   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       46.2 |  36.7 |  25.5 | 18.3 | 16.6 | 26.4
 //   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
 //   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
 //   8192 x 256 -> 512          17.4 |  17.8 |   8.9 |   6.7 |   5.9 | 10.1      4000 x 256 -> 4096        56.6 |  59.5 |  26.4 | 18.5 | 16.5 | 13.7
 //   500 rows, 8 experts, 4096 -> 4096   36.3 | 33.5 | 30.3 | 23.2 | 30.2 | 29.6      4000 rows, 64 experts, 2048 -> 1408   62.4 | 61.8 | 38.1 | 34.8 | 43.8 | 39.0
+// and of rows of one to four units 16 | 32 | SHORT + 16 | 32 | the best of MID | 256:
+//   3 x 436 -> 8870             3.2 |   3.5 |   3.0 |   3.1 |   4.3 |   8.9       1 x 1024 -> 4096          3.0 |   3.3 |   3.4 |  3.6 |  4.7 |  9.7
+//   476 x 303 -> 1000           4.6 |   4.3 |   3.4 |   3.9 |   4.4 |  12.7       200 x 512 -> 16384       15.6 |  16.5 |   8.8 |  8.4 |  6.4 | 10.0
+//   500 rows, 64 experts, 512 -> 2048   17.4 | 23.3 | 10.5 | 10.2 | 15.1 | 19.6      8000 rows, 64 experts, 256 -> 1024   43.3 | 43.1 | 13.8 | 12.6 | 16.6 | 19.2
+//   300 gated rows, 60 experts, 1024 -> 1408   23.9 | 33.0 | 21.0 | 22.1 | 26.5 | 46.2      8000 rows, 16 experts, 512 -> 2048   97 | 97 | 37 | 33 | 26.6 | 21.7
 // Ranges of units (the second kernel, its launch and MB of sums: 3.5 us + 0.36 a MB), split over unsplit: 256 x 18944 -> 3584 25.5 | 33.8, 777 x 18944 -> 512 18.9 | 29.4,
 // 100 x 14336 -> 4096 16.3 | 22.7; 64 x 4096 -> 4096, whose estimate is against it, 9.5 | 6.2.
 // The kernel of 16 rows takes eight wavefronts, two units each ahead, where rows have 16 units and more, otherwise four (1 x 18944 -> 3584 10.3 against 12.4, 32 gated
 // rows of 8 experts 4096 -> 14336 83.7 against 88.6; 512 rows of 64 experts, 8 units, 26.4 against 22.2).
-constexpr int MX_MID = 1000;
+constexpr int MX_MID = 1000, MX_SHORT = 2000;
 struct mx4_plan { int kernel, ranges; };
 static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64_t cus, size_t ws_bytes)
 {
@@ -153,6 +158,11 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
     for (const auto& f : few) {
         const double t = tiles(f.rows), shares = (double)frags * t / (double)cus;
         offer({f.rows, 1}, f.launch + fmax(fmax(MB * t / f.rate * (many ? 1.2 : 1.0), f.row * u), fmax((f.start + f.unit * u) * (many ? 1.4 : 1.0) * shares, hbm)));
+    }
+    if (U <= MX_SHORT_UNITS) {
+        const struct { int rows; double launch, start, unit, row; } whole[] = {{16, 2.45, 0.05, 0.42, 0.15}, {32, 2.55, 0.08, 0.70, 0.38}};
+        for (const auto& s : whole)
+            offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.27 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.1 * hbm));
     }
     const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.4, 1.1}, {128, 2.6, 0.70, 2.4, 1.15}};
     for (const auto& m : mid) {
@@ -174,7 +184,7 @@ extern "C" size_t mx4_gemm_workspace_bytes(int64_t R, int64_t E, int64_t O, int6
     if (R < 1 || R > MX_MAX_ROWS || E < 1 || E > MX_MAX_EXPERTS || O < 1 || O >= (1 << 22) || K < 1 || K > MX_MAX_K || (gated != 0 && gated != 1)) return 0;
     const int64_t frags = mx4_frags(O << gated);
     const mx4_plan p = mx4_choose(R, E, mx4_units(K), frags, cu_count(), SIZE_MAX);
-    return p.kernel > MX_MID ? mx4_mid_bytes(R, E, frags, p.kernel - MX_MID, p.ranges) : 0;
+    return p.ranges > 1 ? mx4_mid_bytes(R, E, frags, p.kernel - MX_MID, p.ranges) : 0;
 }
 
 static ss_status mx4_product(bool grouped, const void* codes, const void* scales, const int32_t* offsets, const void* w_vals, const void* w_meta, int64_t R,
@@ -197,6 +207,8 @@ static ss_status mx4_product(bool grouped, const void* codes, const void* scales
     case 16: return c.U >= 16 ? launch_stream<8, 1, 2>(c, hs) : launch_stream<4, 1, 4>(c, hs);
     case 32: return launch_stream<4, 2, 4>(c, hs);
     case 256: return launch_mx4_tile(c, hs);
+    case MX_SHORT + 16:
+    case MX_SHORT + 32: return launch_mx4_short(c, p.kernel - MX_SHORT, hs);
     }
     return launch_mx4_mid(c, p.kernel - MX_MID, p.ranges, workspace, hs);
 }

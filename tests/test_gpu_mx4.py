@@ -229,6 +229,40 @@ def _sampled(rows, cols, codes, scales, w_codes, w_scales, gated, dev=DEV):
     return mo.product(xv, values(w_codes[wi], w_scales[:, wi].contiguous()), gated)
 
 
+SHORT = [(3, 436, 8870, 1), (7, 256, 4100, 1), (64, 512, 8192, 1), (476, 303, 1000, 1), (256, 768, 4096, 1), (100, 1000, 8200, 1), (33, 640, 16384, 1), (500, 512, 2048, 64), (300, 256, 1000, 128),
+         (256, 768, 2048, 32), (1016, 278, 1408, 69), (41, 412, 4224, 126), (300, 1024, 1408, 60), (5000, 250, 1030, 40), (2000, 900, 700, 100),
+         (100, 250, 16384, 1), (3000, 256, 1025, 1), (1500, 512, 360, 1), (300, 768, 1024, 1), (1500, 700, 361, 1), (300, 1024, 1000, 1), (1500, 1000, 360, 1), (1500, 768, 512, 8), (1500, 1024, 511, 8),
+         (1500, 1024, 1024, 64), (3000, 500, 130, 16)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("R,K,O,E", SHORT)
+def test_short_rows(R, K, O, E, gated):
+    """Rows of one to four units, by tiles of 16 and 32 rows whose operands are in registers at once."""
+    g = torch.Generator(device=DEV).manual_seed(R + K)
+    off = groups("skewed", R, E, np.random.default_rng(R)) if E > 1 else np.array([0, R])
+    codes, scales = binding.mx4_quant(torch.randn((R, K), generator=g, device=DEV))
+    rows_e = O << gated
+    wc, ws_ = binding.mx4_quant(0.1 * torch.randn((E * rows_e, K), generator=g, device=DEV))
+    w = binding.mx4_pack(wc, ws_, K, experts=E, gated=gated)
+    whole = torch.full((R + 2, O + 3), 7.0, dtype=torch.bfloat16, device=DEV)
+    Y = whole[1:R + 1, 1:O + 1]
+    if E > 1:
+        binding.mx4_grouped_gemm(codes, scales, torch.from_numpy(off.astype(np.int32)).to(DEV), *w, O, K, gated=gated, out=Y)
+    else:
+        binding.mx4_gemm(codes, scales, *w, O, K, gated=gated, out=Y)
+    assert bool((whole[0] == 7).all()) and bool((whole[R + 1] == 7).all()) and bool((whole[:, :1] == 7).all()) and bool((whole[:, O + 1:] == 7).all())
+    rng = np.random.default_rng(E)
+    cols = torch.from_numpy(np.unique(np.concatenate([rng.integers(0, O, 20), [0, O - 1]]))).to(DEV)
+    for e in range(E):
+        if off[e + 1] > off[e]:
+            rows = torch.from_numpy(np.unique(np.concatenate([rng.integers(off[e], off[e + 1], 8), [off[e], off[e + 1] - 1]]))).to(DEV)
+            part = slice(e * rows_e, (e + 1) * rows_e)
+            ref, tol = _sampled(rows, cols, codes, scales, wc[part], ws_[:, part], gated)
+            check_product(Y[rows][:, cols], ref, tol)
+    assert not bool(Y[off[-1]:].any()) and not bool(Y.isnan().any())
+
+
 # every kernel and several rounds of each: tiles of 256 x 256 (more of them than compute units, an odd last tile, rows of three units and of many), of 128 channels
 # with 32, 64 and 128 rows, ranges of units, few tokens on long rows, rows of one and two units by enough tiles that those of 256 x 256 take them
 FULL = [(4099, 800, 9001, False), (2100, 5120, 4224, False), (1500, 3584, 8200, True), (2304, 768, 16384, False), (777, 5003, 4099, False), (600, 4096, 4096, True),
