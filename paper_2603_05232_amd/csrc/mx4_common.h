@@ -144,6 +144,9 @@ struct mx4_call {
     bool gated;
 };
 
+// a launch counts the threads of a grid's dimension in 32 bits
+inline bool mx4_grid_fits(int64_t workgroups, int64_t threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 // Tiles of 256 channels x 256 rows (mx4_tile.hip).
 ss_status launch_mx4_tile(const mx4_call& c, hipStream_t stream);
 // Tiles of 128 channels x 16 or 32 rows (mx4_short.hip); rows of at most MX_SHORT_UNITS units.

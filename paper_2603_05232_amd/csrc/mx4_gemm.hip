@@ -5,12 +5,14 @@
 
 namespace ss {
 
-// A workgroup of W wavefronts takes FW fragments of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the units of
-// the row; operands go from global memory straight into registers, DEPTH units ahead.
-template <int W, int FW, int TB, int DEPTH, bool GROUPED>
+// Y = X W^T of few token rows.  A workgroup of W wavefronts takes a fragment of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the
+// units of the row; operands go from global memory straight into registers, DEPTH units ahead (a weight is used once: LDS would only
+// add a copy), and the wavefronts' sums meet in LDS.  Bound by the stream of weights; one fragment makes the most workgroups, which is what keeps it going.
+//   1 x 3584 -> 37888: 11.5 us, 72.2 MB fetched at 6.3 TB/s;  16 tokens x 2 experts, gated, 8 experts 4096 -> 14336: 83.8 us, 499.7 MB at 6.0 TB/s
+template <int W, int TB, int DEPTH, bool GROUPED>
 __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
 {
-    constexpr int ACC = FW * TB * 2;                     // blocks of 16 x 16
+    constexpr int ACC = TB * 2;                          // blocks of 16 x 16
     __shared__ __attribute__((aligned(16))) float part[W][ACC][4][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     const int slot = blockIdx.z * gridDim.y + blockIdx.y;
@@ -18,36 +20,27 @@ __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
     if constexpr (GROUPED) t = mx4_find(c.offsets, c.E, c.R, 16 * TB, slot);
     if (t.count <= 0) return;
     const bool none = GROUPED && t.expert == c.E;
-    const int f0 = blockIdx.x * FW;
-    const uint8_t *wv[FW], *wm[FW], *xv[TB], *xm[TB];
-#pragma unroll
-    for (int f = 0; f < FW; ++f) {
-        const int64_t at = ((int64_t)(none ? 0 : t.expert) * c.frags + min(f0 + f, c.frags - 1)) * c.U;
-        wv[f] = c.w_vals + at * MX_FRAGB + lane * 16;
-        wm[f] = c.w_meta + at * MX_FRAGS + lane * 4;
-    }
+    const int f = blockIdx.x;
+    const int64_t at = ((int64_t)(none ? 0 : t.expert) * c.frags + f) * c.U;
+    const uint8_t *const wv = c.w_vals + at * MX_FRAGB + lane * 16, *const wm = c.w_meta + at * MX_FRAGS + lane * 4;
+    const uint8_t *xv[TB], *xm[TB];
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
         const int64_t row = t.first + min(16 * b + n, t.count - 1);
         xv[b] = c.codes + row * c.U * MX_UNITB + q * 32;
         xm[b] = c.scales + row * MX_UNITS + q * 2;
     }
-    struct Unit { v4i w[FW][4], x[TB][2]; int sw[FW], sx[TB]; };
+    struct Unit { v4i w[4], x[TB][2]; int sw, sx[TB]; };
     Unit ring[DEPTH];
-    v4f acc[FW][2][TB];
+    v4f acc[2][TB];
 #pragma unroll
-    for (int f = 0; f < FW; ++f)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int b = 0; b < TB; ++b) acc[f][h][b] = v4f{0, 0, 0, 0};
+        for (int b = 0; b < TB; ++b) acc[h][b] = v4f{0, 0, 0, 0};
     auto load = [&](Unit& r, int u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int f = 0; f < FW; ++f) {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) r.w[f][s] = *reinterpret_cast<const v4i*>(wv[f] + (int64_t)u * MX_FRAGB + s * 1024);
-            r.sw[f] = *reinterpret_cast<const int*>(wm[f] + (int64_t)u * MX_FRAGS);
-        }
+        for (int s = 0; s < 4; ++s) r.w[s] = *reinterpret_cast<const v4i*>(wv + (int64_t)u * MX_FRAGB + s * 1024);
+        r.sw = *reinterpret_cast<const int*>(wm + (int64_t)u * MX_FRAGS);
 #pragma unroll
         for (int b = 0; b < TB; ++b) {
 #pragma unroll
@@ -59,9 +52,7 @@ __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
         unroll<4>([&](auto s) __attribute__((always_inline)) {
             constexpr int T = decltype(s)::value >> 1, H = decltype(s)::value & 1;
 #pragma unroll
-            for (int f = 0; f < FW; ++f)
-#pragma unroll
-                for (int b = 0; b < TB; ++b) acc[f][H][b] = mx4_mma<2 * H + T, T>(r.w[f][2 * T + H], r.x[b][T], acc[f][H][b], r.sw[f], r.sx[b]);
+            for (int b = 0; b < TB; ++b) acc[H][b] = mx4_mma<2 * H + T, T>(r.w[2 * T + H], r.x[b][T], acc[H][b], r.sw, r.sx[b]);
         });
     };
     const int mine = none ? 0 : (c.U - wave + W - 1) / W;       // units wave, wave + W, ...
@@ -75,19 +66,17 @@ __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
             if (i + d + DEPTH < mine) load(ring[d], wave + W * (i + d + DEPTH));
         }
 #pragma unroll
-    for (int f = 0; f < FW; ++f)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int b = 0; b < TB; ++b)
 #pragma unroll
-            for (int b = 0; b < TB; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[wave][(f * TB + b) * 2 + h][i][lane] = acc[f][h][b][i];
+            for (int i = 0; i < 4; ++i) part[wave][b * 2 + h][i][lane] = acc[h][b][i];
     __syncthreads();
     // A thread adds two neighbouring channels of a row, in the order of the wavefronts.
-    for (int i = threadIdx.x; i < FW * TB * 256; i += 64 * W) {
-        const int row = (i >> 4) & 15, pair = i & 15, f = i / (256 * TB), b = (i >> 8) % TB, ch = (f0 + f) * MX_FRAG + 2 * pair;
+    for (int i = threadIdx.x; i < TB * 256; i += 64 * W) {
+        const int row = (i >> 4) & 15, pair = i & 15, b = i >> 8, ch = f * MX_FRAG + 2 * pair;
         if (16 * b + row >= t.count) continue;
-        const int a = (f * TB + b) * 2 + ((pair >> 1) & 1), e = 2 * (pair & 1), l = 16 * (pair >> 2) + row;
+        const int a = b * 2 + ((pair >> 1) & 1), e = 2 * (pair & 1), l = 16 * (pair >> 2) + row;
         float v[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -111,8 +100,8 @@ template <int W, int TB, int DEPTH> static ss_status launch_stream(const mx4_cal
     const int64_t tiles = c.offsets ? mx4_max_tiles(c.R, c.E, 16 * TB) : ((int64_t)c.R + 16 * TB - 1) / (16 * TB);
     const int64_t layers = (tiles + 65534) / 65535;      // of the grid's third dimension
     const dim3 grid((uint32_t)c.frags, (uint32_t)((tiles + layers - 1) / layers), (uint32_t)layers);
-    if (c.offsets) hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, true>), grid, dim3(64 * W), 0, stream, c);
-    else hipLaunchKernelGGL((k_mx4_stream<W, 1, TB, DEPTH, false>), grid, dim3(64 * W), 0, stream, c);
+    if (c.offsets) hipLaunchKernelGGL((k_mx4_stream<W, TB, DEPTH, true>), grid, dim3(64 * W), 0, stream, c);
+    else hipLaunchKernelGGL((k_mx4_stream<W, TB, DEPTH, false>), grid, dim3(64 * W), 0, stream, c);
     return launch_status();
 }
 
@@ -126,7 +115,7 @@ using namespace ss;
 // rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The tiles of 256 rows go in rounds of one for each compute unit; the last
 // round, where most stand still, is shorter, the less of them it has.  The group sizes lie on the device: E experts are taken to have R / E rows
 // each, and half a tile more.  Constants fitted to the times of all on 104 shapes (R = 1 .. 54000, 1 .. 74 units, 360 .. 37888 channels, 1 to 128
-// experts): the choice is 1.03 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+// experts): the choice is 1.03 of the fastest on average, 1.2 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
 //   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       46.2 |  36.7 |  25.5 | 18.3 | 16.6 | 26.4
 //   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
 //   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
@@ -148,6 +137,7 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
     const bool many = E > 1;
     const double used = many ? (double)E * (1.0 - pow(1.0 - 1.0 / (double)E, (double)R)) : 1.0, MB = (double)(frags * U * (MX_FRAGB + MX_FRAGS)) / 1e6;
     const double hbm = used * MB / 5.2, panels = (double)((frags + 3) / 4), wide = (double)((frags + 7) / 8), u = (double)U;
+    auto fits = [&](int64_t T, int64_t threads) { return mx4_grid_fits((frags + 3) / 4 * mx4_max_tiles(R, E, T), threads); };
     auto tiles = [&](int64_t T) { return many ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
     mx4_plan best = {};
     double time = INFINITY;
@@ -162,11 +152,12 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
     if (U <= MX_SHORT_UNITS) {
         const struct { int rows; double launch, start, unit, row; } whole[] = {{16, 2.45, 0.05, 0.42, 0.15}, {32, 2.55, 0.08, 0.70, 0.38}};
         for (const auto& s : whole)
-            offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.27 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.1 * hbm));
+            if (fits(s.rows, 256)) offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.27 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.1 * hbm));
     }
     const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.4, 1.1}, {128, 2.6, 0.70, 2.4, 1.15}};
     for (const auto& m : mid) {
         const double w = panels * tiles(m.rows);
+        if (!fits(m.rows, 512)) continue;
         for (int r = 1; r <= 16 && r <= U; ++r) {
             if (r > 1 && (mx4_mid_bytes(R, E, frags, m.rows, r) > ws_bytes || w * r > 2.0 * (double)cus)) break;
             const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0, shares = fmax(1.0, w * r / (double)cus);

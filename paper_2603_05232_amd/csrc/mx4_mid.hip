@@ -6,6 +6,11 @@
 // once a unit, when each of them holds its operands: the unit's slot is then free for unit u + D, and unit u + 1 has landed, whose
 // operands are read while unit u multiplies.
 //
+// Y = X W^T between a stream of weights and large tiles.  Bound by the direct loads, of which a compute unit gets 38 to 60 bytes a clock: a unit of a 128 x 128
+// tile is 34 KB of them beside 512 cycles of products, and wider tiles would leave compute units without one.  777 x 5003 -> 4099, one tile of 128 rows for a
+// compute unit: 19.8 us, 1.61 PFLOP/s; 2000 rows of 64 experts, 2048 -> 1408, tiles of 32 and 64 rows: 30.8 us, 102.8 MB fetched at 3.3 TB/s, the rest
+// of the time start and end of the tiles.
+//
 // With few tiles and long rows the units of a row are split into ranges, a workgroup each; their sums go through the workspace and a second kernel
 // adds them in the order of the ranges.
 #include "mx4_common.h"
@@ -243,7 +248,7 @@ template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED> static ss
 {
     typedef MidShape<FW, TW, WO, WT, KG, D> S;
     const int64_t panels = (c.frags + 3) / 4, tiles = GROUPED ? mx4_max_tiles(c.R, c.E, S::ROWS) : ((int64_t)c.R + S::ROWS - 1) / S::ROWS, items = panels * tiles;
-    if (items * ranges > INT32_MAX) return SS_ERR_SHAPE;
+    if (!mx4_grid_fits(items * ranges, 512)) return SS_ERR_SHAPE;
     if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>>(S::LDS) != SS_OK) return SS_ERR_HIP;
     const Div by = make_div(GROUPED ? panels : tiles);
     hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>), dim3((uint32_t)(items * ranges)), dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, by, make_div(items),

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void k_mx4_short(mx4_call c, int panels, int t
 template <int NU, int TB> static ss_status launch(const mx4_call& c, hipStream_t stream)
 {
     const int64_t panels = (c.frags + 3) / 4, tiles = c.offsets ? mx4_max_tiles(c.R, c.E, 16 * TB) : ((int64_t)c.R + 16 * TB - 1) / (16 * TB);
-    if (panels * tiles > INT32_MAX) return SS_ERR_SHAPE;
+    if (!mx4_grid_fits(panels * tiles, 256)) return SS_ERR_SHAPE;
     const Div by = make_div(c.offsets ? panels : tiles);
     const dim3 grid((uint32_t)(panels * tiles));
     if (c.offsets) hipLaunchKernelGGL((k_mx4_short<NU, TB, true>), grid, dim3(256), 0, stream, c, (int)panels, (int)tiles, by);

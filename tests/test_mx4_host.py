@@ -54,6 +54,14 @@ def test_refusals(lib):
     assert c(4, 2, None, 0, None, 64) == 1 and c(4, 2, None, 0, ODD, 64) == 3
 
 
+def test_more_threads_than_a_grid_counts(lib):
+    n = 1 << 24
+    assert lib.mx4_quant(ONE, 0, n, n, n, None, n, ONE, ONE, None) == 3 and lib.mx4_quant(ONE, 1, n, 1 << 13, n, None, n, ONE, ONE, None) == 3
+    assert lib.mx4_dequant(ONE, ONE, n, 1 << 13, 1, ONE, n, None) == 3
+    assert lib.mx4_pack(ONE, ONE, 1024, 1 << 18, n, 0, ONE, ONE, None) == 3
+    assert lib.expert_combine(ONE, 8, 1 << 12, 1 << 12, ONE, ONE, n, 2, None, 0, ONE, 1 << 12, None) == 3
+
+
 def test_oracle_against_closed_forms():
     v = np.array([[0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.9, -0.2, -0.26, 4.0, 0.0]])
     code, b = mo.quant(v)
