@@ -24,18 +24,11 @@ template <int FW, int TW, int WO, int WT, int KG, int D> struct MidShape {
     static constexpr int ROWS = 16 * TW * WT, A = 4 * MX_FRAGB, B = ROWS * MX_UNITB, MA = 4 * MX_FRAGS, MB = ROWS * MX_UNITS;
     static constexpr int B_OFF = A, MA_OFF = A + B, MB_OFF = MA_OFF + MA, UNIT = MB_OFF + MB, LDS = D * UNIT;
     static constexpr int NB = ROWS >= 64 ? ROWS / 64 : 1;         // loads of token rows of a wavefront for a unit
-    static constexpr int LOADS = 2 + NB;                          // all its loads, without those of the scales, which some have
+    static constexpr int LOADS = 3 + NB;                          // all its loads: half a fragment, rows, scales
     static constexpr int SUMS = 4 * FW * TW * 1024;               // bytes of the sums that a group hands over
     static constexpr int BLOCKS = TW / KG, NV = 2 * FW * BLOCKS;  // blocks of rows that a wavefront finishes, vectors of four sums of them
     static_assert(FW * WO == 4 && WO * WT * KG == 8 && (KG == 1 || (KG == 2 && TW % 2 == 0 && SUMS * 2 <= LDS)) && LDS <= 160 * 1024, "whole shares");
 };
-
-// Waits until the wavefront has at most A (with = 1) or B loads in flight.
-template <int A, int B> __device__ inline void mid_wait(int with)
-{
-    with = __builtin_amdgcn_readfirstlane(with);
-    asm volatile("s_cmp_eq_u32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%1)\n\ts_branch 2f\n1:\n\ts_waitcnt vmcnt(%2)\n2:" ::"s"(with), "n"(A), "n"(B) : "memory", "scc");
-}
 
 template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
 __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int tiles, Div by, Div by_items, KRanges ranges, int S_ranges, v4f* __restrict__ ws)
@@ -54,51 +47,45 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     if (t.count <= 0) return;
     const bool none = GROUPED && t.expert == c.E;
 
-    // Sources of a unit: half of fragment wave / 2, token rows 8 (8 i + wave) .. + 7 (32 rows: of wavefronts 0 .. 3), and by some wavefronts
-    // scales: all weights' by wavefront 0, 32 rows' by wavefronts 4 .. 7.
-    const int64_t first_frag = (int64_t)(none ? 0 : t.expert) * c.frags;
-    const uint8_t* av = c.w_vals + (first_frag + min(panel * 4 + wave / 2, c.frags - 1)) * U * MX_FRAGB + (wave & 1) * 2048;
-    const uint8_t* am = c.w_meta + (first_frag + panel * 4) * U * MX_FRAGS;
-    const uint8_t *bv = c.codes + (int64_t)t.first * U * MX_UNITB, *bm = c.scales + (int64_t)t.first * MX_UNITS;
-    const int64_t begin = range_first(ranges, range);
-    av += begin * MX_FRAGB;
-    am += begin * MX_FRAGS;
-    bv += begin * MX_UNITB;
-    bm += begin * c.R * MX_UNITS;
+    // Sources of a unit: half of fragment wave / 2, token rows 8 (8 i + wave) .. + 7 (32 rows: of wavefronts 0 .. 3), and scales: fragment `wave`'s of wavefronts
+    // 0 .. 3, those of 32 rows of the others, as far as there are rows in the tile's shape.
+    const int64_t first_frag = (int64_t)(none ? 0 : t.expert) * c.frags + panel * 4, begin = range_first(ranges, range);
+    const int frags_here = c.frags - panel * 4;
+    const bool weights = wave < 4;
+    const uint8_t* av = c.w_vals + ((first_frag + min(wave / 2, frags_here - 1)) * U + begin) * MX_FRAGB + (wave & 1) * 2048;
+    const uint8_t* bv = c.codes + ((int64_t)t.first * U + begin) * MX_UNITB;
+    const uint8_t* mv = weights ? c.w_meta + ((first_frag + min(wave, frags_here - 1)) * U + begin) * MX_FRAGS : c.scales + (begin * c.R + t.first) * MX_UNITS;
+    const int64_t m_next = weights ? MX_FRAGS : (int64_t)c.R * MX_UNITS;
     uint32_t boff[S::NB];
 #pragma unroll
     for (int i = 0; i < S::NB; ++i) {
         const int row = 8 * (8 * i + wave) + (lane >> 3);
         boff[i] = (uint32_t)min(row, t.count - 1) * (uint32_t)(U * MX_UNITB) + mx4_place((lane & 7) ^ swz(row)) * 16;
     }
-    const uint32_t moff = wave == 0 ? (uint32_t)min(lane >> 4, c.frags - 1 - panel * 4) * (uint32_t)(U * MX_FRAGS) + (lane & 15) * 16
-                                    : (uint32_t)min((wave & 3) * 32 + (lane >> 1), t.count - 1) * MX_UNITS + (lane & 1) * 4;
-    const int with = __builtin_amdgcn_readfirstlane(wave == 0 || (wave >= 4 && (wave & 3) * 32 < S::ROWS) ? 1 : 0);
-    const uint32_t lane16 = lane * 16, rows_here = S::ROWS >= 64 || wave < 4 ? ~0u : 0u;
-    const int64_t bm_next = (int64_t)c.R * MX_UNITS;
-    const uint32_t a_dst = lds0 + wave * 2048, b_dst = lds0 + S::B_OFF + wave * 1024, ma_dst = lds0 + S::MA_OFF, mb_dst = lds0 + S::MB_OFF + (wave & 3) * 256;
-    // Load number `piece` of the next unit, into `slot_off`; without `more` by no lane, so that every unit counts the same.
-    auto load = [&](auto piece_c, uint32_t slot_off, bool more) __attribute__((always_inline)) {
+    const uint32_t moff = weights ? (uint32_t)lane * 4 : (uint32_t)min((wave & 3) * 32 + (lane >> 1), t.count - 1) * MX_UNITS + (lane & 1) * 4;
+    const uint32_t lane16 = lane * 16;
+    const int low = wave - 4, b_mask = S::ROWS >= 64 ? -1 : low, m_mask = low | ((wave & 3) * 32 - S::ROWS);      // negative where there is something to load
+    const uint32_t a_dst = lds0 + wave * 2048, b_dst = lds0 + S::B_OFF + wave * 1024, m_dst = lds0 + (weights ? S::MA_OFF : S::MB_OFF) + (wave & 3) * 256;
+    // Load number `piece` of the next unit, into `slot_off`; without `more` by no lane, so that every wavefront and unit counts the same.  No branch: products
+    // that stand before one would be moved behind it, and nothing would run beside the reads any more (777 x 20012 -> 4099: 55 us).
+    auto load = [&](auto piece_c, uint32_t slot_off, int more) __attribute__((always_inline)) {
         constexpr int P = decltype(piece_c)::value;
-        const uint32_t all = __builtin_amdgcn_readfirstlane(more ? ~0u : 0u), some = __builtin_amdgcn_readfirstlane(all & rows_here);
-        if constexpr (P < 2) mx4_load16(av + P * 1024, lane16, a_dst + slot_off + P * 1024, all);
-        else if constexpr (P < S::LOADS) mx4_load16(bv, boff[P - 2], b_dst + slot_off + (P - 2) * 8192, some);
+        if constexpr (P < 2) mx4_load16(av + P * 1024, lane16, a_dst + slot_off + P * 1024, more);
+        else if constexpr (P < S::LOADS - 1) mx4_load16(bv, boff[P - 2], b_dst + slot_off + (P - 2) * 8192, more & b_mask);
         else {
-            if (wave == 0) mx4_load16(am, moff, ma_dst + slot_off, all);
-            else if (with) mx4_load4(bm, moff, mb_dst + slot_off, all, all);
+            mx4_load4(mv, moff, m_dst + slot_off, more & m_mask);
             av += MX_FRAGB;
-            am += MX_FRAGS;
             bv += MX_UNITB;
-            bm += bm_next;
+            mv += m_next;
         }
     };
     // this wavefront's operands: step `group` of its fragments and rows
     const uint32_t ra = wo * FW * MX_FRAGB + group * 2048 + lane * 16, rma = S::MA_OFF + wo * FW * MX_FRAGS + lane * 4;
     const uint32_t rb = S::B_OFF + (wt * TW * 16 + n) * ROWB + ((mx4_place(2 * q + group) ^ swz(n)) << 4), rmb = S::MB_OFF + (wt * TW * 16 + n) * MX_UNITS + 2 * q + group;
 
-    const int units = none ? 0 : range_units(ranges, range);
+    const int units = __builtin_amdgcn_readfirstlane(none ? 0 : range_units(ranges, range));
 #pragma unroll
-    for (int d = 0; d < D; ++d) unroll<S::LOADS + 1>([&](auto p) __attribute__((always_inline)) { load(p, d * S::UNIT, d < units); });
+    for (int d = 0; d < D; ++d) unroll<S::LOADS>([&](auto p) __attribute__((always_inline)) { load(p, d * S::UNIT, d - units); });
     v4f acc[FW][2][TW];
 #pragma unroll
     for (int f = 0; f < FW; ++f)
@@ -122,10 +109,11 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
     // One by one between the products: a wavefront issues in order, and a read or a load that has to wait for room in its queue keeps the
     // products behind it from issuing.
     auto unit = [&](Operands& now, Operands& next, int u) __attribute__((always_inline)) {
-        mid_wait<(D - 2) * (S::LOADS + 1), (D - 2) * S::LOADS>(with);      // unit u + 1 has landed, and this one's operands have arrived
+        wait_vmcnt<(D - 2) * S::LOADS>();                  // unit u + 1 has landed, and this one's operands have arrived
         wait_lgkm0();
         wg_barrier();
         const uint32_t freed = here;
+        const int more = u + D - units;                    // a unit to load: negative
         here = here + S::UNIT == D * S::UNIT ? 0 : here + S::UNIT;       // behind the last unit what an older one left is read, for nothing
 #pragma unroll
         for (int f = 0; f < FW; ++f)
@@ -133,15 +121,15 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
         __builtin_amdgcn_sched_barrier(0);
         unroll<N>([&](auto i_c) __attribute__((always_inline)) {
             constexpr int i = decltype(i_c)::value, T = i / SN, j = i % SN, b = j / (2 * FW), f = (j >> 1) % FW, h = j & 1;
-            constexpr int r0 = i * READS / N, r1 = (i + 1) * READS / N, l0 = i * (S::LOADS + 1) / N, l1 = (i + 1) * (S::LOADS + 1) / N;
+            constexpr int r0 = i * READS / N, r1 = (i + 1) * READS / N, l0 = i * S::LOADS / N, l1 = (i + 1) * S::LOADS / N;
             acc[f][h][b] = mx4_mma<2 * h + T, T>(now.a[T][f][h], now.b[T][b], acc[f][h][b], now.sa[f], now.sb[b]);
             __builtin_amdgcn_sched_barrier(0);
             unroll<r1 - r0>([&](auto p) __attribute__((always_inline)) { read(std::integral_constant<int, r0 + decltype(p)::value>{}, next, here); });
-            unroll<l1 - l0>([&](auto p) __attribute__((always_inline)) { load(std::integral_constant<int, l0 + decltype(p)::value>{}, freed, u + D < units); });
+            unroll<l1 - l0>([&](auto p) __attribute__((always_inline)) { load(std::integral_constant<int, l0 + decltype(p)::value>{}, freed, more); });
             __builtin_amdgcn_sched_barrier(0);
         });
     };
-    mid_wait<(D - 1) * (S::LOADS + 1), (D - 1) * S::LOADS>(with);
+    wait_vmcnt<(D - 1) * S::LOADS>();
     wg_barrier();
     Operands r0, r1;
     unroll<READS>([&](auto p) __attribute__((always_inline)) { read(p, r0, 0); });

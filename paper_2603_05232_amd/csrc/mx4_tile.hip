@@ -156,12 +156,12 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     const int64_t mb_next = (int64_t)c.R * MX_UNITS;
     const uint32_t lane16 = lane * 16, lane4 = lane * 4;
     const uint32_t a_wave = lds0 + wave * 2048, b_wave = lds0 + XT_B_OFF + wave * 1024, ma_wave = lds0 + XT_MA_OFF + wave * 256, mb_wave = lds0 + XT_MB_OFF + wave * 256;
-    auto load_a = [&](int t, int j, uint32_t slot, uint32_t more) __attribute__((always_inline)) {
+    auto load_a = [&](int t, int j, uint32_t slot, int more) __attribute__((always_inline)) {
         mx4_load16(pa.v + (2 * t + j) * 1024, lane16, a_wave + slot + j * 1024, more);
     };
-    auto load_ma = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pa.m, lane4, ma_wave + slot, more, more); };
-    auto load_b = [&](int i, uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
-    auto load_mb = [&](uint32_t slot, uint32_t more) __attribute__((always_inline)) { mx4_load4(pb.m, bmoff, mb_wave + slot, more, more); };
+    auto load_ma = [&](uint32_t slot, int more) __attribute__((always_inline)) { mx4_load4(pa.m, lane4, ma_wave + slot, more); };
+    auto load_b = [&](int i, uint32_t slot, int more) __attribute__((always_inline)) { mx4_load16(pb.v, boff[i], b_wave + slot + i * 8192, more); };
+    auto load_mb = [&](uint32_t slot, int more) __attribute__((always_inline)) { mx4_load4(pb.m, bmoff, mb_wave + slot, more); };
     const uint8_t* const zeros_at = reinterpret_cast<const uint8_t*>(mx4_zeros);
     auto next_a = [&]() __attribute__((always_inline)) {
         const bool none = SHORT && ++ua >= c.U;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     if (!tile_of(0, now)) return;
     pa = weights_of(now);
     set_rows(now);
-    constexpr uint32_t ALL = ~0u;
+    constexpr int ALL = -1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) load_b(i, b0, ALL);
     load_ma(m0, ALL);
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
     wait_vmcnt<10>();
     wg_barrier();
 
-    uint32_t more_a = ALL, more_b = ALL;                  // none where there is no next tile
+    int more_a = ALL, more_b = ALL;                  // none where there is no next tile
     Weights then = pa;                                    // of the next tile
     int have = 1;
     v4f acc[8][4];
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(512) void k_mx4_tile(mx4_call c, int tiles_o)
         pa.v = wrap ? then.v : pa.v;
         pa.m = wrap ? then.m : pa.m;
         if (SHORT) ua = wrap ? 0 : ua;
-        more_a = wrap ? (uint32_t)-have : more_a;
+        more_a = wrap ? -have : more_a;
         step(std::integral_constant<int, 1>{}, waits);
         next_b();
         waits = 1;
