@@ -114,20 +114,20 @@ using namespace ss;
 // unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
 // rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The tiles of 256 rows go in rounds of one for each compute unit; the last
 // round, where most stand still, is shorter, the less of them it has.  The group sizes lie on the device: E experts are taken to have R / E rows
-// each, and half a tile more.  Constants fitted to the times of all on 104 shapes (R = 1 .. 54000, 1 .. 74 units, 360 .. 37888 channels, 1 to 128
-// experts): the choice is 1.03 of the fastest on average, 1.2 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
-//   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       46.2 |  36.7 |  25.5 | 18.3 | 16.6 | 26.4
-//   32 x 3584 -> 37888         24.2 |  19.0 |  19.8 |  20.5 |   -   |   -       777 x 5003 -> 4099        78.1 |  51.1 |  31.5 | 22.2 | 19.9 | 32.6
-//   64 x 3584 -> 4608           7.2 |   7.9 |   7.9 |   9.2 |  12.3 |   -       3200 x 4096 -> 4096      164.7 | 136.5 |  77.5 | 53.8 | 55.7 | 32.5
-//   8192 x 256 -> 512          17.4 |  17.8 |   8.9 |   6.7 |   5.9 | 10.1      4000 x 256 -> 4096        56.6 |  59.5 |  26.4 | 18.5 | 16.5 | 13.7
-//   500 rows, 8 experts, 4096 -> 4096   36.3 | 33.5 | 30.3 | 23.2 | 30.2 | 29.6      4000 rows, 64 experts, 2048 -> 1408   62.4 | 61.8 | 38.1 | 34.8 | 43.8 | 39.0
+// each, and half a tile more.  Constants fitted to the times of all on 122 shapes (R = 1 .. 54000, 1 .. 79 units, 64 .. 37888 channels, 1 to 128
+// experts): the choice is 1.02 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+//   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       49.3 |  36.8 |  24.3 | 17.8 | 14.9 | 27.3
+//   32 x 3584 -> 37888         24.2 |  19.7 |  20.0 |  19.9 | 26.9 | 25.9       777 x 5003 -> 4099        77.7 |  50.9 |  30.0 | 20.7 | 18.1 | 33.6
+//   64 x 3584 -> 4608           7.2 |   7.9 |   7.3 |   7.8 |   9.6 | 22.0       3200 x 4096 -> 4096        183 |   136 |  76.2 | 51.9 | 51.5 | 33.4
+//   8192 x 256 -> 512          17.9 |  18.2 |   8.2 |   5.8 |   5.8 | 10.1       4000 x 256 -> 4096        56.9 |  59.7 |  23.4 | 15.3 | 15.2 | 13.7
+//   500 rows, 8 experts, 4096 -> 4096   43.8 | 33.6 | 30.4 | 22.5 | 27.4 | 29.7      4000 rows, 64 experts, 2048 -> 1408   61.9 | 62.0 | 36.3 | 32.6 | 39.5 | 39.5
 // and of rows of one to four units 16 | 32 | SHORT + 16 | 32 | the best of MID | 256:
-//   3 x 436 -> 8870             3.2 |   3.5 |   3.0 |   3.1 |   4.3 |   8.9       1 x 1024 -> 4096          3.0 |   3.3 |   3.4 |  3.6 |  4.7 |  9.7
-//   476 x 303 -> 1000           4.6 |   4.3 |   3.4 |   3.9 |   4.4 |  12.7       200 x 512 -> 16384       15.6 |  16.5 |   8.8 |  8.4 |  6.4 | 10.0
-//   500 rows, 64 experts, 512 -> 2048   17.4 | 23.3 | 10.5 | 10.2 | 15.1 | 19.6      8000 rows, 64 experts, 256 -> 1024   43.3 | 43.1 | 13.8 | 12.6 | 16.6 | 19.2
-//   300 gated rows, 60 experts, 1024 -> 1408   23.9 | 33.0 | 21.0 | 22.1 | 26.5 | 46.2      8000 rows, 16 experts, 512 -> 2048   97 | 97 | 37 | 33 | 26.6 | 21.7
-// Ranges of units (the second kernel, its launch and MB of sums: 3.5 us + 0.36 a MB), split over unsplit: 256 x 18944 -> 3584 25.5 | 33.8, 777 x 18944 -> 512 18.9 | 29.4,
-// 100 x 14336 -> 4096 16.3 | 22.7; 64 x 4096 -> 4096, whose estimate is against it, 9.5 | 6.2.
+//   3 x 436 -> 8870             3.1 |   3.4 |   3.1 |   3.1 |   3.8 |   8.9       1 x 1024 -> 4096          3.0 |   3.2 |   3.5 |  3.6 |  4.3 |  9.7
+//   476 x 303 -> 1000           4.4 |   4.3 |   3.4 |   4.0 |   4.0 |  12.6       200 x 512 -> 16384       15.1 |  16.5 |   8.7 |  8.4 |  5.9 | 10.0
+//   500 rows, 64 experts, 512 -> 2048   17.4 | 23.4 | 10.6 | 10.0 | 13.7 | 21.4      8000 rows, 64 experts, 256 -> 1024   44.9 | 44.1 | 13.9 | 12.6 | 14.1 | 19.1
+//   300 gated rows, 60 experts, 1024 -> 1408   24.0 | 33.2 | 21.2 | 21.9 | 23.8 | 52.4      8000 rows, 16 experts, 512 -> 2048   85 | 82 | 33 | 28 | 24.6 | 21.8
+// Ranges of units (the second kernel, its launch and MB of sums: 3.5 us + 0.36 a MB), split over unsplit: 256 x 18944 -> 3584 23.5 | 33.8, 777 x 18944 -> 512 17.8 | 28.0,
+// 100 x 14336 -> 4096 15.4 | 22.3; 64 x 4096 -> 4096, whose estimate is against it, 8.7 | 6.1.
 // The kernel of 16 rows takes eight wavefronts, two units each ahead, where rows have 16 units and more, otherwise four (1 x 18944 -> 3584 10.3 against 12.4, 32 gated
 // rows of 8 experts 4096 -> 14336 83.7 against 88.6; 512 rows of 64 experts, 8 units, 26.4 against 22.2).
 constexpr int MX_MID = 1000, MX_SHORT = 2000;
@@ -144,29 +144,29 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
     auto offer = [&](mx4_plan p, double us) {
         if (us < time) { best = p; time = us; }
     };
-    const struct { int rows; double launch, rate, row, start, unit; } few[] = {{16, 2.2, 8.5, 0.14, 0.40, 0.045}, {32, 2.5, 6.0, 0.18, 0.82, 0.08}};
+    const struct { int rows; double launch, rate, row, start, unit; } few[] = {{16, 2.52, 8.5, 0.0, 0.39, 0.056}, {32, 2.67, 5.85, 0.18, 0.73, 0.086}};
     for (const auto& f : few) {
         const double t = tiles(f.rows), shares = (double)frags * t / (double)cus;
-        offer({f.rows, 1}, f.launch + fmax(fmax(MB * t / f.rate * (many ? 1.2 : 1.0), f.row * u), fmax((f.start + f.unit * u) * (many ? 1.4 : 1.0) * shares, hbm)));
+        offer({f.rows, 1}, f.launch + fmax(fmax(MB * t / f.rate * (many ? 0.94 : 1.0), f.row * u), fmax((f.start + f.unit * u) * (many ? 1.6 : 1.0) * shares, hbm)));
     }
     if (U <= MX_SHORT_UNITS) {
-        const struct { int rows; double launch, start, unit, row; } whole[] = {{16, 2.45, 0.05, 0.42, 0.15}, {32, 2.55, 0.08, 0.70, 0.38}};
+        const struct { int rows; double launch, start, unit, row; } whole[] = {{16, 2.6, 0.07, 0.41, 0.27}, {32, 2.65, 0.07, 0.70, 0.40}};
         for (const auto& s : whole)
-            if (fits(s.rows, 256)) offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.27 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.1 * hbm));
+            if (fits(s.rows, 256)) offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.2 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.13 * hbm));
     }
-    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.0, 0.40, 1.2, 1.1}, {64, 2.4, 0.44, 1.4, 1.1}, {128, 2.6, 0.70, 2.4, 1.15}};
+    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.29, 0.39, 0.86, 1.13}, {64, 1.99, 0.42, 1.24, 1.13}, {128, 2.35, 0.56, 2.72, 1.8}};
     for (const auto& m : mid) {
         const double w = panels * tiles(m.rows);
         if (!fits(m.rows, 512)) continue;
         for (int r = 1; r <= 16 && r <= U; ++r) {
             if (r > 1 && (mx4_mid_bytes(R, E, frags, m.rows, r) > ws_bytes || w * r > 2.0 * (double)cus)) break;
             const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0, shares = fmax(1.0, w * r / (double)cus);
-            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * (many ? 1.5 : 1.0) * shares, m.hbm * hbm + 1.0) + add);
+            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * (many ? 1.47 : 1.0) * shares, m.hbm * hbm + 1.0) + add);
         }
     }
     const double all = wide * tiles(256) / (double)cus, part = all - floor(all), full = fmin(1.0, all);
-    const double rounds = all <= 1.0 ? 1.0 : floor(all) + (part > 0.0 ? fmin(1.0, 0.5 + part) : 0.0);
-    offer({256, 1}, 4.8 + fmax(rounds * (fmax(u, 3.0) * (1.15 + 0.45 * full) + (1.5 + 2.3 * full) * (many ? 1.6 : 1.0)), hbm));
+    const double rounds = all <= 1.0 ? 1.0 : floor(all) + (part > 0.0 ? fmin(1.0, 0.33 + part) : 0.0);
+    offer({256, 1}, 3.96 + fmax(rounds * (fmax(u, 3.0) * (1.14 + 0.55 * full) + (1.04 + 3.23 * full) * (many ? 1.71 : 1.0)), hbm));
     return best;
 }
 

@@ -1,15 +1,13 @@
 // Products of microscaled 4-bit operands on tiles of 128 channels x 32, 64 or 128 token rows (mx4_gemm, mx4_grouped_gemm).
 //
-// A workgroup of eight wavefronts takes one tile, in two groups of four that share the tile out alike: group g multiplies step g of every unit, and
-// the groups' sums meet in LDS at the end.  (A group per half of the tile would read the operands of the other half's rows or channels
-// once more: 96 instead of 64 KB of LDS reads a unit.)  Operands go through a ring of D units in LDS, filled by direct loads.  The wavefronts meet
-// once a unit, when each of them holds its operands: the unit's slot is then free for unit u + D, and unit u + 1 has landed, whose
-// operands are read while unit u multiplies.
+// A workgroup of eight wavefronts takes one tile.  Operands go through a ring of D units in LDS, filled by direct loads.  The wavefronts meet once a unit,
+// when each of them holds its operands: the unit's slot is then free for unit u + D, and unit u + 1 has landed, whose operands are read while
+// unit u multiplies.
 //
-// Y = X W^T between a stream of weights and large tiles.  Bound by the direct loads, of which a compute unit gets 38 to 60 bytes a clock: a unit of a 128 x 128
-// tile is 34 KB of them beside 512 cycles of products, and wider tiles would leave compute units without one.  777 x 5003 -> 4099, one tile of 128 rows for a
-// compute unit: 19.8 us, 1.61 PFLOP/s; 2000 rows of 64 experts, 2048 -> 1408, tiles of 32 and 64 rows: 30.8 us, 102.8 MB fetched at 3.3 TB/s, the rest
-// of the time start and end of the tiles.
+// Y = X W^T between a stream of weights and large tiles.  A unit of a 128 x 128 tile is 34 KB of direct loads and 96 KB of reads in LDS beside 512 cycles of
+// products, and takes some 1150: LDS has 130 KB at 128 bytes a cycle to move.  Without the loads it takes 0.8 of that, without the reads 0.75.
+// Wider tiles would leave compute units without one.  777 x 5003 -> 4099, one tile of 128 rows for a compute unit: 17.8 us, 1.79 PFLOP/s, a third of it the start
+// (first loads) and the end; 2000 rows of 64 experts, 2048 -> 1408, tiles of 64 rows: 28.4 us, 98 MB of weights at 3.5 TB/s, the rest start and end.
 //
 // With few tiles and long rows the units of a row are split into ranges, a workgroup each; their sums go through the workspace and a second kernel
 // adds them in the order of the ranges.
@@ -19,25 +17,23 @@
 
 namespace ss {
 
-// a group is WO x WT wavefronts of FW fragments of 32 channels x TW blocks of 16 rows
-template <int FW, int TW, int WO, int WT, int KG, int D> struct MidShape {
+// WO x WT wavefronts of FW fragments of 32 channels x TW blocks of 16 rows
+template <int FW, int TW, int WO, int WT, int D> struct MidShape {
     static constexpr int ROWS = 16 * TW * WT, A = 4 * MX_FRAGB, B = ROWS * MX_UNITB, MA = 4 * MX_FRAGS, MB = ROWS * MX_UNITS;
     static constexpr int B_OFF = A, MA_OFF = A + B, MB_OFF = MA_OFF + MA, UNIT = MB_OFF + MB, LDS = D * UNIT;
     static constexpr int NB = ROWS >= 64 ? ROWS / 64 : 1;         // loads of token rows of a wavefront for a unit
     static constexpr int LOADS = 3 + NB;                          // all its loads: half a fragment, rows, scales
-    static constexpr int SUMS = 4 * FW * TW * 1024;               // bytes of the sums that a group hands over
-    static constexpr int BLOCKS = TW / KG, NV = 2 * FW * BLOCKS;  // blocks of rows that a wavefront finishes, vectors of four sums of them
-    static_assert(FW * WO == 4 && WO * WT * KG == 8 && (KG == 1 || (KG == 2 && TW % 2 == 0 && SUMS * 2 <= LDS)) && LDS <= 160 * 1024, "whole shares");
+    static constexpr int NV = 2 * FW * TW;                        // a wavefront's vectors of four sums
+    static_assert(FW * WO == 4 && WO * WT == 8 && LDS <= 160 * 1024, "whole shares");
 };
 
-template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
+template <int FW, int TW, int WO, int WT, int D, bool GROUPED>
 __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int tiles, Div by, Div by_items, KRanges ranges, int S_ranges, v4f* __restrict__ ws)
 {
-    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    typedef MidShape<FW, TW, WO, WT, D> S;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    constexpr int TS = 2 / KG;                           // steps of a unit that a wavefront multiplies
-    const int group = KG == 2 ? wave >> 2 : 0, wo = wave % WO, wt = wave / WO % WT, U = c.U;
+    const int wo = wave % WO, wt = wave / WO, U = c.U;
     const uint32_t lds0 = lds_address(smem);
     // Neighbouring workgroups of an XCD share a panel's weights (dense) or a tile's rows (grouped).
     const int id = xcd_run(blockIdx.x, panels * tiles * S_ranges), range = quot(id, by_items), item = id - range * panels * tiles, at = quot(item, by);
@@ -79,9 +75,9 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
             mv += m_next;
         }
     };
-    // this wavefront's operands: step `group` of its fragments and rows
-    const uint32_t ra = wo * FW * MX_FRAGB + group * 2048 + lane * 16, rma = S::MA_OFF + wo * FW * MX_FRAGS + lane * 4;
-    const uint32_t rb = S::B_OFF + (wt * TW * 16 + n) * ROWB + ((mx4_place(2 * q + group) ^ swz(n)) << 4), rmb = S::MB_OFF + (wt * TW * 16 + n) * MX_UNITS + 2 * q + group;
+    // this wavefront's operands
+    const uint32_t ra = wo * FW * MX_FRAGB + lane * 16, rma = S::MA_OFF + wo * FW * MX_FRAGS + lane * 4;
+    const uint32_t rb = S::B_OFF + (wt * TW * 16 + n) * ROWB + ((mx4_place(2 * q) ^ swz(n)) << 4), rmb = S::MB_OFF + (wt * TW * 16 + n) * MX_UNITS + 2 * q;
 
     const int units = __builtin_amdgcn_readfirstlane(none ? 0 : range_units(ranges, range));
 #pragma unroll
@@ -93,15 +89,13 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int b = 0; b < TW; ++b) acc[f][h][b] = v4f{0, 0, 0, 0};
-    struct Operands { v4i a[TS][FW][2], b[TS][TW]; int sa[FW], sb[TW]; };
+    struct Operands { v4i a[2][FW][2], b[2][TW]; int sa[FW], sb[TW]; };
     // operand read number `piece` of READS: a step's rows and weights, the next step's, the scales
-    constexpr int SR = 2 * FW + TW, READS = TS * SR + FW + TW, SN = FW * TW * 2, N = TS * SN;
+    constexpr int SR = 2 * FW + TW, READS = 2 * SR + FW + TW, SN = FW * TW * 2, N = 2 * SN;
     auto read = [&](auto piece_c, Operands& r, uint32_t slot_off) __attribute__((always_inline)) {
-        constexpr int P = decltype(piece_c)::value, T = P / SR, Q = P % SR, Z = P - TS * SR;
-        if constexpr (Z >= FW) {
-            const uint8_t* const at = smem + rmb + slot_off + (Z - FW) * 128;
-            r.sb[Z - FW] = KG == 2 ? *at : *reinterpret_cast<const uint16_t*>(at);
-        } else if constexpr (Z >= 0) r.sa[Z] = *reinterpret_cast<const int*>(smem + rma + slot_off + Z * MX_FRAGS);
+        constexpr int P = decltype(piece_c)::value, T = P / SR, Q = P % SR, Z = P - 2 * SR;
+        if constexpr (Z >= FW) r.sb[Z - FW] = *reinterpret_cast<const uint16_t*>(smem + rmb + slot_off + (Z - FW) * 128);
+        else if constexpr (Z >= 0) r.sa[Z] = *reinterpret_cast<const int*>(smem + rma + slot_off + Z * MX_FRAGS);
         else if constexpr (Q < TW) r.b[T][Q] = *reinterpret_cast<const v4i*>(smem + ((rb + slot_off) ^ (T * 32)) + Q * 2048);
         else r.a[T][(Q - TW) >> 1][(Q - TW) & 1] = *reinterpret_cast<const v4i*>(smem + ra + slot_off + T * 2048 + ((Q - TW) >> 1) * MX_FRAGB + ((Q - TW) & 1) * 1024);
     };
@@ -115,9 +109,6 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
         const uint32_t freed = here;
         const int more = u + D - units;                    // a unit to load: negative
         here = here + S::UNIT == D * S::UNIT ? 0 : here + S::UNIT;       // behind the last unit what an older one left is read, for nothing
-#pragma unroll
-        for (int f = 0; f < FW; ++f)
-            if constexpr (KG == 2) now.sa[f] = (uint32_t)now.sa[f] >> (8 * group);
         __builtin_amdgcn_sched_barrier(0);
         unroll<N>([&](auto i_c) __attribute__((always_inline)) {
             constexpr int i = decltype(i_c)::value, T = i / SN, j = i % SN, b = j / (2 * FW), f = (j >> 1) % FW, h = j & 1;
@@ -139,74 +130,33 @@ __global__ __launch_bounds__(512) void k_mx4_mid(mx4_call c, int panels, int til
         unit(r1, r0, u + 1);
     }
     if (u < units) unit(r0, r1, u);
-    v4f* const partial = ws + ((((int64_t)range * panels * tiles + item) * 8 + wave) * S::NV) * 64 + lane;
-    if constexpr (KG == 1) {
-        if (S_ranges > 1) {
+    if (S_ranges > 1) {
+        v4f* const partial = ws + ((((int64_t)range * panels * tiles + item) * 8 + wave) * S::NV) * 64 + lane;
 #pragma unroll
-            for (int b = 0; b < TW; ++b)
-#pragma unroll
-                for (int f = 0; f < FW; ++f)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) partial[((b * FW + f) * 2 + h) * 64] = acc[f][h][b];
-            return;
-        }
-#pragma unroll
-        for (int b = 0; b < TW; ++b) {
-            const int row = 16 * (wt * TW + b) + n;
-            if (row >= t.count) continue;
-            uint16_t* const y = c.Y + (int64_t)(t.first + row) * c.ldy;
-#pragma unroll
-            for (int f = 0; f < FW; ++f) mx4_store8(acc[f][0][b], acc[f][1][b], y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
-        }
-    } else {
-    // The groups' sums: each hands half of its blocks of rows to the other and finishes the rest.
-    wait_lgkm0();
-    wg_barrier();
-    v4f* const mine = reinterpret_cast<v4f*>(smem + group * S::SUMS) + (wave & 3) * (FW * TW * 64) + lane;
-    const v4f* const theirs = reinterpret_cast<const v4f*>(smem + (1 - group) * S::SUMS) + (wave & 3) * (FW * TW * 64) + lane;
-    auto give = [&](auto other) __attribute__((always_inline)) {
-        constexpr int B0 = decltype(other)::value * (TW / 2);
-#pragma unroll
-        for (int b = 0; b < TW / 2; ++b)
+        for (int b = 0; b < TW; ++b)
 #pragma unroll
             for (int f = 0; f < FW; ++f)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) mine[((b * FW + f) * 2 + h) * 64] = acc[f][h][B0 + b];
-    };
-    auto finish = [&](auto own) __attribute__((always_inline)) {
-        constexpr int G = decltype(own)::value, B0 = G * (TW / 2);
-        // lane (n, q): channels 8 q .. + 7 of each fragment, row n of each block; group 0's sums first
+                for (int h = 0; h < 2; ++h) partial[((b * FW + f) * 2 + h) * 64] = acc[f][h][b];
+        return;
+    }
 #pragma unroll
-        for (int b = 0; b < TW / 2; ++b) {
-            const int row = 16 * (wt * TW + B0 + b) + n;
-            uint16_t* const y = c.Y + (int64_t)(t.first + min(row, t.count - 1)) * c.ldy;
+    for (int b = 0; b < TW; ++b) {
+        const int row = 16 * (wt * TW + b) + n;
+        if (row >= t.count) continue;
+        uint16_t* const y = c.Y + (int64_t)(t.first + row) * c.ldy;
 #pragma unroll
-            for (int f = 0; f < FW; ++f) {
-                const v4f v = theirs[((b * FW + f) * 2) * 64], w = theirs[((b * FW + f) * 2 + 1) * 64];
-                const v4f x = acc[f][0][B0 + b], z = acc[f][1][B0 + b];
-                if (S_ranges > 1) {
-                    partial[((b * FW + f) * 2) * 64] = G == 0 ? x + v : v + x;
-                    partial[((b * FW + f) * 2 + 1) * 64] = G == 0 ? z + w : w + z;
-                } else if (row < t.count) mx4_store8(G == 0 ? x + v : v + x, G == 0 ? z + w : w + z, y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
-            }
-        }
-    };
-    if (group == 0) give(std::integral_constant<int, 1>{});
-    else give(std::integral_constant<int, 0>{});
-    wait_lgkm0();
-    wg_barrier();
-    if (group == 0) finish(std::integral_constant<int, 0>{});
-    else finish(std::integral_constant<int, 1>{});
+        for (int f = 0; f < FW; ++f) mx4_store8(acc[f][0][b], acc[f][1][b], y, (panel * 4 + wo * FW + f) * MX_FRAG + 8 * q, c.O, c.gated);
     }
 }
 
 // adds the sums of the ranges, a thread what one lane of the workgroups before had
-template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED>
+template <int FW, int TW, int WO, int WT, int D, bool GROUPED>
 __global__ __launch_bounds__(512) void k_mx4_mid_add(mx4_call c, int panels, int tiles, Div by, int S_ranges, const v4f* __restrict__ ws)
 {
-    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    typedef MidShape<FW, TW, WO, WT, D> S;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    const int group = KG == 2 ? wave >> 2 : 0, wo = wave % WO, wt = wave / WO % WT;
+    const int wo = wave % WO, wt = wave / WO;
     const int item = blockIdx.x, at = quot(item, by);
     const int panel = GROUPED ? item - at * panels : at, slot = GROUPED ? at : item - at * tiles;
     mx4_rows t = {0, slot * S::ROWS, min(S::ROWS, c.R - slot * S::ROWS)};
@@ -223,8 +173,8 @@ __global__ __launch_bounds__(512) void k_mx4_mid_add(mx4_call c, int panels, int
         for (int i = 0; i < S::NV; ++i) sum[i] += from[i * 64];
     }
 #pragma unroll
-    for (int b = 0; b < S::BLOCKS; ++b) {
-        const int row = 16 * (wt * TW + group * S::BLOCKS + b) + n;
+    for (int b = 0; b < TW; ++b) {
+        const int row = 16 * (wt * TW + b) + n;
         if (row >= t.count) continue;
         uint16_t* const y = c.Y + (int64_t)(t.first + row) * c.ldy;
 #pragma unroll
@@ -232,28 +182,32 @@ __global__ __launch_bounds__(512) void k_mx4_mid_add(mx4_call c, int panels, int
     }
 }
 
-template <int FW, int TW, int WO, int WT, int KG, int D, bool GROUPED> static ss_status launch_kind(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
+template <int FW, int TW, int WO, int WT, int D, bool GROUPED> static ss_status launch_kind(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
 {
-    typedef MidShape<FW, TW, WO, WT, KG, D> S;
+    typedef MidShape<FW, TW, WO, WT, D> S;
     const int64_t panels = (c.frags + 3) / 4, tiles = GROUPED ? mx4_max_tiles(c.R, c.E, S::ROWS) : ((int64_t)c.R + S::ROWS - 1) / S::ROWS, items = panels * tiles;
     if (!mx4_grid_fits(items * ranges, 512)) return SS_ERR_SHAPE;
-    if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>>(S::LDS) != SS_OK) return SS_ERR_HIP;
+    if (allow_dynamic_lds<k_mx4_mid<FW, TW, WO, WT, D, GROUPED>>(S::LDS) != SS_OK) return SS_ERR_HIP;
     const Div by = make_div(GROUPED ? panels : tiles);
-    hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, KG, D, GROUPED>), dim3((uint32_t)(items * ranges)), dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, by, make_div(items),
+    hipLaunchKernelGGL((k_mx4_mid<FW, TW, WO, WT, D, GROUPED>), dim3((uint32_t)(items * ranges)), dim3(512), S::LDS, stream, c, (int)panels, (int)tiles, by, make_div(items),
                        k_ranges(c.U, ranges), ranges, static_cast<v4f*>(ws));
     if (launch_status() != SS_OK) return SS_ERR_HIP;
     if (ranges == 1) return SS_OK;
-    hipLaunchKernelGGL((k_mx4_mid_add<FW, TW, WO, WT, KG, D, GROUPED>), dim3((uint32_t)items), dim3(512), 0, stream, c, (int)panels, (int)tiles, by, ranges, static_cast<const v4f*>(ws));
+    hipLaunchKernelGGL((k_mx4_mid_add<FW, TW, WO, WT, D, GROUPED>), dim3((uint32_t)items), dim3(512), 0, stream, c, (int)panels, (int)tiles, by, ranges, static_cast<const v4f*>(ws));
     return launch_status();
 }
-template <int FW, int TW, int WO, int WT, int KG, int D> static ss_status launch(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
+template <int FW, int TW, int WO, int WT, int D> static ss_status launch(const mx4_call& c, int ranges, void* ws, hipStream_t stream)
 {
-    return c.offsets ? launch_kind<FW, TW, WO, WT, KG, D, true>(c, ranges, ws, stream) : launch_kind<FW, TW, WO, WT, KG, D, false>(c, ranges, ws, stream);
+    return c.offsets ? launch_kind<FW, TW, WO, WT, D, true>(c, ranges, ws, stream) : launch_kind<FW, TW, WO, WT, D, false>(c, ranges, ws, stream);
 }
 
 ss_status launch_mx4_mid(const mx4_call& c, int rows, int ranges, void* ws, hipStream_t stream)
 {
-    return rows == 32 ? launch<1, 2, 4, 1, 2, 3>(c, ranges, ws, stream) : rows == 64 ? launch<2, 2, 2, 2, 2, 3>(c, ranges, ws, stream) : launch<2, 2, 2, 4, 1, 4>(c, ranges, ws, stream);
+    // The wavefronts' shares by the fewest LDS reads among those that measured alike; 64 rows as <1, 2, 4, 2, 3>: 29.5 against 28.8 us (2000 rows of 64 experts, 2048 ->
+    // 1408); 128 as <1, 4, 4, 2, 4>: 14.4 against 12.7 (200 x 4096 -> 14336).  Two groups that multiply one step of a unit each and join their sums at the
+    // end read a third less and took 30.5 and 13.0.  Four units in flight in place of three: 36.8 where 64 rows take 30.5 (one workgroup a
+    // compute unit instead of two), no difference at 128.
+    return rows == 32 ? launch<1, 1, 4, 2, 3>(c, ranges, ws, stream) : rows == 64 ? launch<2, 1, 2, 4, 3>(c, ranges, ws, stream) : launch<2, 2, 2, 4, 3>(c, ranges, ws, stream);
 }
 
 }  // namespace ss
