@@ -112,9 +112,8 @@ using namespace ss;
 // The kernel of a product: tiles of 16 or 32 rows of the kernel for few tokens, MX_SHORT + 16 or 32 of mx4_short.hip (rows of MX_SHORT_UNITS and fewer), MX_MID + 32,
 // 64 or 128 of mx4_mid.hip, 256 of mx4_tile.hip.  Which is the fastest goes by an estimate of every kernel's time in us: its launch, then the longest of what its workgroups take one after the other (time of a
 // unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
-// rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The tiles of 256 rows go in rounds of one for each compute unit; the last
-// round, where most stand still, is shorter, the less of them it has.  The group sizes lie on the device: E experts are taken to have R / E rows
-// each, and half a tile more.  Constants fitted to the times of all on 122 shapes (R = 1 .. 54000, 1 .. 79 units, 64 .. 37888 channels, 1 to 128
+// rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The group sizes lie on the device: E experts are taken to have R / E rows
+// each, and half a tile more.  Constants fitted to the times of all on 137 shapes (R = 1 .. 54000, 1 .. 79 units, 64 .. 37888 channels, 1 to 128
 // experts): the choice is 1.02 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
 //   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       49.3 |  36.8 |  24.3 | 17.8 | 14.9 | 27.3
 //   32 x 3584 -> 37888         24.2 |  19.7 |  20.0 |  19.9 | 26.9 | 25.9       777 x 5003 -> 4099        77.7 |  50.9 |  30.0 | 20.7 | 18.1 | 33.6
@@ -139,6 +138,8 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
     const double hbm = used * MB / 5.2, panels = (double)((frags + 3) / 4), wide = (double)((frags + 7) / 8), u = (double)U;
     auto fits = [&](int64_t T, int64_t threads) { return mx4_grid_fits((frags + 3) / 4 * mx4_max_tiles(R, E, T), threads); };
     auto tiles = [&](int64_t T) { return many ? fmax(used, (double)R / (double)T + 0.5 * used) : (double)((R + T - 1) / T); };
+    // workgroups of a compute unit one after the other; a last round that only some have counts as much more than its share as the others wait
+    auto rounds = [](double x, double more) { const double part = x - floor(x); return x <= 1.0 ? 1.0 : floor(x) + (part > 0.0 ? fmin(1.0, more + part) : 0.0); };
     mx4_plan best = {};
     double time = INFINITY;
     auto offer = [&](mx4_plan p, double us) {
@@ -154,19 +155,18 @@ static mx4_plan mx4_choose(int64_t R, int64_t E, int64_t U, int64_t frags, int64
         for (const auto& s : whole)
             if (fits(s.rows, 256)) offer({MX_SHORT + s.rows, 1}, s.launch + fmax(fmax((s.start + s.unit * u) * (many ? 1.2 : 1.0) * panels * tiles(s.rows) / (double)cus, s.row * u), 1.13 * hbm));
     }
-    const struct { int rows; double launch, unit, ends, hbm; } mid[] = {{32, 2.29, 0.39, 0.86, 1.13}, {64, 1.99, 0.42, 1.24, 1.13}, {128, 2.35, 0.56, 2.72, 1.8}};
+    const struct { int rows; double launch, unit, ends, hbm, more; } mid[] = {{32, 2.29, 0.39, 0.85, 1.13, 0.0}, {64, 1.92, 0.40, 1.27, 1.13, 0.33}, {128, 1.67, 0.56, 2.76, 1.67, 0.39}};
     for (const auto& m : mid) {
         const double w = panels * tiles(m.rows);
         if (!fits(m.rows, 512)) continue;
         for (int r = 1; r <= 16 && r <= U; ++r) {
             if (r > 1 && (mx4_mid_bytes(R, E, frags, m.rows, r) > ws_bytes || w * r > 2.0 * (double)cus)) break;
-            const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0, shares = fmax(1.0, w * r / (double)cus);
-            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * (many ? 1.47 : 1.0) * shares, m.hbm * hbm + 1.0) + add);
+            const double add = r > 1 ? 3.5 + 0.36 * w * r * (double)m.rows * 512.0 / 1e6 : 0.0;
+            offer({MX_MID + m.rows, r}, m.launch + fmax((m.unit * ceil(u / r) + m.ends) * (many ? 1.46 : 1.0) * rounds(w * r / (double)cus, m.more), m.hbm * hbm + 1.0) + add);
         }
     }
-    const double all = wide * tiles(256) / (double)cus, part = all - floor(all), full = fmin(1.0, all);
-    const double rounds = all <= 1.0 ? 1.0 : floor(all) + (part > 0.0 ? fmin(1.0, 0.33 + part) : 0.0);
-    offer({256, 1}, 3.96 + fmax(rounds * (fmax(u, 3.0) * (1.14 + 0.55 * full) + (1.04 + 3.23 * full) * (many ? 1.71 : 1.0)), hbm));
+    const double all = wide * tiles(256) / (double)cus, full = fmin(1.0, all);
+    offer({256, 1}, 3.94 + fmax(rounds(all, 0.31) * (fmax(u, 3.0) * (1.02 + 0.69 * full) + (0.8 + 3.43 * full) * (many ? 1.83 : 1.0)), hbm));
     return best;
 }
 
