@@ -7,7 +7,7 @@
 // Two fragments' worth of rows, 64, measured 42.3 us where 32 measure 23.9: a third as many wavefronts fit.  A loop over a tile's rows with the weights
 // kept takes 20.8 to 21.5 there, but 12.6 to 16.5 for 8000 rows, 64 experts, 256 -> 1024 in place of 12.0.
 //   500 rows of 64 experts, 512 -> 2048: 10.2 us, 35.7 MB of weights at 3.5 TB/s;  2032 gated rows of 69 experts, 278 -> 1408: 21.1 us (52 MB of weights);
-//   8000 rows of 64 experts, 256 -> 1024: 12.6 us (the best other kernel 16.6).
+//   8000 rows of 64 experts, 256 -> 1024: 12.6 us (the best other kernel 14.1).
 #include "mx4_common.h"
 #include "device_info.h"
 
