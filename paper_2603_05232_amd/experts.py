@@ -26,13 +26,12 @@ class Packed:
         self.O, self.K, self.experts, self.gated = W.shape[0] // experts // (2 if gated else 1), W.shape[1], experts, gated
         self.codes, self.scales = binding.mx4_quant(W)
         self.w_vals, self.w_meta = binding.mx4_pack(self.codes, self.scales, self.K, experts=experts, gated=gated)
-        self.scratch = None
 
     def __call__(self, codes, scales, offsets=None):
+        # A workspace for each call, so that the allocator keeps it to this call's stream, or to the graph that is being captured: one that calls share would be
+        # written by two streams at once, and a graph would go on writing to one that has been replaced since.
         n = binding.mx4_gemm_workspace_bytes(codes.shape[0], self.O, self.K, experts=self.experts, gated=self.gated)
-        if n and (self.scratch is None or self.scratch.numel() < n):
-            self.scratch = torch.empty((n,), dtype=torch.uint8, device=codes.device)
-        ws = self.scratch if n else None
+        ws = torch.empty((n,), dtype=torch.uint8, device=codes.device) if n else None
         if offsets is None:
             return binding.mx4_gemm(codes, scales, self.w_vals, self.w_meta, self.O, self.K, gated=self.gated, workspace=ws)
         return binding.mx4_grouped_gemm(codes, scales, offsets, self.w_vals, self.w_meta, self.O, self.K, gated=self.gated, workspace=ws)
