@@ -338,23 +338,37 @@ def slide_sparse_gemm_static(X_lifted, s_x, w_vals, w_meta, s_w, O: int, dtype: 
 
 # ---- microscaled 4-bit operands and layers of experts -------------------------------------------------------------------------
 
-def _row_stride(t: torch.Tensor) -> int:
+# A kernel reads and writes through every address that it is given, so each of them has to lie on the GPU of the operator's first tensor.
+
+def _beside(t: torch.Tensor, first: torch.Tensor) -> bool:
+    return first.is_cuda and t.is_cuda and t.get_device() == first.get_device()
+
+
+def _row_stride(t: torch.Tensor, first: torch.Tensor) -> int:
     """Elements between the rows of a matrix whose rows are dense (of a single row: its width)."""
     rows, width = t.shape
-    assert t.is_cuda and (width < 2 or t.stride(1) == 1)
+    assert _beside(t, first) and (width < 2 or t.stride(1) == 1)
     return t.stride(0) if rows > 1 else width
 
 
-def _dense_i32(t: torch.Tensor, what: str) -> int:
+def _dense_i32(t: torch.Tensor, what: str, first: torch.Tensor) -> int:
     if t.dtype != torch.int32:
         raise TypeError(f"{what} must be int32, got {t.dtype}")
-    assert t.is_cuda and t.is_contiguous()
+    assert _beside(t, first) and t.is_contiguous()
     return t.data_ptr()
 
 
-def _mx4_operand(codes: torch.Tensor, scales: torch.Tensor, K: int):
+def _workspace(t, first: torch.Tensor):
+    """(address, bytes) of an optional workspace."""
+    if t is None:
+        return None, 0
+    assert _beside(t, first) and t.is_contiguous()
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _mx4_operand(codes: torch.Tensor, scales: torch.Tensor, K: int, first: torch.Tensor):
     """Checks that codes[R, 128 U] and scales[U, R, 8] are rows of K values."""
-    assert codes.is_cuda and codes.is_contiguous() and scales.is_contiguous() and codes.dtype == scales.dtype == torch.uint8
+    assert _beside(codes, first) and _beside(scales, first) and codes.is_contiguous() and scales.is_contiguous() and codes.dtype == scales.dtype == torch.uint8
     assert codes.shape[1] == mx4_row_bytes(K) and scales.shape == (codes.shape[1] // 128, codes.shape[0], 8)
 
 
@@ -385,8 +399,8 @@ def mx4_quant(X: torch.Tensor, rows=None, codes=None, scales=None):
     if scales is None:
         scales = X.new_empty((width // 128, R, 8), dtype=torch.uint8)
     assert codes.shape[0] == R
-    _mx4_operand(codes, scales, K)
-    code = load().mx4_quant(X.data_ptr(), _in_code(X), M, K, _row_stride(X), None if rows is None else _dense_i32(rows, "rows"), R, codes.data_ptr(),
+    _mx4_operand(codes, scales, K, X)
+    code = load().mx4_quant(X.data_ptr(), _in_code(X), M, K, _row_stride(X, X), None if rows is None else _dense_i32(rows, "rows", X), R, codes.data_ptr(),
                             scales.data_ptr(), _stream())
     if code:
         _check(code, "mx4_quant")
@@ -400,11 +414,11 @@ def mx4_dequant(codes: torch.Tensor, scales: torch.Tensor, K: int, dtype: torch.
     done = _mx4_calls.mx4_dequant(codes, scales, K, _IN_CODE.get(dtype), out)
     if done is not None:
         return done
-    _mx4_operand(codes, scales, K)
+    _mx4_operand(codes, scales, K, codes)
     if out is None:
         out = codes.new_empty((codes.shape[0], K), dtype=dtype)
     assert out.shape == (codes.shape[0], K)
-    code = load().mx4_dequant(codes.data_ptr(), scales.data_ptr(), codes.shape[0], K, _in_code(out), out.data_ptr(), _row_stride(out), _stream())
+    code = load().mx4_dequant(codes.data_ptr(), scales.data_ptr(), codes.shape[0], K, _in_code(out), out.data_ptr(), _row_stride(out, codes), _stream())
     if code:
         _check(code, "mx4_dequant")
     return out
@@ -418,7 +432,7 @@ def mx4_packed_sizes(O: int, K: int, experts: int = 1, gated: bool = False):
 
 def mx4_pack(codes: torch.Tensor, scales: torch.Tensor, K: int, experts: int = 1, gated: bool = False):
     """Codes of experts x [O,K] weights (gated: of experts x [2 O,K], gate's rows before up's) -> (w_vals, w_meta)."""
-    _mx4_operand(codes, scales, K)
+    _mx4_operand(codes, scales, K, codes)
     O, rest = divmod(codes.shape[0], experts * (2 if gated else 1))
     if rest:
         raise SlideSparseError(3, "mx4_pack")
@@ -434,14 +448,15 @@ def mx4_gemm_workspace_bytes(R: int, O: int, K: int, experts: int = 1, gated: bo
 
 
 def _mx4_product(name, offsets, codes, scales, w_vals, w_meta, experts, O, K, gated, out, workspace):
-    _mx4_operand(codes, scales, K)
+    _mx4_operand(codes, scales, K, codes)
     sizes = _mx4_sizes(O, K, experts, gated)
+    assert _beside(w_vals, codes) and _beside(w_meta, codes) and w_vals.dtype == w_meta.dtype == torch.uint8
     assert w_vals.is_contiguous() and w_meta.is_contiguous() and (w_vals.numel(), w_meta.numel()) == sizes
     R = codes.shape[0]
     if out is None:
         out = codes.new_empty((R, O), dtype=torch.bfloat16)
     assert out.dtype == torch.bfloat16 and out.shape == (R, O)
-    tail = (O, K, int(gated), out.data_ptr(), _row_stride(out), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    tail = (O, K, int(gated), out.data_ptr(), _row_stride(out, codes), *_workspace(workspace, codes), _stream())
     if offsets is None:
         code = load().mx4_gemm(codes.data_ptr(), scales.data_ptr(), w_vals.data_ptr(), w_meta.data_ptr(), R, *tail)
     else:
@@ -471,7 +486,7 @@ def mx4_grouped_gemm(codes, scales, offsets, w_vals, w_meta, O: int, K: int, gat
     done = _mx4_calls.mx4_product(offsets, codes, scales, w_vals, w_meta, O, K, gated, out, workspace)
     if done is not None:
         return done
-    return _mx4_product("mx4_grouped_gemm", _dense_i32(offsets, "offsets"), codes, scales, w_vals, w_meta, offsets.shape[0] - 1, O, K, gated, out, workspace)
+    return _mx4_product("mx4_grouped_gemm", _dense_i32(offsets, "offsets", codes), codes, scales, w_vals, w_meta, offsets.shape[0] - 1, O, K, gated, out, workspace)
 
 
 def expert_route_workspace_bytes(M: int, E: int, k: int) -> int:
@@ -494,9 +509,8 @@ def expert_route(logits: torch.Tensor, k: int, renormalise: bool = True, workspa
     weights = logits.new_empty((M, max(k, 0)), dtype=torch.float32)
     rows = logits.new_empty((M * max(k, 0),), dtype=torch.int32)
     offsets = logits.new_empty((E + 1,), dtype=torch.int32)
-    code = load().expert_route(logits.data_ptr(), _in_code(logits), M, E, _row_stride(logits), k, int(renormalise), ids.data_ptr(), weights.data_ptr(),
-                               slots.data_ptr(), rows.data_ptr(), offsets.data_ptr(), _ptr(workspace),
-                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
+    code = load().expert_route(logits.data_ptr(), _in_code(logits), M, E, _row_stride(logits, logits), k, int(renormalise), ids.data_ptr(), weights.data_ptr(),
+                               slots.data_ptr(), rows.data_ptr(), offsets.data_ptr(), *_workspace(workspace, logits), _stream())
     if code:
         _check(code, "expert_route")
     return ids, weights, slots, rows, offsets
@@ -511,13 +525,13 @@ def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, 
         return done
     R, O = Y.shape
     M, k = slots.shape
-    assert weights.shape == (M, k) and weights.is_contiguous() and weights.dtype == torch.float32 and Y.dtype == torch.bfloat16
+    assert _beside(weights, Y) and weights.shape == (M, k) and weights.is_contiguous() and weights.dtype == torch.float32 and Y.dtype == torch.bfloat16
     assert base is None or (base.shape == (M, O) and base.dtype == torch.bfloat16)
     if out is None:
         out = Y.new_empty((M, O))
     assert out.shape == (M, O) and out.dtype == torch.bfloat16
-    code = load().expert_combine(Y.data_ptr(), R, O, _row_stride(Y), _dense_i32(slots, "slots"), weights.data_ptr(), M, k, _ptr(base),
-                                 0 if base is None else _row_stride(base), out.data_ptr(), _row_stride(out), _stream())
+    code = load().expert_combine(Y.data_ptr(), R, O, _row_stride(Y, Y), _dense_i32(slots, "slots", Y), weights.data_ptr(), M, k, _ptr(base),
+                                 0 if base is None else _row_stride(base, Y), out.data_ptr(), _row_stride(out, Y), _stream())
     if code:
         _check(code, "expert_combine")
     return out

@@ -202,15 +202,18 @@ struct Mx4 {
 
 bool float_or_bf16(const at::Tensor& t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
 ss_act_dtype in_code(const at::Tensor& t) { return t.scalar_type() == at::kFloat ? SS_IN_F32 : SS_IN_BF16; }
-// a matrix on the GPU whose rows are dense, and the elements between its rows
-bool matrix(const at::Tensor& t) { return t.is_cuda() && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1); }
+// on the GPU of the operator's first tensor: kernels read and write through every address that they are given
+bool beside(const at::Tensor& t, const at::Tensor& first) { return first.is_cuda() && t.device() == first.device(); }
+// a matrix whose rows are dense, and the elements between its rows
+bool matrix(const at::Tensor& t, const at::Tensor& first) { return beside(t, first) && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1); }
 int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
-bool dense(const at::Tensor& t, at::ScalarType type) { return t.is_cuda() && t.scalar_type() == type && t.is_contiguous(); }
+bool dense(const at::Tensor& t, at::ScalarType type, const at::Tensor& first) { return beside(t, first) && t.scalar_type() == type && t.is_contiguous(); }
+bool workspace(PyObject* o, const at::Tensor& first) { return o == Py_None || (beside(THPVariable_Unpack(o), first) && THPVariable_Unpack(o).is_contiguous()); }
 // codes[R, 128 U] and scales[U, R, 8] of rows of K values
-bool code_rows(const at::Tensor& codes, const at::Tensor& scales, int64_t K)
+bool code_rows(const at::Tensor& codes, const at::Tensor& scales, int64_t K, const at::Tensor& first)
 {
     const int64_t width = mx4.row_bytes(K);
-    return width > 0 && dense(codes, at::kByte) && dense(scales, at::kByte) && codes.dim() == 2 && scales.dim() == 3 && codes.size(1) == width &&
+    return width > 0 && dense(codes, at::kByte, first) && dense(scales, at::kByte, first) && codes.dim() == 2 && scales.dim() == 3 && codes.size(1) == width &&
            scales.size(0) == width / 128 && scales.size(1) == codes.size(0) && scales.size(2) == 8;
 }
 PyObject* wrap(at::Tensor& made, PyObject* given) { return made.defined() ? THPVariable_Wrap(std::move(made)) : Py_NewRef(given); }
@@ -230,9 +233,9 @@ PyObject* py_mx4_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (!mx4.quant || n != 4 || !plain(a[0]) || !plain_or_none(a[1]) || !plain_or_none(a[2]) || !plain_or_none(a[3]) || modes_active()) Py_RETURN_NONE;
     const at::Tensor& X = THPVariable_Unpack(a[0]);
-    if (!matrix(X) || !float_or_bf16(X)) Py_RETURN_NONE;
+    if (!matrix(X, X) || !float_or_bf16(X)) Py_RETURN_NONE;
     const int64_t M = X.size(0), K = X.size(1), width = mx4.row_bytes(K);
-    if (width < 0 || (a[1] != Py_None && (THPVariable_Unpack(a[1]).dim() != 1 || !dense(THPVariable_Unpack(a[1]), at::kInt)))) Py_RETURN_NONE;
+    if (width < 0 || (a[1] != Py_None && (THPVariable_Unpack(a[1]).dim() != 1 || !dense(THPVariable_Unpack(a[1]), at::kInt, X)))) Py_RETURN_NONE;
     const int64_t R = a[1] == Py_None ? M : THPVariable_Unpack(a[1]).size(0);
     at::Tensor codes, scales;
     ss_status st;
@@ -246,7 +249,7 @@ PyObject* py_mx4_quant(PyObject*, PyObject* const* a, Py_ssize_t n)
         } else if (a[2] == Py_None) codes = at::empty({R, width}, bytes);
         else if (a[3] == Py_None) scales = at::empty({width / 128, R, 8}, bytes);
         const at::Tensor &c = codes.defined() ? codes : THPVariable_Unpack(a[2]), &s = scales.defined() ? scales : THPVariable_Unpack(a[3]);
-        st = code_rows(c, s, K) && c.size(0) == R
+        st = code_rows(c, s, K, X) && c.size(0) == R
                  ? mx4.quant(X.data_ptr(), in_code(X), M, K, row_stride(X), static_cast<const int32_t*>(address(a[1])), R, c.data_ptr(), s.data_ptr(), current_stream())
                  : SS_ERR_SHAPE;
     }
@@ -266,14 +269,14 @@ PyObject* py_mx4_dequant(PyObject*, PyObject* const* a, Py_ssize_t n)
     int64_t K, type;
     if (!mx4.dequant || n != 5 || !plain(a[0]) || !plain(a[1]) || !integer(a[2], 1, INT64_MAX, K) || !integer(a[3], 0, 1, type) || !plain_or_none(a[4]) || modes_active()) Py_RETURN_NONE;
     const at::Tensor &codes = THPVariable_Unpack(a[0]), &scales = THPVariable_Unpack(a[1]);
-    if (!code_rows(codes, scales, K)) Py_RETURN_NONE;
+    if (!code_rows(codes, scales, K, codes)) Py_RETURN_NONE;
     at::Tensor made;
     ss_status st;
     {
         Unlocked u;
         if (a[4] == Py_None) made = at::empty({codes.size(0), K}, codes.options().dtype(type == SS_IN_F32 ? at::kFloat : at::kBFloat16));
         const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[4]);
-        st = matrix(y) && float_or_bf16(y) && y.size(0) == codes.size(0) && y.size(1) == K
+        st = matrix(y, codes) && float_or_bf16(y) && y.size(0) == codes.size(0) && y.size(1) == K
                  ? mx4.dequant(codes.data_ptr(), scales.data_ptr(), codes.size(0), K, in_code(y), y.data_ptr(), row_stride(y), current_stream())
                  : SS_ERR_SHAPE;
     }
@@ -293,10 +296,10 @@ PyObject* py_mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n)
     const bool grouped = a[0] != Py_None;
     const int gated = a[7] == Py_True;
     const at::Tensor &codes = THPVariable_Unpack(a[1]), &scales = THPVariable_Unpack(a[2]), &wv = THPVariable_Unpack(a[3]), &wm = THPVariable_Unpack(a[4]);
-    if (!code_rows(codes, scales, K) || (grouped && (THPVariable_Unpack(a[0]).dim() != 1 || !dense(THPVariable_Unpack(a[0]), at::kInt)))) Py_RETURN_NONE;
+    if (!code_rows(codes, scales, K, codes) || (grouped && (THPVariable_Unpack(a[0]).dim() != 1 || !dense(THPVariable_Unpack(a[0]), at::kInt, codes))) || !workspace(a[9], codes)) Py_RETURN_NONE;
     const int64_t R = codes.size(0), E = grouped ? THPVariable_Unpack(a[0]).size(0) - 1 : 1;
     size_t vb, mb;
-    if (mx4.packed_sizes(E, O, K, gated, &vb, &mb) != SS_OK || !dense(wv, at::kByte) || !dense(wm, at::kByte) || (size_t)wv.numel() != vb || (size_t)wm.numel() != mb) Py_RETURN_NONE;
+    if (mx4.packed_sizes(E, O, K, gated, &vb, &mb) != SS_OK || !dense(wv, at::kByte, codes) || !dense(wm, at::kByte, codes) || (size_t)wv.numel() != vb || (size_t)wm.numel() != mb) Py_RETURN_NONE;
     void* const ws = address(a[9]);
     const size_t ws_bytes = a[9] == Py_None ? 0 : THPVariable_Unpack(a[9]).nbytes();
     at::Tensor made;
@@ -305,7 +308,7 @@ PyObject* py_mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n)
         Unlocked u;
         if (a[8] == Py_None) made = at::empty({R, O}, codes.options().dtype(at::kBFloat16));
         const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[8]);
-        if (!matrix(y) || y.scalar_type() != at::kBFloat16 || y.size(0) != R || y.size(1) != O) st = SS_ERR_SHAPE;
+        if (!matrix(y, codes) || y.scalar_type() != at::kBFloat16 || y.size(0) != R || y.size(1) != O) st = SS_ERR_SHAPE;
         else if (grouped)
             st = mx4.grouped_gemm(codes.data_ptr(), scales.data_ptr(), static_cast<const int32_t*>(address(a[0])), wv.data_ptr(), wm.data_ptr(), R, E, O, K, gated, y.data_ptr(),
                                   row_stride(y), ws, ws_bytes, current_stream());
@@ -323,7 +326,7 @@ PyObject* py_expert_route(PyObject*, PyObject* const* a, Py_ssize_t n)
     int64_t k;
     if (!mx4.route || n != 4 || !plain(a[0]) || !integer(a[1], 1, 64, k) || !PyBool_Check(a[2]) || !plain_or_none(a[3]) || modes_active()) Py_RETURN_NONE;
     const at::Tensor& x = THPVariable_Unpack(a[0]);
-    if (!matrix(x) || !float_or_bf16(x) || k > x.size(1)) Py_RETURN_NONE;
+    if (!matrix(x, x) || !float_or_bf16(x) || k > x.size(1) || !workspace(a[3], x)) Py_RETURN_NONE;
     const int64_t M = x.size(0), E = x.size(1);
     at::Tensor ids, weights, slots, rows, offsets, scratch;
     ss_status st;
@@ -361,10 +364,10 @@ PyObject* py_expert_combine(PyObject*, PyObject* const* a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (!mx4.combine || n != 5 || !plain(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain_or_none(a[3]) || !plain_or_none(a[4]) || modes_active()) Py_RETURN_NONE;
     const at::Tensor &Y = THPVariable_Unpack(a[0]), &slots = THPVariable_Unpack(a[1]), &weights = THPVariable_Unpack(a[2]);
-    if (!matrix(Y) || Y.scalar_type() != at::kBFloat16 || slots.dim() != 2 || !dense(slots, at::kInt) || !dense(weights, at::kFloat) || weights.sizes() != slots.sizes()) Py_RETURN_NONE;
+    if (!matrix(Y, Y) || Y.scalar_type() != at::kBFloat16 || slots.dim() != 2 || !dense(slots, at::kInt, Y) || !dense(weights, at::kFloat, Y) || weights.sizes() != slots.sizes()) Py_RETURN_NONE;
     const int64_t M = slots.size(0), k = slots.size(1), O = Y.size(1);
     if (k > INT_MAX) Py_RETURN_NONE;
-    auto fits = [&](const at::Tensor& t) { return matrix(t) && t.scalar_type() == at::kBFloat16 && t.size(0) == M && t.size(1) == O; };
+    auto fits = [&](const at::Tensor& t) { return matrix(t, Y) && t.scalar_type() == at::kBFloat16 && t.size(0) == M && t.size(1) == O; };
     if (a[3] != Py_None && !fits(THPVariable_Unpack(a[3]))) Py_RETURN_NONE;
     at::Tensor made;
     ss_status st;
