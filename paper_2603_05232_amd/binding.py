@@ -351,10 +351,10 @@ def _row_stride(t: torch.Tensor, first: torch.Tensor) -> int:
     return t.stride(0) if rows > 1 else width
 
 
-def _dense_i32(t: torch.Tensor, what: str, first: torch.Tensor) -> int:
+def _dense_i32(t: torch.Tensor, what: str, first: torch.Tensor, dims: int = 1) -> int:
     if t.dtype != torch.int32:
         raise TypeError(f"{what} must be int32, got {t.dtype}")
-    assert _beside(t, first) and t.is_contiguous()
+    assert _beside(t, first) and t.is_contiguous() and t.dim() == dims
     return t.data_ptr()
 
 
@@ -530,7 +530,7 @@ def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, 
     if out is None:
         out = Y.new_empty((M, O))
     assert out.shape == (M, O) and out.dtype == torch.bfloat16
-    code = load().expert_combine(Y.data_ptr(), R, O, _row_stride(Y, Y), _dense_i32(slots, "slots", Y), weights.data_ptr(), M, k, _ptr(base),
+    code = load().expert_combine(Y.data_ptr(), R, O, _row_stride(Y, Y), _dense_i32(slots, "slots", Y, dims=2), weights.data_ptr(), M, k, _ptr(base),
                                  0 if base is None else _row_stride(base, Y), out.data_ptr(), _row_stride(out, Y), _stream())
     if code:
         _check(code, "expert_combine")

@@ -124,3 +124,13 @@ def test_packed_weights_of_another_type_are_refused(library, op, name):
     with pytest.raises(AssertionError):
         call(tensors)
     assert library.launched == []
+
+
+@pytest.mark.parametrize("op,name", [("mx4_quant", "rows"), ("mx4_grouped_gemm", "offsets")])
+def test_lists_of_two_dimensions_are_refused(library, op, name):
+    """Their first dimension alone would be taken for the number of rows, or of experts."""
+    tensors, call = operands()[op]
+    tensors[name] = there((tensors[name].numel(), 2), I32)
+    with pytest.raises(AssertionError):
+        call(tensors)
+    assert library.launched == []
