@@ -36,6 +36,9 @@ _CALLED = ("slide_lifted_ld", "act_lift_quant", "slide_sparse_gemm_ws", "slide_s
 _CALLED_MX4 = ("mx4_row_bytes", "mx4_quant", "mx4_dequant", "mx4_packed_sizes", "mx4_gemm", "mx4_grouped_gemm", "expert_route_workspace_bytes", "expert_route",
                "expert_combine")                          # of its bind_mx4()
 
+# the calls that it does
+_MODULE_CALLS = ("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused", "mx4_quant", "mx4_dequant", "mx4_product", "expert_route", "expert_combine")
+
 _lib = None
 _calls = None
 _mx4_calls = None                                         # the module again, for the 4-bit expert layer's calls
@@ -105,16 +108,18 @@ def load():
 
 
 def _load_calls(lib):
-    """The extension module, told which library to call; without one that was built for this torch, a stand-in that leaves every
-    call to the general path, which needs the library alone."""
+    """The extension module, told which library to call; without one that was built for this torch and from these sources, as far as its names tell, a stand-in
+    that leaves every call to the general path, which needs the library alone."""
     try:
         from . import _calls as calls
         if calls.torch_version != str(torch.__version__):
             raise ImportError(f"built for torch {calls.torch_version}, not {torch.__version__}")
+        missing = [name for name in (*_MODULE_CALLS, "bind", "bind_mx4") if not hasattr(calls, name)]
+        if missing:
+            raise ImportError(f"an older build, without {', '.join(missing)}")
     except (ImportError, AttributeError) as e:
         warnings.warn(f"{CALLS_PATH} cannot be used ({e}): calls go through ctypes, 6 us more on the host for each layer", RuntimeWarning, stacklevel=3)
-        return types.SimpleNamespace(**dict.fromkeys(("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused", "mx4_quant", "mx4_dequant", "mx4_product",
-                                                    "expert_route", "expert_combine"), lambda *args: None))
+        return types.SimpleNamespace(**dict.fromkeys(_MODULE_CALLS, lambda *args: None))
     calls.bind(SlideSparseError, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED))
     calls.bind_mx4(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED_MX4))
     return calls
