@@ -214,7 +214,10 @@ ss_status slide_sparse_gemm_fused_ws(const void* Xq, const float* s_x, const voi
  *   codes[row][mx4_row_bytes(K)]        two codes to a byte, the even value in the low half; 128 bytes a unit
  *   scales[unit][row][8]                byte j: values 32 j .. 32 j + 31 of the unit; mx4_row_scales(K) bytes a row in all
  * Limits: 1 <= K <= 2^24, rows <= 2^24, experts <= 1024; codes, scales and packed weights 16-byte aligned; other matrices need
- * the alignment of an element, whatever their strides. */
+ * the alignment of an element, whatever their strides.  A launch counts its threads in 32 bits, so these are refused as well (SS_ERR_SHAPE), from some 2^35
+ * values on: mx4_quant where rows of codes x ceil(K / 512) (fp32) or ceil(K / 1024) (bf16) pass 2^26 - 4, mx4_dequant where rows x ceil(K / 512) do,
+ * expert_combine where M x ceil(O / 8) pass 2^32 - 256, mx4_pack where fragments of 32 rows x units pass 2^24 - 1 (64 GiB of packed codes;
+ * experts follow one another there, so more of them can be packed in parts). */
 int64_t mx4_row_bytes(int64_t K);       /* 128 ceil(K / 256); -1 on a bad K */
 int64_t mx4_row_scales(int64_t K);      /* 8 ceil(K / 256); -1 on a bad K */
 
