@@ -24,8 +24,27 @@ class Packed:
 
     def __init__(self, W: torch.Tensor, experts: int = 1, gated: bool = False):
         self.O, self.K, self.experts, self.gated = W.shape[0] // experts // (2 if gated else 1), W.shape[1], experts, gated
-        self.codes, self.scales = binding.mx4_quant(W)
-        self.w_vals, self.w_meta = binding.mx4_pack(self.codes, self.scales, self.K, experts=experts, gated=gated)
+        self.w_vals, self.w_meta = binding.mx4_pack(*binding.mx4_quant(W), self.K, experts=experts, gated=gated)
+
+    def _rows(self, packed: torch.Tensor, order) -> torch.Tensor:
+        """What was packed, [rows, units, bytes], from the operand order of csrc/mx4_common.h: its dimensions in `order` are those of a fragment's rows, the unit, the bytes."""
+        t = packed.permute(order).reshape(self.experts, packed.shape[1] * 32, packed.shape[2], -1)
+        if not self.gated:
+            return t[:, :self.O].flatten(0, 1)
+        return t[:, :2 * self.O].unflatten(1, (self.O, 2)).transpose(1, 2).flatten(0, 2)
+
+    # The codes and scales of the weights, read back from the packed ones: a layer does not need them, and kept beside those they would double its memory.
+    @property
+    def codes(self) -> torch.Tensor:
+        """[rows, 128 units], as mx4_quant wrote them."""
+        units = binding.mx4_row_bytes(self.K) // 128
+        return self._rows(self.w_vals.view(self.experts, -1, units, 2, 2, 4, 4, 4, 16), (0, 1, 6, 4, 7, 2, 5, 3, 8)).flatten(1).contiguous()
+
+    @property
+    def scales(self) -> torch.Tensor:
+        """[units, rows, 8], as mx4_quant wrote them."""
+        units = binding.mx4_row_bytes(self.K) // 128
+        return self._rows(self.w_meta.view(self.experts, -1, units, 4, 4, 4, 2, 2), (0, 1, 4, 6, 5, 2, 3, 7)).transpose(0, 1).contiguous()
 
     def __call__(self, codes, scales, offsets=None):
         # A workspace for each call, so that the allocator keeps it to this call's stream, or to the graph that is being captured: one that calls share would be
