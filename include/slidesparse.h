@@ -228,7 +228,8 @@ int64_t mx4_row_scales(int64_t K);      /* 8 ceil(K / 256); -1 on a bad K */
 ss_status mx4_quant(const void* X, ss_act_dtype in_dtype, int64_t M, int64_t K, int64_t ldx, const int32_t* rows, int64_t R,
                     void* codes, void* scales, void* stream);
 
-/* The values that codes[R] and their scales stand for, as fp32 (exact) or bf16 (exact but for magnitudes below 2^-133), row stride ldy. */
+/* The values that codes[R] and their scales stand for, as fp32 or bf16, row stride ldy.  Both hold them exactly; magnitudes of 2^128 and more, which mx4_quant does
+ * not write, give an infinity. */
 ss_status mx4_dequant(const void* codes, const void* scales, int64_t R, int64_t K, ss_act_dtype out_dtype, void* Y, int64_t ldy,
                       void* stream);
 

@@ -36,7 +36,8 @@ __device__ inline float row_sum(float v) { return __int_as_float(row_all(__float
 // below its own, whatever the order in which they were set.
 // A lane keeps KL choices, number 16 c + l.
 // ONE: the only workgroup, which then knows the order; otherwise slots gets the places and counts[workgroup][expert] the numbers of rows.
-// Bound by instructions (8192 x 128 bf16, k = 8: 6.9 us for 2 MB): a choice is about 8 EL + 30 of them, for four tokens at once (a wavefront for each token, 8192 x 128 bf16, k = 8: 14.4 us).
+// Bound by instructions on the compute units that have a workgroup (8192 x 128 bf16, k = 8: 7.0 us for 2 MB, 128 workgroups on 256): a choice is about 8 EL + 30 of
+// them, for four tokens at once (a wavefront for each token, 8192 x 128 bf16, k = 8: 14.4 us).
 template <typename T, int EL, int KL, bool ONE>
 __global__ __launch_bounds__(RT_THREADS) void k_route_choose(const T* __restrict__ logits, int64_t M, int E, int64_t ld, int k, bool renormalise,
                                                              int32_t* __restrict__ ids, float* __restrict__ weights, int32_t* __restrict__ slots,
@@ -153,7 +154,14 @@ __global__ __launch_bounds__(256) void k_route_scan(int32_t* __restrict__ counts
 }
 
 // Places within the workgroups -> places in the order of the experts.  SCANNED: k_route_scan has added the counts up; otherwise every workgroup adds
-// up all of them itself, which with few workgroups costs less than the launch in between (8192 tokens, 128 experts: 5.0 us against 3.9 and 4.3).  Bound by those waits: 3.7 us for 8192 x 8 places.
+// up all of them itself, which with few workgroups costs less than the launch in between.  Bound by those waits: 4.0 us for 8192 x 8 places.
+// The whole call, own sums | scan, us, at 128 | 256 | 320 | 512 workgroups:
+//     8 experts, k = 2    6.3 |  7.5      7.1 |  8.0      9.6 |  9.4     11.0 |  9.8
+//    64, k = 4            7.2 |  8.6      8.2 |  9.1     11.2 | 10.9     12.7 | 11.8
+//   128, k = 8           10.7 | 11.6     12.3 | 12.5     17.8 | 16.1     22.2 | 17.8
+//   256, k = 8           14.8 | 14.9     18.0 | 16.7     27.5 | 22.0     34.7 | 24.7
+//  1024, k = 8           55.5 | 51.0     65.1 | 54.8      122 | 96.0      144 |  101
+// so beyond 128 experts the line comes late.
 constexpr int RT_OWN_SUMS = 256;         // workgroups up to which they do
 template <bool SCANNED>
 __global__ __launch_bounds__(RT_THREADS) void k_route_place(const int32_t* __restrict__ ids, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
@@ -220,7 +228,7 @@ __device__ inline void get8(const uint16_t* p, int have, float (&f)[8])
 }
 
 // out = sum of weights Y[slots] + base, in the order of the choices.  A thread takes eight columns of a token; with a known number of rows (K > 0) it asks for
-// all of them before it adds the first.  Bound by HBM: 8192 tokens of 8 rows of 2048 57.5 us, 270.5 MB read and 33.6 written at 5.3 TB/s.
+// all of them before it adds the first.  Bound by HBM: 8192 tokens of 8 rows of 2048 57.5 us in a trace, 270.5 MB read and 33.6 written at 5.3 TB/s.
 template <int K>
 __global__ __launch_bounds__(256) void k_combine(const uint16_t* __restrict__ Y, int64_t R, int64_t O, int64_t ldy, const int32_t* __restrict__ slots,
                                                  const float* __restrict__ weights, int64_t M, int k, const uint16_t* __restrict__ base, int64_t ldb,

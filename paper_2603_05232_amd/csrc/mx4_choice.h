@@ -10,7 +10,8 @@ namespace ss {
 // unit and of a workgroup's start and end, times workgroups for each compute unit), what the weights take that are read once for every tile of
 // rows (MB over MB per us, L2 and memory-side cache), and the weights from HBM.  The group sizes lie on the device: E experts are taken to have R / E rows
 // each, and half a tile more.  Constants fitted to the times of all on 137 shapes (R = 1 .. 54000, 1 .. 79 units, 64 .. 37888 channels, 1 to 128
-// experts): the choice is 1.02 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us:
+// experts): the choice is 1.02 of the fastest on average, 1.3 at most.  Times of 16 | 32 | MID + 32 | 64 | 128 | 256, us a call of 24 in a graph, over so many sets of
+// weights that they come from HBM (a call on weights that the memory-side cache holds, or one alone in a trace, is up to a tenth shorter):
 //   1 x 3584 -> 37888          14.0 |  15.3 |  18.4 |  19.1 |   -   |   -       200 x 4096 -> 14336       49.3 |  36.8 |  24.3 | 17.8 | 14.9 | 27.3
 //   32 x 3584 -> 37888         24.2 |  19.7 |  20.0 |  19.9 | 26.9 | 25.9       777 x 5003 -> 4099        77.7 |  50.9 |  30.0 | 20.7 | 18.1 | 33.6
 //   64 x 3584 -> 4608           7.2 |   7.9 |   7.3 |   7.8 |   9.6 | 22.0       3200 x 4096 -> 4096        183 |   136 |  76.2 | 51.9 | 51.5 | 33.4

@@ -7,7 +7,8 @@ namespace ss {
 // Y = X W^T of few token rows.  A workgroup of W wavefronts takes a fragment of 32 channels and a tile of 16 TB token rows.  The wavefronts share out the
 // units of the row; operands go from global memory straight into registers, DEPTH units ahead (a weight is used once: LDS would only
 // add a copy), and the wavefronts' sums meet in LDS.  Bound by the stream of weights; one fragment makes the most workgroups, which is what keeps it going.
-//   1 x 3584 -> 37888: 11.5 us, 72.2 MB fetched at 6.3 TB/s;  16 tokens x 2 experts, gated, 8 experts 4096 -> 14336: 83.8 us, 499.7 MB at 6.0 TB/s
+//   1 x 3584 -> 37888: 11.6 us, 72.2 MB fetched at 6.2 TB/s, part of it from the memory-side cache (13.5 from HBM);  16 tokens x 2 experts, gated, 8 experts
+//   4096 -> 14336: 81 .. 84 us, 499.7 MB at 6.0 TB/s
 template <int W, int TB, int DEPTH, bool GROUPED>
 __global__ __launch_bounds__(64 * W) void k_mx4_stream(mx4_call c)
 {

@@ -7,8 +7,8 @@
 // Y = X W^T between a stream of weights and large tiles.  A unit of a 128 x 128 tile has 512 cycles of products, 470 of reads in LDS and 34 KB of direct loads,
 // and takes some 1150 cycles; without the loads 0.8 of that, without the reads 0.75, without both 0.65.  So no one of them bounds it but the meeting, once
 // for every 16 products of a wavefront, up to which all three have to be done.  Wider tiles would leave compute units without one.
-// 777 x 5003 -> 4099, one tile of 128 rows for a compute unit: 17.2 us, 1.85 PFLOP/s, a third of it the start (first loads) and the end;
-// 2000 rows of 64 experts, 2048 -> 1408, tiles of 64 rows: 27.1 us, 100.5 MB fetched at 3.7 TB/s, the rest start and end.
+// 777 x 5003 -> 4099, one tile of 128 rows for a compute unit: 17.1 us in a trace, 1.86 PFLOP/s, a third of it the start (first loads) and the end;
+// 2000 rows of 64 experts, 2048 -> 1408, tiles of 64 rows: 27.3 us, 100.5 MB fetched at 3.7 TB/s, the rest start and end.
 //
 // With few tiles and long rows the units of a row are split into ranges, a workgroup each; their sums go through the workspace and a second kernel
 // adds them in the order of the ranges.

@@ -2,8 +2,8 @@
 //
 // Y = X W^T of many rows.  Bound by power: at 8192 x 16384 -> 8192 the products alone take 60 % of the time at the clock they leave, LDS reads of operands
 // 19 %, direct loads 10 %.  So the tile is as large as the registers and LDS allow, which makes the fewest reads of both a product.
-//   8192 x 3584 -> 37888: 506 us, 4.40 PFLOP/s;  8192 rows of 8 experts, 14336 -> 4096: 266 us, 3.62 (a third round a quarter full; even groups 218);
-//   8192 x 16384 -> 8192: 4.8 PFLOP/s;  4000 x 256 -> 4096, one unit a row: 13.7 us
+//   8192 x 3584 -> 37888: 510 .. 526 us on one card and another, 4.2 .. 4.4 PFLOP/s;  8192 rows of 8 experts, 14336 -> 4096: 268 us, 3.59 (a third round a
+//   quarter full; even groups 218);  8192 x 16384 -> 8192: 453 us, 4.86 PFLOP/s;  4000 x 256 -> 4096, one unit a row: 13.7 us
 //
 // Persistent workgroups of eight wavefronts, two per SIMD, of 128 channels x 64 rows = 8 x 4 blocks of the 16x16x128 instruction; a unit of 256
 // values is two steps.
