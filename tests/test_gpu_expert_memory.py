@@ -13,12 +13,14 @@ def test_no_more_than_the_packed_weights():
     hidden, inner, experts = 2048, 1408, 8
     binding.load()
     torch.cuda.synchronize()
-    before = torch.cuda.memory_allocated()
+    # what was asked for: what is allocated also counts the unused ends of blocks that the allocator has cached
+    requested = lambda: torch.cuda.memory_stats()["requested_bytes.all.current"]  # noqa: E731
+    before = requested()
     layer = ExpertLayer(DEV, hidden, inner, experts, top=2, shared=True)
-    held = torch.cuda.memory_allocated() - before
+    held = requested() - before
     parts = [n for K, O, E, gated in ((hidden, inner, experts, True), (inner, hidden, experts, False), (hidden, inner, 1, True), (inner, hidden, 1, False))
              for n in binding.mx4_packed_sizes(O, K, E, gated)] + [4 * experts * hidden]
-    assert held <= sum(parts) + 512 * len(parts)                  # the allocator's rounding
+    assert held <= sum(parts)
     assert layer.router.shape == (experts, hidden)
 
 
