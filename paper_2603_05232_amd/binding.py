@@ -30,18 +30,22 @@ EXPORTS = ("slide_lifted_k", "slide_lifted_ld", "slide_packed_sizes", "slide_pru
            "slide_static_scratch_bytes", "slide_sparse_gemm_static",
            "mx4_row_bytes", "mx4_row_scales", "mx4_quant", "mx4_dequant", "mx4_packed_sizes", "mx4_pack", "mx4_gemm_workspace_bytes", "mx4_gemm",
            "mx4_grouped_gemm", "expert_route_workspace_bytes", "expert_route", "expert_combine",
+           "kv_page_bytes", "kv_tables_workspace_bytes", "kv_tables", "kv_write", "kv_read", "kv_attention_workspace_bytes", "kv_attention",
            "ss_status_string", "slide_format_version")
 # entry points that the extension module calls, at the addresses of the library loaded here (order of its bind())
 _CALLED = ("slide_lifted_ld", "act_lift_quant", "slide_sparse_gemm_ws", "slide_sparse_gemm_fused_ws")
 _CALLED_MX4 = ("mx4_row_bytes", "mx4_quant", "mx4_dequant", "mx4_packed_sizes", "mx4_gemm", "mx4_grouped_gemm", "expert_route_workspace_bytes", "expert_route",
                "expert_combine")                          # of its bind_mx4()
+_CALLED_KV = ("kv_page_bytes", "kv_tables_workspace_bytes", "kv_tables", "kv_write", "kv_read", "kv_attention")      # of its bind_kv()
 
 # the calls that it does
-_MODULE_CALLS = ("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused", "mx4_quant", "mx4_dequant", "mx4_product", "expert_route", "expert_combine")
+_MODULE_CALLS = ("act_lift_quant", "slide_sparse_gemm", "slide_sparse_gemm_fused", "mx4_quant", "mx4_dequant", "mx4_product", "expert_route", "expert_combine", "kv_tables", "kv_write", "kv_read",
+                 "kv_attention")
 
 _lib = None
 _calls = None
 _mx4_calls = None                                         # the module again, for the 4-bit expert layer's calls
+_kv_calls = None                                          # and for those on a cache
 
 
 class SlideSparseError(RuntimeError):
@@ -52,7 +56,7 @@ class SlideSparseError(RuntimeError):
 
 def load():
     """Load the shared library (raises if it has not been built)."""
-    global _lib, _calls, _mx4_calls
+    global _lib, _calls, _mx4_calls, _kv_calls
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -96,14 +100,21 @@ def load():
                             ("mx4_grouped_gemm", [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, i64, vp, sz, vp], i32),
                             ("expert_route_workspace_bytes", [i64, i64, i64], sz),
                             ("expert_route", [vp, i32, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp], i32),
-                            ("expert_combine", [vp, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp], i32)):
+                            ("expert_combine", [vp, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, i64, vp], i32),
+                            ("kv_page_bytes", [i64, i64, i64, i32], i64),
+                            ("kv_tables_workspace_bytes", [i64, i64], sz),
+                            ("kv_tables", [vp, vp, i64, vp, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp], i32),
+                            ("kv_write", [vp, i64, i64, vp, i64, i64, i32, i64, i64, i64, vp, vp, i64, i64, i32, vp], i32),
+                            ("kv_read", [vp, i64, i64, i32, vp, i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp], i32),
+                            ("kv_attention_workspace_bytes", [i64, i64, i64, i64], sz),
+                            ("kv_attention", [vp, i32, i64, i64, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, i64, i64, ctypes.c_float, i64, vp, i64, i64, vp, sz, vp], i32)):
         fn = getattr(lib, name)
         fn.argtypes, fn.restype = args, res
     lib.ss_status_string.argtypes = [i32]
     lib.ss_status_string.restype = ctypes.c_char_p
     lib.slide_format_version.restype = i32
     calls = _load_calls(lib)
-    _lib, _calls, _mx4_calls = lib, calls, calls
+    _lib, _calls, _mx4_calls, _kv_calls = lib, calls, calls, calls
     return lib
 
 
@@ -114,7 +125,7 @@ def _load_calls(lib):
         from . import _calls as calls
         if calls.torch_version != str(torch.__version__):
             raise ImportError(f"built for torch {calls.torch_version}, not {torch.__version__}")
-        missing = [name for name in (*_MODULE_CALLS, "bind", "bind_mx4") if not hasattr(calls, name)]
+        missing = [name for name in (*_MODULE_CALLS, "bind", "bind_mx4", "bind_kv") if not hasattr(calls, name)]
         if missing:
             raise ImportError(f"an older build, without {', '.join(missing)}")
     except (ImportError, AttributeError) as e:
@@ -122,6 +133,7 @@ def _load_calls(lib):
         return types.SimpleNamespace(**dict.fromkeys(_MODULE_CALLS, lambda *args: None))
     calls.bind(SlideSparseError, *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED))
     calls.bind_mx4(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED_MX4))
+    calls.bind_kv(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED_KV))
     return calls
 
 
@@ -539,4 +551,137 @@ def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, 
                                  0 if base is None else _row_stride(base, Y), out.data_ptr(), _row_stride(out, Y), _stream())
     if code:
         _check(code, "expert_combine")
+    return out
+
+
+# ---- a paged cache of keys and values --------------------------------------------------------------------------------------------
+
+# The stream is the current device's, so the tensors have to be there too.
+
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _here(first: torch.Tensor) -> None:
+    assert first.is_cuda and first.get_device() == _current_device()
+
+
+@functools.lru_cache(maxsize=4096, typed=True)
+def kv_page_bytes(heads: int, page: int, D: int, dtype: str) -> int:
+    return int(load().kv_page_bytes(heads, page, D, DTYPE_CODE[dtype]))
+
+
+def _kv_heads(t: torch.Tensor, first: torch.Tensor):
+    """(elements between tokens, between heads) of [N, H, D] whose heads are dense."""
+    N, H, D = t.shape
+    assert _beside(t, first) and (D < 2 or t.stride(2) == 1)
+    return t.stride(0) if N > 1 else H * D, t.stride(1) if H > 1 else D
+
+
+def _kv_pages(pages: torch.Tensor, heads: int, page: int, D: int, dtype: str, first: torch.Tensor):
+    """(address, number) of pages[P, kv_page_bytes]."""
+    n = kv_page_bytes(heads, page, D, dtype)
+    if n < 0:
+        raise SlideSparseError(3, "kv_page_bytes")
+    assert _beside(pages, first) and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.dim() == 2 and pages.shape[1] == n
+    return pages.data_ptr(), pages.shape[0]
+
+
+def kv_tables_workspace_bytes(B: int, N: int) -> int:
+    return int(load().kv_tables_workspace_bytes(B, N))
+
+
+def kv_tables(lens: torch.Tensor, want: torch.Tensor, table: torch.Tensor, pool: torch.Tensor, left: torch.Tensor, page: int, N: int, new_lens=None, new_left=None, workspace=None):
+    """Pages for B requests that go from lens[B] to want[B] tokens (int32): table[B,W] and the stack of free pages pool[0 .. left[0] - 1] are brought up to date in place
+    -> (new_lens[B], new_left[1], slots[N], offsets[B + 1]); new_lens may be lens and new_left may be left."""
+    if _kv_calls is None:
+        load()
+    done = _kv_calls.kv_tables(lens, want, table, pool, left, page, N, new_lens, new_left, workspace)
+    if done is not None:
+        return done
+    _here(lens)
+    B, W = table.shape
+    if workspace is None:
+        n = kv_tables_workspace_bytes(B, N)
+        workspace = lens.new_empty((n,), dtype=torch.uint8) if n else None
+    if new_lens is None:
+        new_lens = torch.empty_like(lens)
+    if new_left is None:
+        new_left = torch.empty_like(left)
+    assert lens.shape == want.shape == new_lens.shape == (B,) and left.shape == new_left.shape == (1,)
+    if table.dtype != torch.int32:
+        raise TypeError(f"table must be int32, got {table.dtype}")
+    slots, offsets = lens.new_empty((max(N, 0),)), lens.new_empty((B + 1,))
+    code = load().kv_tables(_dense_i32(lens, "lens", lens), _dense_i32(want, "want", lens), B, table.data_ptr(), _row_stride(table, lens), W, page, _dense_i32(pool, "pool", lens), pool.shape[0],
+                            _dense_i32(left, "left", lens), N, _dense_i32(new_lens, "new_lens", lens), _dense_i32(new_left, "new_left", lens), slots.data_ptr(), offsets.data_ptr(),
+                            *_workspace(workspace, lens), _stream())
+    if code:
+        _check(code, "kv_tables")
+    return new_lens, new_left, slots, offsets
+
+
+def kv_write(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, page: int, dtype: str):
+    """K, V [N,H,D] fp32/bf16 (strides between tokens and heads allowed) into slots[N] (int32) of pages[P, kv_page_bytes(H, page, D, dtype)] uint8."""
+    if _kv_calls is None:
+        load()
+    done = _kv_calls.kv_write(K, V, slots, pages, page, dtype)
+    if done is not None:
+        return
+    _here(K)
+    N, H, D = K.shape
+    assert V.shape == K.shape and V.dtype == K.dtype and slots.shape == (N,)
+    at, P = _kv_pages(pages, H, page, D, dtype, K)
+    code = load().kv_write(K.data_ptr(), *_kv_heads(K, K), V.data_ptr(), *_kv_heads(V, K), _in_code(K), N, H, D, _dense_i32(slots, "slots", K), at, P, page, DTYPE_CODE[dtype], _stream())
+    if code:
+        _check(code, "kv_write")
+
+
+def kv_read(pages: torch.Tensor, slots: torch.Tensor, heads: int, D: int, page: int, dtype: str, out_dtype: torch.dtype = torch.bfloat16, K=None, V=None):
+    """What pages hold of slots[N] -> (K, V) [N,heads,D] fp32 or bf16."""
+    if _kv_calls is None:
+        load()
+    done = _kv_calls.kv_read(pages, slots, heads, D, page, dtype, _IN_CODE.get(out_dtype), K, V)
+    if done is not None:
+        return done
+    _here(pages)
+    at, P = _kv_pages(pages, heads, page, D, dtype, pages)
+    N = slots.shape[0]
+    if K is None:
+        K = pages.new_empty((N, heads, D), dtype=out_dtype)
+    if V is None:
+        V = torch.empty_like(K)
+    assert K.shape == V.shape == (N, heads, D) and K.dtype == V.dtype
+    code = load().kv_read(at, P, page, DTYPE_CODE[dtype], _dense_i32(slots, "slots", pages), N, heads, D, _in_code(K), K.data_ptr(), *_kv_heads(K, pages), V.data_ptr(),
+                          *_kv_heads(V, pages), _stream())
+    if code:
+        _check(code, "kv_read")
+    return K, V
+
+
+def kv_attention_workspace_bytes(B: int, Hq: int, heads: int, D: int) -> int:
+    return int(load().kv_attention_workspace_bytes(B, Hq, heads, D))
+
+
+def kv_attention(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, heads: int, page: int, dtype: str, scale=None, window: int = 0, out=None, workspace=None):
+    """out[B,Hq,D] bf16: attention of q[B,Hq,D] (fp32/bf16), one new token of each request, over the lens[B] cached tokens (with a window, the last `window` of them) that lie in
+    the pages of table[B,W].  scale: D^-0.5 if None; workspace: optional uint8 device tensor (kv_attention_workspace_bytes) that lets long requests use the whole chip."""
+    if _kv_calls is None:
+        load()
+    done = _kv_calls.kv_attention(q, pages, table, lens, heads, page, dtype, scale, window, out, workspace)
+    if done is not None:
+        return done
+    _here(q)
+    B, Hq, D = q.shape
+    at, P = _kv_pages(pages, heads, page, D, dtype, q)
+    if table.dtype != torch.int32:
+        raise TypeError(f"table must be int32, got {table.dtype}")
+    assert table.shape[0] == B and lens.shape == (B,)
+    if out is None:
+        out = q.new_empty((B, Hq, D), dtype=torch.bfloat16)
+    assert out.shape == (B, Hq, D) and out.dtype == torch.bfloat16
+    code = load().kv_attention(q.data_ptr(), _in_code(q), *_kv_heads(q, q), at, P, page, DTYPE_CODE[dtype], table.data_ptr(), _row_stride(table, q), table.shape[1],
+                               _dense_i32(lens, "lens", q), B, Hq, heads, D, D ** -0.5 if scale is None else scale, window, out.data_ptr(), *_kv_heads(out, q),
+                               *_workspace(workspace, q), _stream())
+    if code:
+        _check(code, "kv_attention")
     return out

@@ -1,0 +1,500 @@
+// kv_attention: the attention of one new token of each request over its pages of a cache.
+//
+//   out[b, head] = sum over t of p_t v_t / sum over t of p_t,   p_t = exp(scale q . k_t - m),   t in [max(0, len - window), len)
+//
+// One pass with a running maximum and sum for each head.  A request's blocks of 32 tokens are divided over workgroups, and a workgroup's over its wavefronts; what these hold (maximum,
+// sum, weighted values) is joined in LDS, and what workgroups hold by a second kernel through the caller's workspace.
+#include "kv_common.h"
+#include "quant_common.h"
+
+namespace ss {
+
+constexpr int KA_WAVES = 4;                          // wavefronts of a workgroup
+constexpr int KA_COLUMNS = 16;                       // query heads of a product
+constexpr int KA_LEAST = 16;                         // blocks that are worth a workgroup of their own
+
+typedef uint32_t ka16_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t ka16f_t __attribute__((ext_vector_type(4), aligned(4)));
+
+// ---- how the blocks are divided ----
+// Lengths are known on the device alone, so every workgroup works the division out for itself: it is a few loads and sums over the requests, and both kernels get the same.
+struct KaDivision {
+    const int32_t* lens;
+    int B, most, window;                             // requests; tokens that a row of the table has room for; 0: no window
+    float share;                                     // over the sum of all blocks: one more than what a workgroup takes; 0: requests are not divided
+};
+struct KaSpan { int first, blocks, len, from; };     // blocks of a request that hold tokens to be seen: positions from .. len - 1
+__device__ inline KaSpan ka_span(const KaDivision& d, int b)
+{
+    KaSpan s;
+    s.len = b < d.B ? min(max(d.lens[b], 0), d.most) : 0;
+    s.from = d.window > 0 ? max(s.len - d.window, 0) : 0;
+    s.first = s.from / KV_BLOCK;
+    s.blocks = s.len > s.from ? (s.len + KV_BLOCK - 1) / KV_BLOCK - s.first : 0;
+    return s;
+}
+// blocks of a workgroup
+__device__ inline int ka_per(const KaDivision& d)
+{
+    if (d.share == 0.0f) return INT32_MAX;
+    const int lane = threadIdx.x & 63;
+    float sum = 0.0f;
+    for (int b0 = 0; b0 < d.B; b0 += 64) sum += (float)ka_span(d, b0 + lane).blocks;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);      // the same order in every wavefront of both kernels
+    return max(KA_LEAST, (int)(sum * d.share) + 1);
+}
+__device__ inline int ka_parts(int blocks, int per) { return blocks <= per ? 1 : (blocks + per - 1) / per; }
+
+// ---- types ----
+template <int DT> struct Ka;
+template <> struct Ka<SS_BF16> {
+    typedef v8bf frag;
+    __device__ static v4f mma(frag a, frag b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Ka<SS_FP16> {
+    typedef v8h frag;
+    __device__ static v4f mma(frag a, frag b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Ka<SS_I8> : Ka<SS_BF16> {};       // codes of 8 bits are exact in bf16
+template <> struct Ka<SS_FP8_E4M3> : Ka<SS_BF16> {};
+
+__device__ inline uint32_t ka_pack(float a, float b, Ka<SS_BF16>) { return pack_bf16x2(a, b); }
+__device__ inline uint32_t ka_pack(float a, float b, Ka<SS_FP16>) { return f32_to_f16_bits(a) | (uint32_t)f32_to_f16_bits(b) << 16; }
+
+// eight codes of 8 bits as bf16
+template <int DT> __device__ inline v8bf ka_widen(uint32_t lo, uint32_t hi)
+{
+    v4i r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w = h ? hi : lo;
+        float f[4];
+        if constexpr (DT == SS_FP8_E4M3) {
+            f[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0); f[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+            f[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2); f[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = (float)(int8_t)(w >> (8 * e));
+        }
+        // the upper halves: nothing is lost
+        r[2 * h] = (int)__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+        r[2 * h + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+    }
+    return __builtin_bit_cast(v8bf, r);
+}
+
+struct KaArgs {
+    const void* q; int64_t ldq, hq;
+    const uint8_t* pages; int64_t page_bytes;
+    const int32_t* table; int64_t ldt;
+    int H, G, tiles, D, page, P;                     // heads of keys, query heads to each, products that take
+    float scale;                                     // of the scores, times log2(e)
+    uint16_t* out; int64_t ldo, ho;
+    float2* sums;                                    // [item][head of keys][tile][column]: maximum, sum
+    float* parts;                                    // the same [.. , 32 NS]: weighted values
+    int items;
+    Div by_units, by_blocks;                         // H tiles; blocks of a page
+    KaDivision division;
+};
+
+// DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32)
+template <int DT, int NS, int QP>
+__global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
+{
+    constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 8 ? NT : 8;
+    typedef typename Ka<DT>::frag frag;
+    __shared__ float4 joined[KA_WAVES][CHUNK][64];
+    __shared__ float2 wave_sums[KA_WAVES][KA_COLUMNS];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int item = quot(blockIdx.x, a.by_units), unit = blockIdx.x - item * a.H * a.tiles, h = unit / a.tiles, tile = unit - h * a.tiles;
+
+    // this workgroup's request and its part of it
+    const int per = ka_per(a.division);
+    int b = -1, part = 0, parts = 0;
+    KaSpan span = {0, 0, 0, 0};
+    for (int b0 = 0, before = 0; b0 < a.division.B; b0 += 64) {
+        const KaSpan s = ka_span(a.division, b0 + lane);
+        const int n = b0 + lane < a.division.B ? ka_parts(s.blocks, per) : 0, upto = before + wave_scan_add(n);
+        const uint64_t has = __ballot(upto > item);
+        if (has) {
+            const int at = __ffsll((unsigned long long)has) - 1;
+            b = b0 + at;
+            parts = __builtin_amdgcn_readlane(n, at);
+            part = item - (__builtin_amdgcn_readlane(upto, at) - parts);
+            span = {__builtin_amdgcn_readlane(s.first, at), __builtin_amdgcn_readlane(s.blocks, at), __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.from, at)};
+            break;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (b < 0) return;
+    const int each = (span.blocks + parts - 1) / parts, lo = span.first + part * each, end = min(lo + each, span.first + span.blocks);
+
+    // the queries: lane (r, j) holds values 32 s + 8 j .. + 7 of head r
+    const int column = tile * KA_COLUMNS + r;
+    frag q[QP][NS];
+    float back = a.scale;                            // of a score
+    {
+        float f[NS][8];
+        const bool there = column < a.G;
+        const int64_t row = b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int d = 32 * s + 8 * j, have = there ? a.D - d : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
+            if constexpr (QP == 1) {
+                const uint16_t* const p = static_cast<const uint16_t*>(a.q) + row + d;
+                if (have >= 8) {
+                    const ka16_t v = *reinterpret_cast<const ka16_t*>(p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { f[s][2 * e] = __uint_as_float(v[e] << 16); f[s][2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u); }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < have) f[s][e] = bf16_bits_to_f32(p[e]);
+                }
+            } else {
+                const float* const p = static_cast<const float*>(a.q) + row + d;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < have) f[s][e] = p[e];
+            }
+        }
+        if constexpr (DT == SS_FP16) {
+            // half has 5 bits of exponent: a head's values are brought below 1 by a power of two, which its scores get back
+            float most = 0.0f;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[s][e]));
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const int x = most > 0x1p-100f && most < INFINITY ? min((int)(__float_as_uint(most) >> 23) - 126, 126) : 0;      // most < 2^x, or 4 times that
+            const float down = __uint_as_float((uint32_t)(127 - x) << 23);
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[s][e] *= down;
+            back *= __uint_as_float((uint32_t)(127 + x) << 23);
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int p = 0; p < QP; ++p) {
+                v4i w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t both = ka_pack(f[s][2 * e], f[s][2 * e + 1], Ka<DT>());
+                    w[e] = (int)both;
+                    if (p + 1 < QP) {                // what the piece left out; of an infinity nothing
+                        typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
+                        typedef half_t two_t __attribute__((ext_vector_type(2)));
+                        const two_t t = __builtin_bit_cast(two_t, both);
+#pragma unroll
+                        for (int o = 0; o < 2; ++o) {
+                            float& x = f[s][2 * e + o];
+                            x = fabsf(x) < INFINITY ? x - (float)t[o] : 0.0f;
+                        }
+                    }
+                }
+                q[p][s] = __builtin_bit_cast(frag, w);
+            }
+    }
+
+    // The probabilities of half are taken 2^14 times as large, so that the smallest ones keep their bits: all of them, the sum too.
+    constexpr float LIFT = DT == SS_FP16 ? 14.0f : 0.0f;
+    float top = -INFINITY, sum = 0.0f;               // of head r: its maximum in all j, the sum of this j's tokens
+    v4f o[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[n] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int per_page = a.page / KV_BLOCK;
+    const int32_t* const row = a.table + b * a.ldt;
+    for (int block = lo + wave; block < end; block += KA_WAVES) {
+        const int index = quot(block, a.by_blocks), id = __builtin_amdgcn_readfirstlane(row[index]);
+        if (id < 0 || id >= a.P) continue;           // no page: nothing to see
+        const uint8_t* const from = a.pages + id * a.page_bytes + (int64_t)(h * per_page + block - index * per_page) * BLOCK;
+        uint4 k[LOADS], v[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) k[i] = load_once(reinterpret_cast<const uint4*>(from + i * 1024) + lane);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) v[i] = load_once(reinterpret_cast<const uint4*>(from + HALF + i * 1024) + lane);
+        float ks[8], vs[8];
+        if constexpr (ES == 1) {
+            const float* const scales = reinterpret_cast<const float*>(from + 2 * HALF) + 8 * j;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { ks[e] = scales[e]; vs[e] = scales[KV_BLOCK + e]; }
+        }
+        // scores of tokens 8 j + 4 t + i
+        v4f s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                frag f;
+                if constexpr (ES == 2) f = __builtin_bit_cast(frag, k[2 * i + t]);
+                else f = t ? ka_widen<DT>(k[i].z, k[i].w) : ka_widen<DT>(k[i].x, k[i].y);
+#pragma unroll
+                for (int p = 0; p < QP; ++p) s[t] = Ka<DT>::mma(f, q[p][i], s[t]);
+            }
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ES == 1 ? back * ks[e] : back);
+        const int at = block * KV_BLOCK + 8 * j;
+        const bool whole = block * KV_BLOCK >= span.from && block * KV_BLOCK + KV_BLOCK <= span.len;
+        uint32_t seen = 0xFF;
+        if (!whole) {                                // what nobody wrote may be anything, a NaN too
+            seen = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool there = at + e >= span.from && at + e < span.len;
+                seen |= there ? 1u << e : 0u;
+                x[e] = there ? x[e] : -INFINITY;
+            }
+        }
+        float most = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const float top_now = fmaxf(top, most), base = top_now == -INFINITY ? 0.0f : top_now - LIFT, less = top == top_now ? 1.0f : __builtin_amdgcn_exp2f(top - top_now);
+        top = top_now;
+        float y[8], add = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { y[e] = __builtin_amdgcn_exp2f(x[e] - base); add += y[e]; }
+        sum = sum * less + add;
+        if constexpr (ES == 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = seen >> e & 1 ? y[e] * vs[e] : 0.0f;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n] *= less;
+        // The probabilities as operands.  bf16 alone would cost as much again as the rounding of the result, so what it leaves out is multiplied as well.
+        constexpr int PP = DT == SS_FP16 ? 1 : 2;
+        frag p[PP];
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+            v4i w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = (int)ka_pack(y[2 * e], y[2 * e + 1], Ka<DT>());
+                if (i + 1 < PP) {
+                    y[2 * e] -= __uint_as_float((uint32_t)w[e] << 16);
+                    y[2 * e + 1] -= __uint_as_float((uint32_t)w[e] & 0xFFFF0000u);
+                }
+            }
+            p[i] = __builtin_bit_cast(frag, w);
+        }
+        if (!whole) {                                // 0 times a NaN is none
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if constexpr (ES == 2) w[c] &= (seen >> (2 * c) & 1 ? 0xFFFFu : 0u) | (seen >> (2 * c + 1) & 1 ? 0xFFFF0000u : 0u);
+                    else {
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) m |= seen >> (4 * (c & 1) + e) & 1 ? 0xFFu << (8 * e) : 0u;
+                        w[c] &= m;
+                    }
+                }
+                v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            frag f;
+            if constexpr (ES == 2) f = __builtin_bit_cast(frag, v[n]);
+            else f = n & 1 ? ka_widen<DT>(v[n >> 1].z, v[n >> 1].w) : ka_widen<DT>(v[n >> 1].x, v[n >> 1].y);
+#pragma unroll
+            for (int i = 0; i < PP; ++i) o[n] = Ka<DT>::mma(f, p[i], o[n]);
+        }
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+
+    // the wavefronts' shares: lane (r, j) holds values 16 n + 4 j + i of head r in o[n][i]
+    if (j == 0) wave_sums[wave][r] = make_float2(top, sum);
+    __syncthreads();
+    float all_top = -INFINITY, all_sum = 0.0f, weight[KA_WAVES];
+#pragma unroll
+    for (int w = 0; w < KA_WAVES; ++w) all_top = fmaxf(all_top, wave_sums[w][r].x);
+#pragma unroll
+    for (int w = 0; w < KA_WAVES; ++w) {
+        const float2 s = wave_sums[w][r];
+        weight[w] = s.x == all_top ? 1.0f : __builtin_amdgcn_exp2f(s.x - all_top);      // both may be minus infinity
+        all_sum += s.y * weight[w];
+    }
+    const int64_t place = ((int64_t)item * a.H * a.tiles + unit) * KA_COLUMNS + r;
+    const bool there = column < a.G;
+    if (parts > 1 && wave == 0 && j == 0 && there) a.sums[place] = make_float2(all_top, all_sum);
+    // nothing seen: zeros
+    const float inverse = parts > 1 ? 1.0f : all_sum == 0.0f ? 0.0f : 1.0f / all_sum;
+#pragma unroll
+    for (int n0 = 0; n0 < NT; n0 += CHUNK) {
+        if (n0 > 0) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < CHUNK; ++n)
+            if (n0 + n < NT) joined[wave][n][lane] = make_float4(o[n0 + n][0], o[n0 + n][1], o[n0 + n][2], o[n0 + n][3]);
+        __syncthreads();
+        for (int n = wave; n < CHUNK && n0 + n < NT; n += KA_WAVES) {
+            v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < KA_WAVES; ++w) {
+                const float4 x = joined[w][n][lane];
+                v += v4f{x.x, x.y, x.z, x.w} * weight[w];
+            }
+            const int d = 16 * (n0 + n) + 4 * j;
+            if (!there) continue;
+            if (parts > 1) *reinterpret_cast<float4*>(a.parts + place * (32 * NS) + d) = make_float4(v[0], v[1], v[2], v[3]);
+            else if (d < a.D) {
+                uint16_t* const to = a.out + b * a.ldo + (int64_t)(h * a.G + column) * a.ho + d;
+                const uint32_t w0 = pack_bf16x2(v[0] * inverse, v[1] * inverse), w1 = pack_bf16x2(v[2] * inverse, v[3] * inverse);
+                if (d + 4 <= a.D) *reinterpret_cast<ka8_t*>(to) = ka8_t{w0, w1};
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (d + i < a.D) to[i] = (uint16_t)((i & 2 ? w1 : w0) >> (16 * (i & 1)));
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of a request that was divided: a workgroup for each query head of each request, which leaves where it was not.
+template <int NS>
+__global__ __launch_bounds__(256) void k_kv_join(const KaArgs a)
+{
+    constexpr int WIDTH = 32 * NS;
+    __shared__ float acc[4][WIDTH];
+    __shared__ float wave_sum[4], wave_top[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int heads = a.H * a.G, b = blockIdx.x / heads, head = blockIdx.x - b * heads, h = head / a.G, column = head - h * a.G;
+    const int per = ka_per(a.division);
+    int item = 0, parts = 0;
+    for (int b0 = 0; b0 <= b; b0 += 64) {
+        const int n = b0 + lane <= b ? ka_parts(ka_span(a.division, b0 + lane).blocks, per) : 0, upto = wave_scan_add(n);
+        if (b < b0 + 64) {
+            parts = __builtin_amdgcn_readlane(n, b - b0);
+            item += __builtin_amdgcn_readlane(upto, b - b0) - parts;
+        } else item += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (parts < 2) return;
+    const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = item * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
+    float top = -INFINITY;
+    for (int i = wave * 64 + lane; i < parts; i += 256) top = fmaxf(top, a.sums[first + i * step].x);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (lane == 0) wave_top[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+    constexpr int PER = (WIDTH + 63) / 64;
+    float v[PER], sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) v[c] = 0.0f;
+    for (int i = wave; i < parts; i += 4) {
+        const float2 s = a.sums[first + i * step];
+        const float weight = s.x == top ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
+        sum += s.y * weight;
+        const float* const p = a.parts + (first + i * step) * WIDTH;
+#pragma unroll
+        for (int c = 0; c < PER; ++c)
+            if (64 * c + lane < WIDTH) v[c] += p[64 * c + lane] * weight;
+    }
+#pragma unroll
+    for (int c = 0; c < PER; ++c)
+        if (64 * c + lane < WIDTH) acc[wave][64 * c + lane] = v[c];
+    if (lane == 0) wave_sum[wave] = sum;
+    __syncthreads();
+    sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int d = threadIdx.x; d < a.D; d += 256) {
+        const float x = ((acc[0][d] + acc[1][d]) + (acc[2][d] + acc[3][d])) * inverse;
+        a.out[b * a.ldo + head * a.ho + d] = (uint16_t)pack_bf16x2(x, 0.0f);
+    }
+}
+
+template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool fp32, bool join, int64_t groups, int64_t rows, hipStream_t hs)
+{
+    if (fp32) hipLaunchKernelGGL((k_kv_attend<DT, NS, 2>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
+    else hipLaunchKernelGGL((k_kv_attend<DT, NS, 1>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
+    if (!join) return launch_status();
+    if (launch_status() != SS_OK) return SS_ERR_HIP;
+    hipLaunchKernelGGL(k_kv_join<NS>, dim3((uint32_t)rows), dim3(256), 0, hs, a);
+    return launch_status();
+}
+
+// Workgroups that all heads' parts come to, about.
+static int64_t wanted_groups() { return 4 * (int64_t)cu_count(); }
+// bytes of a part of a request: sums and values of all heads
+static int64_t part_bytes(int64_t units, int64_t D) { return units * KA_COLUMNS * (8 + 4 * 32 * kv_steps(D)); }
+
+}  // namespace ss
+
+using namespace ss;
+
+static bool valid_attention(int64_t B, int64_t Hq, int64_t H, int64_t D)
+{
+    return B >= 0 && B <= KV_MAX_REQUESTS && H >= 1 && H <= KV_MAX_HEADS && Hq >= H && Hq <= KV_MAX_HEADS && Hq % H == 0 && D >= 1 && D <= KV_MAX_D;
+}
+
+extern "C" size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H, int64_t D)
+{
+    if (!valid_attention(B, Hq, H, D) || B == 0) return 0;
+    const int64_t units = H * ((Hq / H + KA_COLUMNS - 1) / KA_COLUMNS);
+    return (size_t)((wanted_groups() / units + 2 + B) * part_bytes(units, D));
+}
+
+extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* table,
+                                  int64_t ldt, int64_t W, const int32_t* lens, int64_t B, int64_t Hq, int64_t H, int64_t D, float scale, int64_t window, void* out, int64_t ldo,
+                                  int64_t ho, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if ((in_dtype != SS_IN_F32 && in_dtype != SS_IN_BF16) || !valid_dtype(dtype)) return SS_ERR_DTYPE;
+    constexpr int64_t FAR = (int64_t)1 << 40;
+    if (!valid_attention(B, Hq, H, D) || !kv_valid_page(H, page, D, dtype) || !kv_valid_slots(P, page) || W < 1 || W > INT32_MAX / page - 1 || ldt < W || window < 0 || !(scale - scale == 0.0f) ||
+        ldq < 0 || ldq > FAR || hq < 0 || hq > FAR || ldo < 0 || ldo > FAR || ho < 0 || ho > FAR || ldt > FAR)
+        return SS_ERR_SHAPE;
+    if (B == 0) return SS_OK;
+    if (!Q || !pages || !table || !lens || !out || (!workspace && workspace_bytes > 0)) return SS_ERR_NULL;
+    if (((uintptr_t)Q & (in_dtype == SS_IN_F32 ? 3 : 1)) || ((uintptr_t)out & 1) || (((uintptr_t)table | (uintptr_t)lens) & 3) || ((uintptr_t)pages & 15)) return SS_ERR_SHAPE;
+    if ((uintptr_t)workspace & 15) return SS_ERR_WORKSPACE;
+    const int ns = kv_steps(D);
+    KaArgs a = {};
+    a.q = Q; a.ldq = ldq; a.hq = hq;
+    a.pages = static_cast<const uint8_t*>(pages);
+    a.page_bytes = kv_bytes_of_page(H, page, D, dtype);
+    a.table = table; a.ldt = ldt;
+    a.H = (int)H; a.G = (int)(Hq / H); a.tiles = (a.G + KA_COLUMNS - 1) / KA_COLUMNS; a.D = (int)D; a.page = (int)page; a.P = (int)P;
+    a.scale = scale * 1.44269504088896340736f;
+    a.out = static_cast<uint16_t*>(out); a.ldo = ldo; a.ho = ho;
+    const int64_t units = H * a.tiles;
+    // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.
+    const int64_t room = (int64_t)(workspace_bytes / (size_t)part_bytes(units, D)) - B - 2, want = wanted_groups() / units, wanted = room < want ? room : want;
+    const bool join = wanted > 0 && W * page > (int64_t)KA_LEAST * KV_BLOCK;
+    a.division = {lens, (int)B, (int)(W * page), (int)(window < INT32_MAX ? window : 0), join ? 1.0f / (float)wanted : 0.0f};
+    a.items = (int)(join ? wanted + 2 + B : B);
+    a.sums = static_cast<float2*>(workspace);
+    a.parts = join ? reinterpret_cast<float*>(a.sums + a.items * units * KA_COLUMNS) : nullptr;
+    a.by_units = make_div(units);
+    a.by_blocks = make_div(page / KV_BLOCK);
+    const int64_t groups = a.items * units, rows = B * Hq;
+    if (!mx4_grid_fits(groups, 64 * KA_WAVES) || !mx4_grid_fits(rows, 256)) return SS_ERR_SHAPE;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    const bool fp32 = in_dtype == SS_IN_F32;
+#define SS_KA(DT)                                                                     \
+    switch (ns) {                                                                     \
+    case 1: return launch_attend<DT, 1>(a, fp32, join, groups, rows, hs);             \
+    case 2: return launch_attend<DT, 2>(a, fp32, join, groups, rows, hs);             \
+    case 3: return launch_attend<DT, 3>(a, fp32, join, groups, rows, hs);             \
+    case 4: return launch_attend<DT, 4>(a, fp32, join, groups, rows, hs);             \
+    case 6: return launch_attend<DT, 6>(a, fp32, join, groups, rows, hs);             \
+    default: return launch_attend<DT, 8>(a, fp32, join, groups, rows, hs);            \
+    }
+    switch (dtype) {
+    case SS_I8: SS_KA(SS_I8)
+    case SS_FP8_E4M3: SS_KA(SS_FP8_E4M3)
+    case SS_BF16: SS_KA(SS_BF16)
+    default: SS_KA(SS_FP16)
+    }
+#undef SS_KA
+}

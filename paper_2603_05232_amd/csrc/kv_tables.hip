@@ -1,0 +1,173 @@
+// kv_tables: the pages of requests whose lengths change, and the slots of their new tokens, without a trip to the host.
+#include "kv_common.h"
+
+namespace ss {
+
+constexpr int KT_THREADS = 1024;
+constexpr int KT_CAP = 1 << 30;                      // sums stop here, above any number that means something
+constexpr int64_t KT_ONE_LAUNCH = 8192;              // new tokens up to which the plan's workgroup fills in the slots too
+
+__device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
+
+// inclusive sum over the workgroup's threads (values >= 0); total: that of all
+__device__ inline int block_scan(int v, int* part, int& total)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int sum = min(v, KT_CAP);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(sum, d, 64);
+        if (lane >= d) sum = cap_add(sum, other);
+    }
+    __syncthreads();                                 // part is free again
+    if (lane == 63) part[wave] = sum;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < KT_THREADS / 64; ++w) {
+        if (w < wave) before = cap_add(before, part[w]);
+        total = cap_add(total, part[w]);
+    }
+    return cap_add(before, sum);
+}
+
+// What filling in needs of each request.
+struct KtPlan {
+    int32_t start[KV_MAX_REQUESTS + 1];              // its first new token's row
+    int32_t len[KV_MAX_REQUESTS];                    // its length before
+    int32_t first[KV_MAX_REQUESTS];                  // pages taken by requests before it; -1: it gets no slots
+    int32_t pages;                                   // free pages, those that were given back among them
+};
+
+// Row i: the request that it belongs to, its position there, its page.  A new page is entered in the table by the row that begins it.
+__device__ inline void kt_fill(const KtPlan& plan, int i, int B, int32_t* __restrict__ table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P,
+                               int32_t* __restrict__ slots)
+{
+    if (i >= plan.start[B]) { slots[i] = -1; return; }
+    int lo = 0, hi = B;                              // the last request that begins at or before i
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (plan.start[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    const int first = plan.first[lo];
+    if (first < 0) { slots[i] = -1; return; }
+    const int len = plan.len[lo], at = len + (i - plan.start[lo]), column = quot(at, by_page), row = at - column * page, have = quot(len + page - 1, by_page);
+    int32_t* const cell = table + lo * ldt + column;
+    int id;
+    if (column >= have) {
+        const int k = plan.pages - 1 - (first + column - have);      // from the top of the stack
+        id = k >= 0 && k < P ? pool[k] : -1;
+        if (row == 0) *cell = id;
+    } else id = *cell;
+    slots[i] = id >= 0 && id < P ? id * page + row : -1;
+}
+
+// One workgroup.  The requests' numbers are few; bound by the launch and its waits.  Every input is read before the barrier behind which outputs are written, so new_lens may be
+// lens and new_left may be left.
+template <bool WHOLE>
+__global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, const int32_t* want, int B, int32_t* table, int64_t ldt, int W, int page, Div by_page, int32_t* pool, int P,
+                                                        const int32_t* left, int N, int32_t* new_lens, int32_t* new_left, int32_t* __restrict__ slots,
+                                                        int32_t* __restrict__ offsets, KtPlan* __restrict__ out)
+{
+    __shared__ KtPlan plan;
+    __shared__ int part[KT_THREADS / 64];
+    __shared__ int taken;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, most = W * page;
+    const int free_before = min(max(*left, 0), P);
+    if (threadIdx.x == 0) taken = 0;
+    int rows = 0, pages = 0, back = 0;               // sums of the requests before
+    constexpr int PER = (int)KV_MAX_REQUESTS / KT_THREADS;
+    int wanted[PER], upto[PER];                      // the thread's requests: length wanted (-1: not possible); pages that are taken up to this one, if it takes any
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int b0 = q * KT_THREADS, b = b0 + threadIdx.x;
+        wanted[q] = upto[q] = 0;
+        if (b0 >= B) continue;                       // the same for all threads
+        const int l = b < B ? min(max(lens[b], 0), most) : 0, w = b < B ? max(want[b], 0) : 0;
+        const int have = quot(l + page - 1, by_page), need = quot(min(w, most) + page - 1, by_page);
+        int all;
+        const int grow = max(w - l, 0), end = block_scan(min(grow, N + 1), part, all), end_all = cap_add(rows, end);
+        rows = cap_add(rows, all);
+        const bool possible = w <= most && end_all <= N;
+        const int more = possible ? max(need - have, 0) : 0;
+        const int up = cap_add(pages, block_scan(more, part, all));
+        pages = cap_add(pages, all);
+        const int fewer = w < l ? have - need : 0, given = cap_add(back, block_scan(fewer, part, all));
+        back = cap_add(back, all);
+        if (b < B) {
+            plan.start[b] = min(end_all - min(grow, N + 1), N);
+            plan.len[b] = l;
+            plan.first[b] = up - more;
+        }
+        upto[q] = more > 0 ? up : 0;
+        wanted[q] = possible || w <= l ? w : -1;
+        // pages given back, a wavefront for each request that has any
+        for (uint64_t has = __ballot(fewer > 0); has; has &= has - 1) {
+            const int at = __ffsll((unsigned long long)has) - 1, n = __builtin_amdgcn_readlane(fewer, at), to = free_before + __builtin_amdgcn_readlane(given - fewer, at);
+            const int32_t* const from = table + (int64_t)(b0 + wave * 64 + at) * ldt + __builtin_amdgcn_readlane(need, at);
+            for (int i = lane; i < n; i += 64)
+                if (to + i < P) pool[to + i] = from[i];
+        }
+    }
+    const int all_pages = min(cap_add(free_before, back), P);
+    if (threadIdx.x == 0) { plan.start[B] = min(rows, N); plan.pages = all_pages; }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int b = q * KT_THREADS + threadIdx.x;
+        if (b >= B) continue;
+        const bool served = wanted[q] >= 0 && upto[q] <= all_pages;
+        if (!served) plan.first[b] = -1;
+        else if (upto[q] > 0) atomicMax(&taken, upto[q]);            // whole numbers: the order does not matter
+        new_lens[b] = served ? wanted[q] : plan.len[b];
+        offsets[b] = plan.start[b];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) { offsets[B] = plan.start[B]; *new_left = all_pages - taken; }
+    if constexpr (WHOLE) {
+        for (int i = threadIdx.x; i < N; i += KT_THREADS) kt_fill(plan, i, B, table, ldt, page, by_page, pool, P, slots);
+    } else {
+        for (int b = threadIdx.x; b <= B; b += KT_THREADS) out->start[b] = plan.start[b];
+        for (int b = threadIdx.x; b < B; b += KT_THREADS) { out->len[b] = plan.len[b]; out->first[b] = plan.first[b]; }
+        if (threadIdx.x == 0) out->pages = plan.pages;
+    }
+}
+
+__global__ __launch_bounds__(256) void k_kv_slots(const KtPlan* __restrict__ plan, int B, int32_t* table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P, int N,
+                                                  int32_t* __restrict__ slots)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < N) kt_fill(*plan, i, B, table, ldt, page, by_page, pool, P, slots);
+}
+
+}  // namespace ss
+
+using namespace ss;
+
+static bool valid_tables(int64_t B, int64_t N) { return B >= 0 && B <= KV_MAX_REQUESTS && N >= 0 && N <= KV_MAX_TOKENS; }
+
+extern "C" size_t kv_tables_workspace_bytes(int64_t B, int64_t N) { return valid_tables(B, N) && N > KT_ONE_LAUNCH ? sizeof(KtPlan) : 0; }
+
+extern "C" ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t B, int32_t* table, int64_t ldt, int64_t W, int64_t page, int32_t* pool, int64_t P, const int32_t* left,
+                               int64_t N, int32_t* new_lens, int32_t* new_left, int32_t* slots, int32_t* offsets, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!valid_tables(B, N) || page < KV_BLOCK || page > 4096 || page % KV_BLOCK || !kv_valid_slots(P, page) || W < 1 || W > INT32_MAX / page - 1 || ldt < W) return SS_ERR_SHAPE;
+    if ((B > 0 && (!lens || !want || !table || !new_lens)) || !pool || !left || !new_left || !offsets || (N > 0 && !slots)) return SS_ERR_NULL;
+    if (((uintptr_t)lens | (uintptr_t)want | (uintptr_t)table | (uintptr_t)pool | (uintptr_t)left | (uintptr_t)new_lens | (uintptr_t)new_left | (uintptr_t)slots | (uintptr_t)offsets) & 3) return SS_ERR_SHAPE;
+    const size_t need = kv_tables_workspace_bytes(B, N);
+    if (need > 0 && !workspace) return SS_ERR_NULL;
+    if (((uintptr_t)workspace & 15) || workspace_bytes < need) return SS_ERR_WORKSPACE;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    const Div by_page = make_div(page);
+    KtPlan* const plan = static_cast<KtPlan*>(workspace);
+    auto args = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(1), dim3(KT_THREADS), 0, hs, lens, want, (int)B, table, ldt, (int)W, (int)page, by_page, pool, (int)P, left, (int)N, new_lens, new_left, slots, offsets, plan);
+        return launch_status();
+    };
+    if (need == 0) return args(k_kv_plan<true>);
+    if (args(k_kv_plan<false>) != SS_OK) return SS_ERR_HIP;
+    hipLaunchKernelGGL(k_kv_slots, dim3((uint32_t)((N + 255) / 256)), dim3(256), 0, hs, plan, (int)B, table, ldt, (int)page, by_page, pool, (int)P, (int)N, slots);
+    return launch_status();
+}

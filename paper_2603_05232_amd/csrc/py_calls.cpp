@@ -1,4 +1,4 @@
-// The calls of a model's forward pass (quantisation, sparse GEMMs, the 4-bit expert layer) as CPython functions: argument reading, output
+// The calls of a model's forward pass (quantisation, sparse GEMMs, the 4-bit expert layer, a cache's operators) as CPython functions: argument reading, output
 // allocation and the C call without going through ctypes and torch's Python layer.  Layers of few tokens are bound by the time
 // between launches, most of which was spent there (quantisation + GEMM of 16 x 512 x 512: see binding.py).
 //
@@ -19,6 +19,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <limits.h>
+#include <math.h>
 #include <string.h>
 #include "slidesparse.h"
 
@@ -395,6 +396,173 @@ PyObject* py_bind_mx4(PyObject*, PyObject* args)
     Py_RETURN_NONE;
 }
 
+// ---- a paged cache of keys and values ----
+struct Kv {
+    decltype(&::kv_page_bytes) page_bytes;
+    decltype(&::kv_tables_workspace_bytes) tables_workspace;
+    decltype(&::kv_tables) tables;
+    decltype(&::kv_write) write;
+    decltype(&::kv_read) read;
+    decltype(&::kv_attention) attention;
+} kv;                                                 // zeros until bind_kv()
+
+// [N, H, D] whose heads are dense, and the elements between its tokens and heads
+bool head_rows(const at::Tensor& t, const at::Tensor& first) { return beside(t, first) && t.dim() == 3 && (t.size(2) < 2 || t.stride(2) == 1); }
+int64_t token_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
+int64_t head_stride(const at::Tensor& t) { return t.size(1) > 1 ? t.stride(1) : t.size(2); }
+bool list_of(const at::Tensor& t, int64_t n, const at::Tensor& first) { return dense(t, at::kInt, first) && t.dim() == 1 && t.size(0) == n; }
+bool cache_pages(const at::Tensor& t, int64_t H, int64_t page, int64_t D, ss_dtype dtype, const at::Tensor& first)
+{
+    return dense(t, at::kByte, first) && t.dim() == 2 && t.size(1) == kv.page_bytes(H, page, D, dtype);
+}
+// the stream is the current device's, so the tensors have to be there too
+bool here(const at::Tensor& first) { return first.is_cuda() && first.get_device() == c10::hip::current_device(); }
+int32_t* ints(const at::Tensor& t) { return static_cast<int32_t*>(t.data_ptr()); }
+
+// kv_tables(lens, want, table, pool, left, page, N, new_lens, new_left, workspace)
+PyObject* py_kv_tables(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t page, N;
+    if (!kv.tables || n != 10 || !plain(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain(a[3]) || !plain(a[4]) || !integer(a[5], 1, INT_MAX, page) || !integer(a[6], 0, 1 << 20, N) ||
+        !plain_or_none(a[7]) || !plain_or_none(a[8]) || !plain_or_none(a[9]) || modes_active())
+        Py_RETURN_NONE;
+    const at::Tensor &lens = THPVariable_Unpack(a[0]), &want = THPVariable_Unpack(a[1]), &table = THPVariable_Unpack(a[2]), &pool = THPVariable_Unpack(a[3]), &left = THPVariable_Unpack(a[4]);
+    if (!here(lens) || !matrix(table, lens) || table.scalar_type() != at::kInt || !dense(pool, at::kInt, lens) || pool.dim() != 1 || !workspace(a[9], lens)) Py_RETURN_NONE;
+    const int64_t B = table.size(0), W = table.size(1);
+    if (!list_of(lens, B, lens) || !list_of(want, B, lens) || !list_of(left, 1, lens) || (a[7] != Py_None && !list_of(THPVariable_Unpack(a[7]), B, lens)) ||
+        (a[8] != Py_None && !list_of(THPVariable_Unpack(a[8]), 1, lens)))
+        Py_RETURN_NONE;
+    at::Tensor new_lens, new_left, slots, offsets, scratch;
+    ss_status st;
+    {
+        Unlocked u;
+        // one allocation for the results; none is handed out that the caller gave
+        const bool own_lens = a[7] == Py_None, own_left = a[8] == Py_None;
+        const at::Tensor all = at::empty({N + B + 1 + (own_lens ? B : 0) + (own_left ? 1 : 0)}, lens.options());
+        slots = part(all, 0, {N}, at::kInt);
+        offsets = part(all, N, {B + 1}, at::kInt);
+        if (own_lens) new_lens = part(all, N + B + 1, {B}, at::kInt);
+        if (own_left) new_left = part(all, N + B + 1 + (own_lens ? B : 0), {1}, at::kInt);
+        void* ws = address(a[9]);
+        size_t ws_bytes = a[9] == Py_None ? 0 : THPVariable_Unpack(a[9]).nbytes();
+        if (a[9] == Py_None && (ws_bytes = kv.tables_workspace(B, N)) > 0) { scratch = at::empty({(int64_t)ws_bytes}, lens.options().dtype(at::kByte)); ws = scratch.data_ptr(); }
+        st = kv.tables(ints(lens), ints(want), B, ints(table), row_stride(table), W, page, ints(pool), pool.size(0), ints(left), N, own_lens ? ints(new_lens) : static_cast<int32_t*>(address(a[7])),
+                       own_left ? ints(new_left) : static_cast<int32_t*>(address(a[8])), ints(slots), ints(offsets), ws, ws_bytes, current_stream());
+    }
+    if (st != SS_OK) return refused(st, "kv_tables");
+    PyObject* r = PyTuple_New(4);
+    if (!r) return nullptr;
+    PyObject* const all[4] = {wrap(new_lens, a[7]), wrap(new_left, a[8]), THPVariable_Wrap(std::move(slots)), THPVariable_Wrap(std::move(offsets))};
+    bool whole = true;
+    for (int i = 0; i < 4; ++i) {
+        whole = whole && all[i];
+        if (all[i]) PyTuple_SET_ITEM(r, i, all[i]);
+    }
+    if (!whole) Py_CLEAR(r);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_write(K, V, slots, pages, page, dtype): True where it was done
+PyObject* py_kv_write(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t page;
+    Type t;
+    if (!kv.write || n != 6 || !plain(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain(a[3]) || !integer(a[4], 1, INT_MAX, page) || !operand_type(a[5], t) || modes_active()) Py_RETURN_NONE;
+    const at::Tensor &K = THPVariable_Unpack(a[0]), &V = THPVariable_Unpack(a[1]), &slots = THPVariable_Unpack(a[2]), &pages = THPVariable_Unpack(a[3]);
+    if (!here(K) || !head_rows(K, K) || !head_rows(V, K) || !float_or_bf16(K) || V.scalar_type() != K.scalar_type() || V.sizes() != K.sizes() || !list_of(slots, K.size(0), K) ||
+        !cache_pages(pages, K.size(1), page, K.size(2), t.code, K))
+        Py_RETURN_NONE;
+    ss_status st;
+    {
+        Unlocked u;
+        st = kv.write(K.data_ptr(), token_stride(K), head_stride(K), V.data_ptr(), token_stride(V), head_stride(V), in_code(K), K.size(0), K.size(1), K.size(2), ints(slots), pages.data_ptr(),
+                      pages.size(0), page, t.code, current_stream());
+    }
+    if (st != SS_OK) return refused(st, "kv_write");
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_read(pages, slots, heads, D, page, dtype, fp32 or bf16 as ss_act_dtype, K, V)
+PyObject* py_kv_read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t H, D, page, type;
+    Type t;
+    if (!kv.read || n != 9 || !plain(a[0]) || !plain(a[1]) || !integer(a[2], 1, INT_MAX, H) || !integer(a[3], 1, INT_MAX, D) || !integer(a[4], 1, INT_MAX, page) || !operand_type(a[5], t) ||
+        !integer(a[6], 0, 1, type) || !plain_or_none(a[7]) || !plain_or_none(a[8]) || modes_active())
+        Py_RETURN_NONE;
+    const at::Tensor &pages = THPVariable_Unpack(a[0]), &slots = THPVariable_Unpack(a[1]);
+    if (!here(pages) || !cache_pages(pages, H, page, D, t.code, pages) || slots.dim() != 1 || !dense(slots, at::kInt, pages)) Py_RETURN_NONE;
+    const int64_t N = slots.size(0);
+    at::Tensor K, V;
+    ss_status st;
+    {
+        Unlocked u;
+        const auto out = pages.options().dtype(type == SS_IN_F32 ? at::kFloat : at::kBFloat16);
+        if (a[7] == Py_None) K = at::empty({N, H, D}, out);
+        if (a[8] == Py_None) V = at::empty({N, H, D}, a[7] == Py_None ? out : THPVariable_Unpack(a[7]).options());
+        const at::Tensor &k = K.defined() ? K : THPVariable_Unpack(a[7]), &v = V.defined() ? V : THPVariable_Unpack(a[8]);
+        st = head_rows(k, pages) && head_rows(v, pages) && float_or_bf16(k) && v.scalar_type() == k.scalar_type() && k.size(0) == N && k.size(1) == H && k.size(2) == D && v.sizes() == k.sizes()
+                 ? kv.read(pages.data_ptr(), pages.size(0), page, t.code, ints(slots), N, H, D, in_code(k), k.data_ptr(), token_stride(k), head_stride(k), v.data_ptr(), token_stride(v), head_stride(v),
+                           current_stream())
+                 : SS_ERR_SHAPE;
+    }
+    if (st != SS_OK) return refused(st, "kv_read");
+    PyObject *pk = wrap(K, a[7]), *pv = wrap(V, a[8]);
+    PyObject* r = pk && pv ? PyTuple_Pack(2, pk, pv) : nullptr;
+    Py_XDECREF(pk);
+    Py_XDECREF(pv);
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_attention(q, pages, table, lens, heads, page, dtype, scale, window, out, workspace)
+PyObject* py_kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    int64_t H, page, window;
+    Type t;
+    if (!kv.attention || n != 11 || !plain(a[0]) || !plain(a[1]) || !plain(a[2]) || !plain(a[3]) || !integer(a[4], 1, INT_MAX, H) || !integer(a[5], 1, INT_MAX, page) || !operand_type(a[6], t) ||
+        (a[7] != Py_None && !PyFloat_CheckExact(a[7])) || !integer(a[8], 0, INT64_MAX, window) || !plain_or_none(a[9]) || !plain_or_none(a[10]) || modes_active())
+        Py_RETURN_NONE;
+    const at::Tensor &q = THPVariable_Unpack(a[0]), &pages = THPVariable_Unpack(a[1]), &table = THPVariable_Unpack(a[2]), &lens = THPVariable_Unpack(a[3]);
+    if (!here(q) || !head_rows(q, q) || !float_or_bf16(q) || !matrix(table, q) || table.scalar_type() != at::kInt || table.size(0) != q.size(0) || !list_of(lens, q.size(0), q) ||
+        !cache_pages(pages, H, page, q.size(2), t.code, q) || !workspace(a[10], q))
+        Py_RETURN_NONE;
+    const int64_t B = q.size(0), Hq = q.size(1), D = q.size(2);
+    const float scale = (float)(a[7] == Py_None ? 1.0 / sqrt((double)D) : PyFloat_AS_DOUBLE(a[7]));
+    void* const ws = address(a[10]);
+    const size_t ws_bytes = a[10] == Py_None ? 0 : THPVariable_Unpack(a[10]).nbytes();
+    at::Tensor made;
+    ss_status st;
+    {
+        Unlocked u;
+        if (a[9] == Py_None) made = at::empty({B, Hq, D}, q.options().dtype(at::kBFloat16));
+        const at::Tensor& y = made.defined() ? made : THPVariable_Unpack(a[9]);
+        st = head_rows(y, q) && y.scalar_type() == at::kBFloat16 && y.sizes() == q.sizes()
+                 ? kv.attention(q.data_ptr(), in_code(q), token_stride(q), head_stride(q), pages.data_ptr(), pages.size(0), page, t.code, ints(table), row_stride(table), table.size(1), ints(lens), B, Hq, H,
+                                D, scale, window, y.data_ptr(), token_stride(y), head_stride(y), ws, ws_bytes, current_stream())
+                 : SS_ERR_SHAPE;
+    }
+    if (st != SS_OK) return refused(st, "kv_attention");
+    return wrap(made, a[9]);
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_kv(the addresses of Kv's functions in their order), behind bind()
+PyObject* py_bind_kv(PyObject*, PyObject* args)
+{
+    unsigned long long f[6];
+    if (!PyArg_ParseTuple(args, "KKKKKK", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5])) return nullptr;
+    kv = {reinterpret_cast<decltype(kv.page_bytes)>(f[0]), reinterpret_cast<decltype(kv.tables_workspace)>(f[1]), reinterpret_cast<decltype(kv.tables)>(f[2]),
+          reinterpret_cast<decltype(kv.write)>(f[3]), reinterpret_cast<decltype(kv.read)>(f[4]), reinterpret_cast<decltype(kv.attention)>(f[5])};
+    Py_RETURN_NONE;
+}
+
 // bind(SlideSparseError, slide_lifted_ld, act_lift_quant, slide_sparse_gemm_ws, slide_sparse_gemm_fused_ws), the last four as
 // addresses; library() tells these
 PyObject* py_bind(PyObject*, PyObject* args)
@@ -424,6 +592,11 @@ PyMethodDef methods[] = {{"act_lift_quant", SS_PY(py_act_lift_quant), nullptr},
                          {"mx4_product", SS_PY(py_mx4_product), nullptr},
                          {"expert_route", SS_PY(py_expert_route), nullptr},
                          {"expert_combine", SS_PY(py_expert_combine), nullptr},
+                         {"kv_tables", SS_PY(py_kv_tables), nullptr},
+                         {"kv_write", SS_PY(py_kv_write), nullptr},
+                         {"kv_read", SS_PY(py_kv_read), nullptr},
+                         {"kv_attention", SS_PY(py_kv_attention), nullptr},
+                         {"bind_kv", py_bind_kv, METH_VARARGS, nullptr},
                          {"bind_mx4", py_bind_mx4, METH_VARARGS, nullptr},
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {"library", py_library, METH_NOARGS, nullptr},
