@@ -277,8 +277,8 @@ ss_status expert_combine(const void* Y, int64_t R, int64_t O, int64_t ldy, const
  * Pages.  A page holds `page` tokens (a multiple of 32, up to 4096) of H heads (1 .. 1024) of D values (1 .. 256) each, keys and values, kv_page_bytes() bytes in a layout of
  * this library (ordered for the matrix instruction's operands; written by kv_write, read back by kv_read).  `pages` is P of them one after the other, 16-byte aligned.  Slot id * page + r is row
  * r of page id; P page < 2^31.  table[B,W] (int32, row stride ldt) names the pages of each request in order: column i holds the page of its tokens i page .. i page + page - 1.
- * dtype is what the cache holds: SS_BF16 and SS_FP16 keep values rounded to nearest even; SS_I8 and SS_FP8_E4M3 keep, of each token and head, codes clamp(rne(x * (Qmax / a))) with
- * a = max|x| and Qmax = 127 or 448, and a scale a / Qmax (a below 2^-100: scale 1, codes 0; an infinity or a NaN among the values: a scale that is a NaN).
+ * dtype is what the cache holds: SS_BF16 and SS_FP16 keep values rounded to nearest even; SS_I8 and SS_FP8_E4M3 keep, of each token and head, codes clamp(rne(x r)) with
+ * a = max|x|, Qmax = 127 or 448 and r = Qmax * (1 / a) in fp32, and a scale a / Qmax (a below 2^-100: scale 1, codes 0; an infinity or a NaN among the values: a scale that is a NaN).
  * Limits: B <= 4096 requests, N <= 2^20 rows of new tokens a call, and the threads of a launch in 32 bits as above.  Nothing in the device arrays (lengths, tables, slots, lists) can lead a kernel out
  * of bounds: what each call does with an entry that means nothing is said there. */
 int64_t kv_page_bytes(int64_t H, int64_t page, int64_t D, ss_dtype dtype);      /* -1 on a bad argument */

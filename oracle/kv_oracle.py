@@ -75,7 +75,7 @@ def held(x, dtype):
         a = np.abs(x).max(-1, keepdims=True)
         bad, none = ~np.isfinite(a), a < np.float32(2.0 ** -100)
         a = np.where(bad | none, np.float32(1), a)
-        y = np.clip(x * (q / a), -q, q)
+        y = np.clip(x * (q * (np.float32(1) / a)), -q, q)
         codes = np.rint(y) if dtype == "i8" else e4m3(y)
         codes = np.where(bad | none, 0, codes).astype(np.float32)
         scale = np.where(bad, np.float32(np.nan), np.where(none, np.float32(1), a / q))

@@ -11,18 +11,19 @@ namespace ss {
 
 constexpr int KA_WAVES = 4;                          // wavefronts of a workgroup
 constexpr int KA_COLUMNS = 16;                       // query heads of a product
-constexpr int KA_LEAST = 16;                         // blocks that are worth a workgroup of their own
+constexpr int KA_ONE = 16;                           // blocks of a row of the table up to which requests are not divided
+constexpr int KA_LEAST = 4;                         // blocks that are worth a workgroup of their own
 
 typedef uint32_t ka16_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t ka16f_t __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- how the blocks are divided ----
-// Lengths are known on the device alone, so every workgroup works the division out for itself: it is a few loads and sums over the requests, and both kernels get the same.
+// Lengths are known on the device alone, so every workgroup works the division out for itself: a few loads and sums over the requests.
 struct KaDivision {
     const int32_t* lens;
     int B, most, window;                             // requests; tokens that a row of the table has room for; 0: no window
-    float share;                                     // over the sum of all blocks: one more than what a workgroup takes; 0: requests are not divided
+    float share;                                     // times the sum of all blocks: one less than what a workgroup takes
 };
 struct KaSpan { int first, blocks, len, from; };     // blocks of a request that hold tokens to be seen: positions from .. len - 1
 __device__ inline KaSpan ka_span(const KaDivision& d, int b)
@@ -35,14 +36,13 @@ __device__ inline KaSpan ka_span(const KaDivision& d, int b)
     return s;
 }
 // blocks of a workgroup
-__device__ inline int ka_per(const KaDivision& d)
+__device__ inline int ka_per(const KaDivision& d, const KaSpan& mine)
 {
-    if (d.share == 0.0f) return INT32_MAX;
     const int lane = threadIdx.x & 63;
-    float sum = 0.0f;
-    for (int b0 = 0; b0 < d.B; b0 += 64) sum += (float)ka_span(d, b0 + lane).blocks;
+    float sum = (float)mine.blocks;
+    for (int b0 = 64; b0 < d.B; b0 += 64) sum += (float)ka_span(d, b0 + lane).blocks;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);      // the same order in every wavefront of both kernels
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);      // the same order in every wavefront
     return max(KA_LEAST, (int)(sum * d.share) + 1);
 }
 __device__ inline int ka_parts(int blocks, int per) { return blocks <= per ? 1 : (blocks + per - 1) / per; }
@@ -63,26 +63,27 @@ template <> struct Ka<SS_FP8_E4M3> : Ka<SS_BF16> {};
 __device__ inline uint32_t ka_pack(float a, float b, Ka<SS_BF16>) { return pack_bf16x2(a, b); }
 __device__ inline uint32_t ka_pack(float a, float b, Ka<SS_FP16>) { return f32_to_f16_bits(a) | (uint32_t)f32_to_f16_bits(b) << 16; }
 
-// eight codes of 8 bits as bf16
+// eight codes of 8 bits as bf16, which holds them exactly
 template <int DT> __device__ inline v8bf ka_widen(uint32_t lo, uint32_t hi)
 {
-    v4i r;
+    if constexpr (DT == SS_FP8_E4M3) {
+        typedef __bf16 two __attribute__((ext_vector_type(2)));
+        const two a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+        const two c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+        return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        v4i r;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t w = h ? hi : lo;
-        float f[4];
-        if constexpr (DT == SS_FP8_E4M3) {
-            f[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0); f[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
-            f[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2); f[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
-        } else {
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w = h ? hi : lo;
+            float f[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = (float)(int8_t)(w >> (8 * e));
+            r[2 * h] = (int)__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
+            r[2 * h + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
         }
-        // the upper halves: nothing is lost
-        r[2 * h] = (int)__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
-        r[2 * h + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+        return __builtin_bit_cast(v8bf, r);
     }
-    return __builtin_bit_cast(v8bf, r);
 }
 
 struct KaArgs {
@@ -92,6 +93,7 @@ struct KaArgs {
     int H, G, tiles, D, page, P;                     // heads of keys, query heads to each, products that take
     float scale;                                     // of the scores, times log2(e)
     uint16_t* out; int64_t ldo, ho;
+    int2* plan;                                      // of each request: its first item, its parts (if requests are divided)
     float2* sums;                                    // [item][head of keys][tile][column]: maximum, sum
     float* parts;                                    // the same [.. , 32 NS]: weighted values
     int items;
@@ -99,11 +101,13 @@ struct KaArgs {
     KaDivision division;
 };
 
+// wavefronts of a SIMD that registers are kept for
+constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : ns <= 6 ? 2 : 1; }
 // DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32)
 template <int DT, int NS, int QP>
-__global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
+__global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const KaArgs a)
 {
-    constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 8 ? NT : 8;
+    constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 32 / KA_WAVES ? NT : 32 / KA_WAVES;
     typedef typename Ka<DT>::frag frag;
     __shared__ float4 joined[KA_WAVES][CHUNK][64];
     __shared__ float2 wave_sums[KA_WAVES][KA_COLUMNS];
@@ -111,57 +115,121 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
     const int item = quot(blockIdx.x, a.by_units), unit = blockIdx.x - item * a.H * a.tiles, h = unit / a.tiles, tile = unit - h * a.tiles;
 
     // this workgroup's request and its part of it
-    const int per = ka_per(a.division);
-    int b = -1, part = 0, parts = 0;
+    int b = -1, part = 0, parts = 1;
     KaSpan span = {0, 0, 0, 0};
-    for (int b0 = 0, before = 0; b0 < a.division.B; b0 += 64) {
-        const KaSpan s = ka_span(a.division, b0 + lane);
-        const int n = b0 + lane < a.division.B ? ka_parts(s.blocks, per) : 0, upto = before + wave_scan_add(n);
-        const uint64_t has = __ballot(upto > item);
-        if (has) {
-            const int at = __ffsll((unsigned long long)has) - 1;
-            b = b0 + at;
-            parts = __builtin_amdgcn_readlane(n, at);
-            part = item - (__builtin_amdgcn_readlane(upto, at) - parts);
-            span = {__builtin_amdgcn_readlane(s.first, at), __builtin_amdgcn_readlane(s.blocks, at), __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.from, at)};
-            break;
+    if (!a.plan) {
+        b = item;
+        span = ka_span(a.division, b);
+    } else {
+        const KaSpan mine = ka_span(a.division, lane);   // of the first 64 requests, which mostly are all
+        const int per = ka_per(a.division, mine);
+        for (int b0 = 0, before = 0; b0 < a.division.B; b0 += 64) {
+            const KaSpan s = b0 == 0 ? mine : ka_span(a.division, b0 + lane);
+            const int n = b0 + lane < a.division.B ? ka_parts(s.blocks, per) : 0, upto = before + wave_scan_add(n);
+            const uint64_t has = __ballot(upto > item);
+            if (has) {
+                const int at = __ffsll((unsigned long long)has) - 1;
+                b = b0 + at;
+                parts = __builtin_amdgcn_readlane(n, at);
+                part = item - (__builtin_amdgcn_readlane(upto, at) - parts);
+                span = {__builtin_amdgcn_readlane(s.first, at), __builtin_amdgcn_readlane(s.blocks, at), __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.from, at)};
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
         }
-        before = __builtin_amdgcn_readlane(upto, 63);
     }
     if (b < 0) return;
+    if (a.plan && part == 0 && unit == 0 && threadIdx.x == 0) a.plan[b] = make_int2(item, parts);
     const int each = (span.blocks + parts - 1) / parts, lo = span.first + part * each, end = min(lo + each, span.first + span.blocks);
 
-    // the queries: lane (r, j) holds values 32 s + 8 j .. + 7 of head r
+    // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.
     const int column = tile * KA_COLUMNS + r;
+    const bool there = column < a.G;
+    uint32_t raw[NS][4 * QP];
+    {
+        const int64_t at = b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq + 8 * j;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int have = there ? a.D - 32 * s - 8 * j : 0;
+#pragma unroll
+            for (int e = 0; e < 4 * QP; ++e) raw[s][e] = 0;
+            if constexpr (QP == 1) {
+                const uint16_t* const p = static_cast<const uint16_t*>(a.q) + at + 32 * s;
+                if (have >= 8) {
+                    const ka16_t x = *reinterpret_cast<const ka16_t*>(p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) raw[s][e] = x[e];
+                } else if (have > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < have) raw[s][e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+                }
+            } else {
+                const float* const p = static_cast<const float*>(a.q) + at + 32 * s;
+                if (have >= 8) {
+                    const ka16f_t x = *reinterpret_cast<const ka16f_t*>(p), y = *reinterpret_cast<const ka16f_t*>(p + 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { raw[s][e] = x[e]; raw[s][4 + e] = y[e]; }
+                } else if (have > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < have) raw[s][e] = __float_as_uint(p[e]);
+                }
+            }
+        }
+    }
+    const int per_page = a.page / KV_BLOCK;
+    const int32_t* const row = a.table + b * a.ldt;
+    // This wavefront's blocks are first, first + KA_WAVES, ..: lane i holds the page of the i-th of 64 of them.  The keys of the next block are asked for when those of this one have
+    // been multiplied, the values likewise, into the same registers: a block is always under way.
+    const int first = lo + wave, blocks = first < end ? (end - first + KA_WAVES - 1) / KA_WAVES : 0;
+    int ids = 0, at_page = 0;                        // at_page: this lane's block of its page
+    bool valid = false, next_valid = false;
+    const uint8_t* from = a.pages;
+    uint4 k[LOADS], v[LOADS];
+    float ks[8], vs[8];
+    auto go_to = [&](int i) {
+        if ((i & 63) == 0) {
+            const int block = min(first + (i + lane) * KA_WAVES, end - 1), index = quot(block, a.by_blocks);
+            ids = row[index];
+            at_page = block - index * per_page;
+        }
+        const int id = __builtin_amdgcn_readlane(ids, i & 63);
+        next_valid = id >= 0 && id < a.P;            // no page: nothing to see, whatever is read instead
+        from = a.pages + (next_valid ? id : 0) * a.page_bytes + (int64_t)(h * per_page + __builtin_amdgcn_readlane(at_page, i & 63)) * BLOCK;
+    };
+    auto load_keys = [&]() {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) k[i] = load_once(reinterpret_cast<const uint4*>(from + i * 1024) + lane);
+        if constexpr (ES == 1) {
+            const float4* const scales = reinterpret_cast<const float4*>(from + 2 * HALF) + 2 * j;
+            const float4 x = scales[0], y = scales[1];
+            ks[0] = x.x; ks[1] = x.y; ks[2] = x.z; ks[3] = x.w; ks[4] = y.x; ks[5] = y.y; ks[6] = y.z; ks[7] = y.w;
+        }
+    };
+    auto load_values = [&]() {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) v[i] = load_once(reinterpret_cast<const uint4*>(from + HALF + i * 1024) + lane);
+        if constexpr (ES == 1) {
+            const float4* const scales = reinterpret_cast<const float4*>(from + 2 * HALF + 4 * KV_BLOCK) + 2 * j;
+            const float4 x = scales[0], y = scales[1];
+            vs[0] = x.x; vs[1] = x.y; vs[2] = x.z; vs[3] = x.w; vs[4] = y.x; vs[5] = y.y; vs[6] = y.z; vs[7] = y.w;
+        }
+    };
+    if (blocks > 0) {
+        go_to(0);
+        load_keys();
+        load_values();
+    }
+    // as operands
     frag q[QP][NS];
     float back = a.scale;                            // of a score
     {
         float f[NS][8];
-        const bool there = column < a.G;
-        const int64_t row = b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int d = 32 * s + 8 * j, have = there ? a.D - d : 0;
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[s][e] = 0.0f;
-            if constexpr (QP == 1) {
-                const uint16_t* const p = static_cast<const uint16_t*>(a.q) + row + d;
-                if (have >= 8) {
-                    const ka16_t v = *reinterpret_cast<const ka16_t*>(p);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { f[s][2 * e] = __uint_as_float(v[e] << 16); f[s][2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u); }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < have) f[s][e] = bf16_bits_to_f32(p[e]);
-                }
-            } else {
-                const float* const p = static_cast<const float*>(a.q) + row + d;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < have) f[s][e] = p[e];
-            }
-        }
+            for (int e = 0; e < 8; ++e) f[s][e] = __uint_as_float(QP == 2 ? raw[s][e * (QP - 1)] : e & 1 ? raw[s][e >> 1] & 0xFFFF0000u : raw[s][e >> 1] << 16);
         if constexpr (DT == SS_FP16) {
             // half has 5 bits of exponent: a head's values are brought below 1 by a power of two, which its scores get back
             float most = 0.0f;
@@ -209,23 +277,9 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
     v4f o[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[n] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int per_page = a.page / KV_BLOCK;
-    const int32_t* const row = a.table + b * a.ldt;
-    for (int block = lo + wave; block < end; block += KA_WAVES) {
-        const int index = quot(block, a.by_blocks), id = __builtin_amdgcn_readfirstlane(row[index]);
-        if (id < 0 || id >= a.P) continue;           // no page: nothing to see
-        const uint8_t* const from = a.pages + id * a.page_bytes + (int64_t)(h * per_page + block - index * per_page) * BLOCK;
-        uint4 k[LOADS], v[LOADS];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) k[i] = load_once(reinterpret_cast<const uint4*>(from + i * 1024) + lane);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) v[i] = load_once(reinterpret_cast<const uint4*>(from + HALF + i * 1024) + lane);
-        float ks[8], vs[8];
-        if constexpr (ES == 1) {
-            const float* const scales = reinterpret_cast<const float*>(from + 2 * HALF) + 8 * j;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { ks[e] = scales[e]; vs[e] = scales[KV_BLOCK + e]; }
-        }
+    for (int step = 0; step < blocks; ++step) {
+        const int block = first + step * KA_WAVES;
+        valid = next_valid;
         // scores of tokens 8 j + 4 t + i
         v4f s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
@@ -241,14 +295,18 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ES == 1 ? back * ks[e] : back);
+        if (step + 1 < blocks) {
+            go_to(step + 1);
+            load_keys();
+        }
         const int at = block * KV_BLOCK + 8 * j;
-        const bool whole = block * KV_BLOCK >= span.from && block * KV_BLOCK + KV_BLOCK <= span.len;
+        const bool whole = valid && block * KV_BLOCK >= span.from && block * KV_BLOCK + KV_BLOCK <= span.len;
         uint32_t seen = 0xFF;
         if (!whole) {                                // what nobody wrote may be anything, a NaN too
             seen = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool there = at + e >= span.from && at + e < span.len;
+                const bool there = valid && at + e >= span.from && at + e < span.len;
                 seen |= there ? 1u << e : 0u;
                 x[e] = there ? x[e] : -INFINITY;
             }
@@ -309,6 +367,7 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
 #pragma unroll
             for (int i = 0; i < PP; ++i) o[n] = Ka<DT>::mma(f, p[i], o[n]);
         }
+        if (step + 1 < blocks) load_values();
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
@@ -326,7 +385,6 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
         all_sum += s.y * weight[w];
     }
     const int64_t place = ((int64_t)item * a.H * a.tiles + unit) * KA_COLUMNS + r;
-    const bool there = column < a.G;
     if (parts > 1 && wave == 0 && j == 0 && there) a.sums[place] = make_float2(all_top, all_sum);
     // nothing seen: zeros
     const float inverse = parts > 1 ? 1.0f : all_sum == 0.0f ? 0.0f : 1.0f / all_sum;
@@ -361,58 +419,77 @@ __global__ __launch_bounds__(64 * KA_WAVES) void k_kv_attend(const KaArgs a)
     }
 }
 
-// Joins the parts of a request that was divided: a workgroup for each query head of each request, which leaves where it was not.
-template <int NS>
-__global__ __launch_bounds__(256) void k_kv_join(const KaArgs a)
+// Joins the parts of a request that was divided: a workgroup for each query head of each request, which leaves where it was not.  A row of weighted values is 8 NS lanes wide.
+constexpr int KJ_EACH = 8;                           // rows that a thread asks for ahead of their weights
+template <int NS, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
 {
-    constexpr int WIDTH = 32 * NS;
-    __shared__ float acc[4][WIDTH];
-    __shared__ float wave_sum[4], wave_top[4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int heads = a.H * a.G, b = blockIdx.x / heads, head = blockIdx.x - b * heads, h = head / a.G, column = head - h * a.G;
-    const int per = ka_per(a.division);
-    int item = 0, parts = 0;
-    for (int b0 = 0; b0 <= b; b0 += 64) {
-        const int n = b0 + lane <= b ? ka_parts(ka_span(a.division, b0 + lane).blocks, per) : 0, upto = wave_scan_add(n);
-        if (b < b0 + 64) {
-            parts = __builtin_amdgcn_readlane(n, b - b0);
-            item += __builtin_amdgcn_readlane(upto, b - b0) - parts;
-        } else item += __builtin_amdgcn_readlane(upto, 63);
-    }
+    constexpr int WIDTH = 32 * NS, LANES = WIDTH / 4, ROWS = THREADS / LANES, ROUND = ROWS * KJ_EACH;
+    __shared__ float4 acc[ROWS][LANES];
+    __shared__ float2 sums[ROUND];
+    __shared__ float row_sums[ROWS], tops[THREADS / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int heads = a.H * a.G, b = blockIdx.x / heads;
+    const int2 plan = a.plan[b];
+    const int parts = plan.y;
     if (parts < 2) return;
-    const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = item * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
-    float top = -INFINITY;
-    for (int i = wave * 64 + lane; i < parts; i += 256) top = fmaxf(top, a.sums[first + i * step].x);
+    const int head = blockIdx.x - b * heads, h = head / a.G, column = head - h * a.G;
+    const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = plan.x * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
+    const int at_row = threadIdx.x / LANES, at = threadIdx.x - at_row * LANES;
+    float top = -INFINITY, sum = 0.0f;
+    v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = 0; i0 < parts; i0 += ROUND) {      // mostly once
+        float4 p[KJ_EACH];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    if (lane == 0) wave_top[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
-    constexpr int PER = (WIDTH + 63) / 64;
-    float v[PER], sum = 0.0f;
+        for (int i = 0; i < KJ_EACH; ++i) {
+            const int q = i0 + at_row + i * ROWS;
+            p[i] = at_row < ROWS && q < parts ? reinterpret_cast<const float4*>(a.parts + (first + q * step) * WIDTH)[at] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        float most = -INFINITY;
+        if (i0 > 0) __syncthreads();
+        for (int i = threadIdx.x; i < ROUND; i += THREADS) {
+            const float2 s = i0 + i < parts ? a.sums[first + (i0 + i) * step] : make_float2(-INFINITY, 0.0f);
+            sums[i] = s;
+            most = fmaxf(most, s.x);
+        }
 #pragma unroll
-    for (int c = 0; c < PER; ++c) v[c] = 0.0f;
-    for (int i = wave; i < parts; i += 4) {
-        const float2 s = a.sums[first + i * step];
-        const float weight = s.x == top ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
-        sum += s.y * weight;
-        const float* const p = a.parts + (first + i * step) * WIDTH;
+        for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+        if (lane == 0) tops[wave] = most;
+        __syncthreads();
 #pragma unroll
-        for (int c = 0; c < PER; ++c)
-            if (64 * c + lane < WIDTH) v[c] += p[64 * c + lane] * weight;
+        for (int w = 0; w < THREADS / 64; ++w) most = fmaxf(most, tops[w]);
+        most = fmaxf(most, top);
+        const float less = top == most ? 1.0f : __builtin_amdgcn_exp2f(top - most);
+        top = most;
+        v *= less;
+        sum *= less;
+#pragma unroll
+        for (int i = 0; i < KJ_EACH; ++i) {
+            const float2 s = sums[min(at_row, ROWS - 1) + i * ROWS];
+            const float weight = s.x == top ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
+            sum += s.y * weight;
+            v += v4f{p[i].x, p[i].y, p[i].z, p[i].w} * weight;
+        }
     }
-#pragma unroll
-    for (int c = 0; c < PER; ++c)
-        if (64 * c + lane < WIDTH) acc[wave][64 * c + lane] = v[c];
-    if (lane == 0) wave_sum[wave] = sum;
+    if (at_row < ROWS) {
+        acc[at_row][at] = make_float4(v[0], v[1], v[2], v[3]);
+        if (at == 0) row_sums[at_row] = sum;
+    }
     __syncthreads();
-    sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+    sum = row_sums[0];
+#pragma unroll
+    for (int r = 1; r < ROWS; ++r) sum += row_sums[r];
     const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-    for (int d = threadIdx.x; d < a.D; d += 256) {
-        const float x = ((acc[0][d] + acc[1][d]) + (acc[2][d] + acc[3][d])) * inverse;
-        a.out[b * a.ldo + head * a.ho + d] = (uint16_t)pack_bf16x2(x, 0.0f);
+    const float* const rows = reinterpret_cast<const float*>(acc);
+    for (int d = threadIdx.x; d < a.D; d += THREADS) {
+        float x = 0.0f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) x += rows[r * WIDTH + d];
+        a.out[b * a.ldo + head * a.ho + d] = (uint16_t)pack_bf16x2(x * inverse, 0.0f);
     }
 }
+
+constexpr int64_t KJ_ROWS = 512;                     // query heads of all requests up to which the parts are joined by large workgroups
 
 template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool fp32, bool join, int64_t groups, int64_t rows, hipStream_t hs)
 {
@@ -420,14 +497,17 @@ template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool f
     else hipLaunchKernelGGL((k_kv_attend<DT, NS, 1>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
     if (!join) return launch_status();
     if (launch_status() != SS_OK) return SS_ERR_HIP;
-    hipLaunchKernelGGL(k_kv_join<NS>, dim3((uint32_t)rows), dim3(256), 0, hs, a);
+    if (rows <= KJ_ROWS) hipLaunchKernelGGL((k_kv_join<NS, 512>), dim3((uint32_t)rows), dim3(512), 0, hs, a);
+    else hipLaunchKernelGGL((k_kv_join<NS, 128>), dim3((uint32_t)rows), dim3(128), 0, hs, a);
     return launch_status();
 }
 
 // Workgroups that all heads' parts come to, about.
-static int64_t wanted_groups() { return 4 * (int64_t)cu_count(); }
+static int64_t wanted_groups() { return 2 * (int64_t)cu_count(); }
 // bytes of a part of a request: sums and values of all heads
 static int64_t part_bytes(int64_t units, int64_t D) { return units * KA_COLUMNS * (8 + 4 * 32 * kv_steps(D)); }
+// and of the plan that lies before them
+static int64_t plan_bytes(int64_t B) { return (8 * B + 15) & ~(int64_t)15; }
 
 }  // namespace ss
 
@@ -442,7 +522,7 @@ extern "C" size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H,
 {
     if (!valid_attention(B, Hq, H, D) || B == 0) return 0;
     const int64_t units = H * ((Hq / H + KA_COLUMNS - 1) / KA_COLUMNS);
-    return (size_t)((wanted_groups() / units + 2 + B) * part_bytes(units, D));
+    return (size_t)(plan_bytes(B) + (wanted_groups() / units + 2 + B) * part_bytes(units, D));
 }
 
 extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* table,
@@ -469,16 +549,18 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
     a.out = static_cast<uint16_t*>(out); a.ldo = ldo; a.ho = ho;
     const int64_t units = H * a.tiles;
     // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.
-    const int64_t room = (int64_t)(workspace_bytes / (size_t)part_bytes(units, D)) - B - 2, want = wanted_groups() / units, wanted = room < want ? room : want;
-    const bool join = wanted > 0 && W * page > (int64_t)KA_LEAST * KV_BLOCK;
+    const int64_t bytes = (int64_t)(workspace_bytes < (size_t)1 << 50 ? workspace_bytes : (size_t)1 << 50) - plan_bytes(B);
+    const int64_t room = bytes / part_bytes(units, D) - B - 2, want = wanted_groups() / units, wanted = room < want ? room : want;
+    const bool join = wanted > 1 && W * page > (int64_t)KA_ONE * KV_BLOCK;
     a.division = {lens, (int)B, (int)(W * page), (int)(window < INT32_MAX ? window : 0), join ? 1.0f / (float)wanted : 0.0f};
     a.items = (int)(join ? wanted + 2 + B : B);
-    a.sums = static_cast<float2*>(workspace);
+    a.plan = join ? static_cast<int2*>(workspace) : nullptr;
+    a.sums = join ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan_bytes(B)) : nullptr;
     a.parts = join ? reinterpret_cast<float*>(a.sums + a.items * units * KA_COLUMNS) : nullptr;
     a.by_units = make_div(units);
     a.by_blocks = make_div(page / KV_BLOCK);
     const int64_t groups = a.items * units, rows = B * Hq;
-    if (!mx4_grid_fits(groups, 64 * KA_WAVES) || !mx4_grid_fits(rows, 256)) return SS_ERR_SHAPE;
+    if (!mx4_grid_fits(groups, 64 * KA_WAVES) || !mx4_grid_fits(rows, 128)) return SS_ERR_SHAPE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const bool fp32 = in_dtype == SS_IN_F32;
 #define SS_KA(DT)                                                                     \

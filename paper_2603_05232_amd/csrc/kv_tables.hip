@@ -9,27 +9,23 @@ constexpr int64_t KT_ONE_LAUNCH = 8192;              // new tokens up to which t
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
 
-// inclusive sum over the workgroup's threads (values >= 0); total: that of all
-__device__ inline int block_scan(int v, int* part, int& total)
+// Inclusive sums over the workgroup's threads (values >= 0), of as many numbers as `part` has rows; total: that of all.  part is used anew in every call.
+template <int NUM> __device__ inline void block_scan(int (&v)[NUM], int (*part)[KT_THREADS / 64], int (&total)[NUM])
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int sum = min(v, KT_CAP);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int other = __shfl_up(sum, d, 64);
-        if (lane >= d) sum = cap_add(sum, other);
+    for (int q = 0; q < NUM; ++q) {
+        v[q] = wave_scan(min(v[q], KT_CAP), 0, [](int a, int b) { return cap_add(a, b); });
+        if (lane == 63) part[q][wave] = v[q];
     }
-    __syncthreads();                                 // part is free again
-    if (lane == 63) part[wave] = sum;
     __syncthreads();
-    int before = 0;
-    total = 0;
 #pragma unroll
-    for (int w = 0; w < KT_THREADS / 64; ++w) {
-        if (w < wave) before = cap_add(before, part[w]);
-        total = cap_add(total, part[w]);
+    for (int q = 0; q < NUM; ++q) {
+        const int all = wave_scan(lane < KT_THREADS / 64 ? part[q][lane] : 0, 0, [](int a, int b) { return cap_add(a, b); });      // lane w: of wavefronts 0 .. w
+        const int before = wave == 0 ? 0 : __builtin_amdgcn_readlane(all, wave - 1);
+        v[q] = cap_add(before, v[q]);
+        total[q] = __builtin_amdgcn_readlane(all, 63);
     }
-    return cap_add(before, sum);
 }
 
 // What filling in needs of each request.
@@ -41,19 +37,19 @@ struct KtPlan {
 };
 
 // Row i: the request that it belongs to, its position there, its page.  A new page is entered in the table by the row that begins it.
-__device__ inline void kt_fill(const KtPlan& plan, int i, int B, int32_t* __restrict__ table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P,
+__device__ inline void kt_fill(const int32_t* start, const KtPlan& plan, int i, int B, int32_t* __restrict__ table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P,
                                int32_t* __restrict__ slots)
 {
-    if (i >= plan.start[B]) { slots[i] = -1; return; }
+    if (i >= start[B]) { slots[i] = -1; return; }
     int lo = 0, hi = B;                              // the last request that begins at or before i
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (plan.start[mid] <= i) lo = mid;
+        if (start[mid] <= i) lo = mid;
         else hi = mid;
     }
     const int first = plan.first[lo];
     if (first < 0) { slots[i] = -1; return; }
-    const int len = plan.len[lo], at = len + (i - plan.start[lo]), column = quot(at, by_page), row = at - column * page, have = quot(len + page - 1, by_page);
+    const int len = plan.len[lo], at = len + (i - start[lo]), column = quot(at, by_page), row = at - column * page, have = quot(len + page - 1, by_page);
     int32_t* const cell = table + lo * ldt + column;
     int id;
     if (column >= have) {
@@ -72,9 +68,9 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
                                                         int32_t* __restrict__ offsets, KtPlan* __restrict__ out)
 {
     __shared__ KtPlan plan;
-    __shared__ int part[KT_THREADS / 64];
+    __shared__ int part[2 * (int)(KV_MAX_REQUESTS / KT_THREADS)][3][KT_THREADS / 64];
     __shared__ int taken;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, most = W * page;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, most = W * page;
     const int free_before = min(max(*left, 0), P);
     if (threadIdx.x == 0) taken = 0;
     int rows = 0, pages = 0, back = 0;               // sums of the requests before
@@ -87,28 +83,38 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
         if (b0 >= B) continue;                       // the same for all threads
         const int l = b < B ? min(max(lens[b], 0), most) : 0, w = b < B ? max(want[b], 0) : 0;
         const int have = quot(l + page - 1, by_page), need = quot(min(w, most) + page - 1, by_page);
-        int all;
-        const int grow = max(w - l, 0), end = block_scan(min(grow, N + 1), part, all), end_all = cap_add(rows, end);
-        rows = cap_add(rows, all);
-        const bool possible = w <= most && end_all <= N;
+        const int grow = max(w - l, 0), fewer = w < l ? have - need : 0;
+        int sums[2] = {min(grow, N + 1), fewer}, all[2];
+        block_scan(sums, part[2 * q], all);
+        const int end = cap_add(rows, sums[0]), given = cap_add(back, sums[1]);
+        rows = cap_add(rows, all[0]);
+        back = cap_add(back, all[1]);
+        const bool possible = w <= most && end <= N;
         const int more = possible ? max(need - have, 0) : 0;
-        const int up = cap_add(pages, block_scan(more, part, all));
-        pages = cap_add(pages, all);
-        const int fewer = w < l ? have - need : 0, given = cap_add(back, block_scan(fewer, part, all));
-        back = cap_add(back, all);
+        int taken_to[1] = {more}, all_taken[1];
+        block_scan(taken_to, part[2 * q + 1], all_taken);
+        const int up = cap_add(pages, taken_to[0]);
+        pages = cap_add(pages, all_taken[0]);
         if (b < B) {
-            plan.start[b] = min(end_all - min(grow, N + 1), N);
+            plan.start[b] = min(end - min(grow, N + 1), N);
             plan.len[b] = l;
             plan.first[b] = up - more;
         }
         upto[q] = more > 0 ? up : 0;
         wanted[q] = possible || w <= l ? w : -1;
-        // pages given back, a wavefront for each request that has any
-        for (uint64_t has = __ballot(fewer > 0); has; has &= has - 1) {
-            const int at = __ffsll((unsigned long long)has) - 1, n = __builtin_amdgcn_readlane(fewer, at), to = free_before + __builtin_amdgcn_readlane(given - fewer, at);
-            const int32_t* const from = table + (int64_t)(b0 + wave * 64 + at) * ldt + __builtin_amdgcn_readlane(need, at);
-            for (int i = lane; i < n; i += 64)
-                if (to + i < P) pool[to + i] = from[i];
+        // pages given back: sixteen lanes to a request that has any, four of them at a time
+        for (uint64_t has = __ballot(fewer > 0); has;) {
+            int at = -1;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if (has && lane >> 4 == g) at = __ffsll((unsigned long long)has) - 1;
+                has &= has - 1;
+            }
+            const int from = max(at, 0), n = __shfl(fewer, from, 64), to = free_before + __shfl(given, from, 64) - n, column = __shfl(need, from, 64);
+            if (at < 0) continue;
+            const int32_t* const ids = table + (int64_t)(b0 + wave * 64 + at) * ldt + column;
+            for (int x = lane & 15; x < n; x += 16)
+                if (to + x < P) pool[to + x] = ids[x];
         }
     }
     const int all_pages = min(cap_add(free_before, back), P);
@@ -127,7 +133,7 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
     __syncthreads();
     if (threadIdx.x == 0) { offsets[B] = plan.start[B]; *new_left = all_pages - taken; }
     if constexpr (WHOLE) {
-        for (int i = threadIdx.x; i < N; i += KT_THREADS) kt_fill(plan, i, B, table, ldt, page, by_page, pool, P, slots);
+        for (int i = threadIdx.x; i < N; i += KT_THREADS) kt_fill(plan.start, plan, i, B, table, ldt, page, by_page, pool, P, slots);
     } else {
         for (int b = threadIdx.x; b <= B; b += KT_THREADS) out->start[b] = plan.start[b];
         for (int b = threadIdx.x; b < B; b += KT_THREADS) { out->len[b] = plan.len[b]; out->first[b] = plan.first[b]; }
@@ -135,11 +141,15 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
     }
 }
 
+// The same by as many workgroups as the rows fill, for which the plan went through memory.
 __global__ __launch_bounds__(256) void k_kv_slots(const KtPlan* __restrict__ plan, int B, int32_t* table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P, int N,
                                                   int32_t* __restrict__ slots)
 {
+    __shared__ int32_t start[KV_MAX_REQUESTS + 1];
+    for (int b = threadIdx.x; b <= B; b += 256) start[b] = plan->start[b];
+    __syncthreads();
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < N) kt_fill(*plan, i, B, table, ldt, page, by_page, pool, P, slots);
+    if (i < N) kt_fill(start, *plan, i, B, table, ldt, page, by_page, pool, P, slots);
 }
 
 }  // namespace ss

@@ -101,7 +101,7 @@ __device__ inline void kv_scale(uint32_t largest, float qmax, float& scale, floa
     const float a = __uint_as_float(largest);
     const bool bad = largest >= 0x7F800000u, none = a < 0x1p-100f;
     scale = bad ? __uint_as_float(0x7FC00000u) : none ? 1.0f : a / qmax;
-    inverse = bad || none ? 0.0f : qmax / a;
+    inverse = bad || none ? 0.0f : qmax * (1.0f / a);
 }
 
 __device__ inline uint32_t kv_row_max(uint32_t v)    // over eight lanes side by side

@@ -250,9 +250,9 @@ def test_attention(Hq, H, D, page, source, dtype):
     cache = Cache(np.random.default_rng(Hq + D), LENS, H, D, page, dtype)
     q = queries(len(LENS), Hq, D, source)
     got = cache(q)
-    assert bool((cache.scratch == 0x7F).all())                     # none of these is long enough to be divided
     cache.check(got, q)
-    assert bool((got[0] == 0).all()) and torch.equal(got, cache(q, ws=False))
+    cache.check(cache(q, ws=False), q)
+    assert bool((got[0] == 0).all())
     for window in (1, 33, 100):
         cache.check(cache(q, window=window), q, window=window)
 
@@ -284,7 +284,7 @@ def test_attention_with_less_room(room):
     cache = Cache(np.random.default_rng(1), [6000, 700], 2, 64, 64, "bf16")
     q = queries(2, 4, 64, "bf16")
     per = 2 * 16 * (8 + 4 * 64)                                    # a part: two heads of keys, sixteen columns
-    n = (4 + room) * per
+    n = 16 + (4 + room) * per                                      # behind the division of two requests
     ws = torch.zeros((n + 64,), dtype=torch.uint8, device=DEV)
     got = binding.kv_attention(q, cache.pages, i32(cache.table), i32(cache.lens), 2, 64, "bf16", workspace=ws[:n])
     cache.check(got, q)

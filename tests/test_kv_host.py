@@ -85,8 +85,8 @@ def test_oracle_of_what_a_cache_holds(dtype):
         want = x.to(torch.bfloat16 if dtype == "bf16" else torch.float16).float().numpy()
     else:
         a = x.abs().amax(-1, keepdim=True)
-        y = x * (ko.LARGEST[dtype] / a)
-        want = ((torch.round(y) if dtype == "i8" else y.to(torch.float8_e4m3fn).float()) * (a / ko.LARGEST[dtype])).numpy()
+        y = x * (torch.reciprocal(a) * ko.LARGEST[dtype])
+        want = ((torch.round(y) if dtype == "i8" else y.to(torch.float8_e4m3fn).float()) * (a / torch.full_like(a, ko.LARGEST[dtype]))).numpy()
     assert np.array_equal(got, want)
     if dtype in ko.LARGEST:
         odd = ko.held(np.array([[0.0, 0.0], [np.inf, 1.0], [1.0, np.nan], [1e-38, 0.0]], np.float32), dtype)
