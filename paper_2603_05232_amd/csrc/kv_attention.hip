@@ -12,7 +12,6 @@ namespace ss {
 constexpr int KA_WAVES = 4;                          // wavefronts of a workgroup
 constexpr int KA_COLUMNS = 16;                       // query heads of a product
 constexpr int KA_ONE = 16;                           // blocks of a row of the table up to which requests are not divided
-constexpr int KA_LEAST = 4;                         // blocks that are worth a workgroup of their own
 
 typedef uint32_t ka16_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
@@ -43,7 +42,8 @@ __device__ inline int ka_per(const KaDivision& d, const KaSpan& mine)
     for (int b0 = 64; b0 < d.B; b0 += 64) sum += (float)ka_span(d, b0 + lane).blocks;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);      // the same order in every wavefront
-    return max(KA_LEAST, (int)(sum * d.share) + 1);
+    const float n = sum * d.share;
+    return n < 8 * KA_WAVES ? KA_WAVES * max(1, (int)(n * (1.0f / KA_WAVES) + 0.999f)) : (int)n + 1;      // whole rounds of the wavefronts, while these are few
 }
 __device__ inline int ka_parts(int blocks, int per) { return blocks <= per ? 1 : (blocks + per - 1) / per; }
 
@@ -102,10 +102,10 @@ struct KaArgs {
 };
 
 // wavefronts of a SIMD that registers are kept for
-constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : ns <= 6 ? 2 : 1; }
+constexpr int ka_fit(int es, int ns) { return ns <= 4 ? 3 : ns <= 6 || es == 1 ? 2 : 1; }
 // DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32)
 template <int DT, int NS, int QP>
-__global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const KaArgs a)
+__global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_attend(const KaArgs a)
 {
     constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 32 / KA_WAVES ? NT : 32 / KA_WAVES;
     typedef typename Ka<DT>::frag frag;
