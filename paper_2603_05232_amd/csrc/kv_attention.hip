@@ -148,33 +148,35 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
     uint32_t raw[NS][4 * QP];
     {
         const int64_t at = b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq + 8 * j;
+        typedef typename std::conditional<QP == 1, uint16_t, float>::type T;
+        const T* const p = static_cast<const T*>(a.q) + at;
+        // whole pieces first, all of them: a branch between two loads makes the second wait for the first
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            const int have = there ? a.D - 32 * s - 8 * j : 0;
-#pragma unroll
-            for (int e = 0; e < 4 * QP; ++e) raw[s][e] = 0;
+            const bool all = there && 32 * s + 8 * j + 8 <= a.D;
             if constexpr (QP == 1) {
-                const uint16_t* const p = static_cast<const uint16_t*>(a.q) + at + 32 * s;
-                if (have >= 8) {
-                    const ka16_t x = *reinterpret_cast<const ka16_t*>(p);
+                ka16_t x = {0, 0, 0, 0};
+                if (all) x = *reinterpret_cast<const ka16_t*>(p + 32 * s);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) raw[s][e] = x[e];
-                } else if (have > 0) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < have) raw[s][e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-                }
+                for (int e = 0; e < 4; ++e) raw[s][e] = x[e];
             } else {
-                const float* const p = static_cast<const float*>(a.q) + at + 32 * s;
-                if (have >= 8) {
-                    const ka16f_t x = *reinterpret_cast<const ka16f_t*>(p), y = *reinterpret_cast<const ka16f_t*>(p + 4);
+                ka16f_t x = {0, 0, 0, 0}, y = x;
+                if (all) { x = *reinterpret_cast<const ka16f_t*>(p + 32 * s); y = *reinterpret_cast<const ka16f_t*>(p + 32 * s + 4); }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { raw[s][e] = x[e]; raw[s][4 + e] = y[e]; }
-                } else if (have > 0) {
+                for (int e = 0; e < 4; ++e) { raw[s][e] = x[e]; raw[s][4 + e] = y[e]; }
+            }
+        }
+        if (a.D & 7) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < have) raw[s][e] = __float_as_uint(p[e]);
-                }
+            for (int s = 0; s < NS; ++s) {
+                const int have = there ? a.D - 32 * s - 8 * j : 0;
+                if (have <= 0 || have >= 8) continue;
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < have) {
+                        if constexpr (QP == 1) raw[s][e >> 1] |= (uint32_t)p[32 * s + e] << (16 * (e & 1));
+                        else raw[s][e] = __float_as_uint(p[32 * s + e]);
+                    }
             }
         }
     }
