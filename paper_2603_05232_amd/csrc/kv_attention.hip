@@ -102,10 +102,10 @@ struct KaArgs {
 };
 
 // wavefronts of a SIMD that registers are kept for
-constexpr int ka_fit(int es, int ns) { return ns <= 4 ? 3 : ns <= 6 || es == 1 ? 2 : 1; }
+constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : 2; }
 // DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32)
 template <int DT, int NS, int QP>
-__global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_attend(const KaArgs a)
+__global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const KaArgs a)
 {
     constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 32 / KA_WAVES ? NT : 32 / KA_WAVES;
     typedef typename Ka<DT>::frag frag;
@@ -142,40 +142,45 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
     if (a.plan && part == 0 && unit == 0 && threadIdx.x == 0) a.plan[b] = make_int2(item, parts);
     const int each = (span.blocks + parts - 1) / parts, lo = span.first + part * each, end = min(lo + each, span.first + span.blocks);
 
-    // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.
+    // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.  Long heads are shared out among the wavefronts, which leave their operands in LDS:
+    // all of them would take the registers that a second wavefront of the SIMD needs.
+    constexpr bool SHARED = NS > 4;
+    constexpr int OWN = SHARED ? (NS + KA_WAVES - 1) / KA_WAVES : NS;
+    __shared__ v4i shared_q[SHARED ? QP : 1][SHARED ? NS : 1][64];
+    auto own = [&](int u) { return SHARED ? wave + u * KA_WAVES : u; };
     const int column = tile * KA_COLUMNS + r;
     const bool there = column < a.G;
-    uint32_t raw[NS][4 * QP];
+    uint32_t raw[OWN][4 * QP];
     {
-        const int64_t at = b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq + 8 * j;
         typedef typename std::conditional<QP == 1, uint16_t, float>::type T;
-        const T* const p = static_cast<const T*>(a.q) + at;
+        const T* const p = static_cast<const T*>(a.q) + (b * a.ldq + (int64_t)(h * a.G + (there ? column : 0)) * a.hq);
         // whole pieces first, all of them: a branch between two loads makes the second wait for the first
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const bool all = there && 32 * s + 8 * j + 8 <= a.D;
+        for (int u = 0; u < OWN; ++u) {
+            const int d = 32 * own(u) + 8 * j;
+            const bool all = there && d + 8 <= a.D;
             if constexpr (QP == 1) {
                 ka16_t x = {0, 0, 0, 0};
-                if (all) x = *reinterpret_cast<const ka16_t*>(p + 32 * s);
+                if (all) x = *reinterpret_cast<const ka16_t*>(p + d);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) raw[s][e] = x[e];
+                for (int e = 0; e < 4; ++e) raw[u][e] = x[e];
             } else {
                 ka16f_t x = {0, 0, 0, 0}, y = x;
-                if (all) { x = *reinterpret_cast<const ka16f_t*>(p + 32 * s); y = *reinterpret_cast<const ka16f_t*>(p + 32 * s + 4); }
+                if (all) { x = *reinterpret_cast<const ka16f_t*>(p + d); y = *reinterpret_cast<const ka16f_t*>(p + d + 4); }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { raw[s][e] = x[e]; raw[s][4 + e] = y[e]; }
+                for (int e = 0; e < 4; ++e) { raw[u][e] = x[e]; raw[u][4 + e] = y[e]; }
             }
         }
         if (a.D & 7) {
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int have = there ? a.D - 32 * s - 8 * j : 0;
+            for (int u = 0; u < OWN; ++u) {
+                const int d = 32 * own(u) + 8 * j, have = there ? a.D - d : 0;
                 if (have <= 0 || have >= 8) continue;
 #pragma unroll
                 for (int e = 0; e < 7; ++e)
                     if (e < have) {
-                        if constexpr (QP == 1) raw[s][e >> 1] |= (uint32_t)p[32 * s + e] << (16 * (e & 1));
-                        else raw[s][e] = __float_as_uint(p[32 * s + e]);
+                        if constexpr (QP == 1) raw[u][e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+                        else raw[u][e] = __float_as_uint(p[d + e]);
                     }
             }
         }
@@ -224,39 +229,45 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
         load_values();
     }
     // as operands
-    frag q[QP][NS];
+    frag q[SHARED ? 1 : QP][SHARED ? 1 : NS];
     float back = a.scale;                            // of a score
     {
-        float f[NS][8];
+        float f[OWN][8];
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+        for (int u = 0; u < OWN; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[s][e] = __uint_as_float(QP == 2 ? raw[s][e * (QP - 1)] : e & 1 ? raw[s][e >> 1] & 0xFFFF0000u : raw[s][e >> 1] << 16);
+            for (int e = 0; e < 8; ++e) f[u][e] = __uint_as_float(QP == 2 ? raw[u][e * (QP - 1)] : e & 1 ? raw[u][e >> 1] & 0xFFFF0000u : raw[u][e >> 1] << 16);
         if constexpr (DT == SS_FP16) {
             // half has 5 bits of exponent: a head's values are brought below 1 by a power of two, which its scores get back
             float most = 0.0f;
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+            for (int u = 0; u < OWN; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[s][e]));
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[u][e]));
             most = fmaxf(most, __shfl_xor(most, 16, 64));
             most = fmaxf(most, __shfl_xor(most, 32, 64));
+            if constexpr (SHARED) {
+                if (j == 0) wave_sums[wave][r].x = most;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < KA_WAVES; ++w) most = fmaxf(most, wave_sums[w][r].x);
+            }
             const int x = most > 0x1p-100f && most < INFINITY ? min((int)(__float_as_uint(most) >> 23) - 126, 126) : 0;      // most < 2^x, or 4 times that
             const float down = __uint_as_float((uint32_t)(127 - x) << 23);
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+            for (int u = 0; u < OWN; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[s][e] *= down;
+                for (int e = 0; e < 8; ++e) f[u][e] *= down;
             back *= __uint_as_float((uint32_t)(127 + x) << 23);
         }
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+        for (int u = 0; u < OWN; ++u)
 #pragma unroll
             for (int p = 0; p < QP; ++p) {
                 v4i w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t both = ka_pack(f[s][2 * e], f[s][2 * e + 1], Ka<DT>());
+                    const uint32_t both = ka_pack(f[u][2 * e], f[u][2 * e + 1], Ka<DT>());
                     w[e] = (int)both;
                     if (p + 1 < QP) {                // what the piece left out; of an infinity nothing
                         typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
@@ -264,14 +275,21 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
                         const two_t t = __builtin_bit_cast(two_t, both);
 #pragma unroll
                         for (int o = 0; o < 2; ++o) {
-                            float& x = f[s][2 * e + o];
+                            float& x = f[u][2 * e + o];
                             x = fabsf(x) < INFINITY ? x - (float)t[o] : 0.0f;
                         }
                     }
                 }
-                q[p][s] = __builtin_bit_cast(frag, w);
+                if constexpr (!SHARED) q[p][u] = __builtin_bit_cast(frag, w);
+                else if (own(u) < NS) shared_q[p][own(u)][lane] = w;
             }
+        if constexpr (SHARED) __syncthreads();
     }
+    int at_query = lane;
+    auto query = [&](int p, int s) -> frag {
+        if constexpr (SHARED) return __builtin_bit_cast(frag, shared_q[p][s][at_query]);
+        else return q[p][s];
+    };
 
     // The probabilities of half are taken 2^14 times as large, so that the smallest ones keep their bits: all of them, the sum too.
     constexpr float LIFT = DT == SS_FP16 ? 14.0f : 0.0f;
@@ -282,6 +300,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
     for (int step = 0; step < blocks; ++step) {
         const int block = first + step * KA_WAVES;
         valid = next_valid;
+        if constexpr (SHARED) asm volatile("" : "+v"(at_query));      // read anew for every block, not kept in registers
         // scores of tokens 8 j + 4 t + i
         v4f s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
@@ -292,7 +311,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
                 if constexpr (ES == 2) f = __builtin_bit_cast(frag, k[2 * i + t]);
                 else f = t ? ka_widen<DT>(k[i].z, k[i].w) : ka_widen<DT>(k[i].x, k[i].y);
 #pragma unroll
-                for (int p = 0; p < QP; ++p) s[t] = Ka<DT>::mma(f, q[p][i], s[t]);
+                for (int p = 0; p < QP; ++p) s[t] = Ka<DT>::mma(f, query(p, i), s[t]);
             }
         float x[8];
 #pragma unroll
@@ -421,23 +440,24 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(kv_es(DT), NS)) void k_kv_att
     }
 }
 
-// Joins the parts of a request that was divided: a workgroup for each query head of each request, which leaves where it was not.  A row of weighted values is 8 NS lanes wide.
+// Joins the parts of a request that was divided: a workgroup for each query head of each request, or for each 32 values of it, which leaves where it was not.  SLICE: steps of 32 values of a workgroup,
+// whose rows are 8 lanes wide each.
 constexpr int KJ_EACH = 8;                           // rows that a thread asks for ahead of their weights
-template <int NS, int THREADS>
+template <int NS, int SLICE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
 {
-    constexpr int WIDTH = 32 * NS, LANES = WIDTH / 4, ROWS = THREADS / LANES, ROUND = ROWS * KJ_EACH;
+    constexpr int WIDTH = 32 * NS, LANES = 8 * SLICE, ROWS = THREADS / LANES, ROUND = ROWS * KJ_EACH;
     __shared__ float4 acc[ROWS][LANES];
     __shared__ float2 sums[ROUND];
     __shared__ float row_sums[ROWS], tops[THREADS / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int heads = a.H * a.G, b = blockIdx.x / heads;
+    const int slice = blockIdx.x % (NS / SLICE), index = blockIdx.x / (NS / SLICE), heads = a.H * a.G, b = index / heads;
     const int2 plan = a.plan[b];
     const int parts = plan.y;
     if (parts < 2) return;
-    const int head = blockIdx.x - b * heads, h = head / a.G, column = head - h * a.G;
+    const int head = index - b * heads, h = head / a.G, column = head - h * a.G;
     const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = plan.x * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
-    const int at_row = threadIdx.x / LANES, at = threadIdx.x - at_row * LANES;
+    const int at_row = threadIdx.x / LANES, at = threadIdx.x - at_row * LANES, column0 = slice * 32 * SLICE;      // its first value
     float top = -INFINITY, sum = 0.0f;
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int i0 = 0; i0 < parts; i0 += ROUND) {      // mostly once
@@ -445,7 +465,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
 #pragma unroll
         for (int i = 0; i < KJ_EACH; ++i) {
             const int q = i0 + at_row + i * ROWS;
-            p[i] = at_row < ROWS && q < parts ? reinterpret_cast<const float4*>(a.parts + (first + q * step) * WIDTH)[at] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            p[i] = at_row < ROWS && q < parts ? reinterpret_cast<const float4*>(a.parts + (first + q * step) * WIDTH + column0)[at] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         float most = -INFINITY;
         if (i0 > 0) __syncthreads();
@@ -483,15 +503,13 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
     for (int r = 1; r < ROWS; ++r) sum += row_sums[r];
     const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
     const float* const rows = reinterpret_cast<const float*>(acc);
-    for (int d = threadIdx.x; d < a.D; d += THREADS) {
+    for (int d = threadIdx.x; d < 32 * SLICE && column0 + d < a.D; d += THREADS) {
         float x = 0.0f;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) x += rows[r * WIDTH + d];
-        a.out[b * a.ldo + head * a.ho + d] = (uint16_t)pack_bf16x2(x * inverse, 0.0f);
+        for (int r = 0; r < ROWS; ++r) x += rows[r * 32 * SLICE + d];
+        a.out[b * a.ldo + head * a.ho + column0 + d] = (uint16_t)pack_bf16x2(x * inverse, 0.0f);
     }
 }
-
-constexpr int64_t KJ_ROWS = 512;                     // query heads of all requests up to which the parts are joined by large workgroups
 
 template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool fp32, bool join, int64_t groups, int64_t rows, hipStream_t hs)
 {
@@ -499,13 +517,14 @@ template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool f
     else hipLaunchKernelGGL((k_kv_attend<DT, NS, 1>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
     if (!join) return launch_status();
     if (launch_status() != SS_OK) return SS_ERR_HIP;
-    if (rows <= KJ_ROWS) hipLaunchKernelGGL((k_kv_join<NS, 512>), dim3((uint32_t)rows), dim3(512), 0, hs, a);
-    else hipLaunchKernelGGL((k_kv_join<NS, 128>), dim3((uint32_t)rows), dim3(128), 0, hs, a);
+    if (rows * NS <= cu_count()) hipLaunchKernelGGL((k_kv_join<NS, 1, 512>), dim3((uint32_t)(rows * NS)), dim3(512), 0, hs, a);
+    else if (rows <= 2 * cu_count()) hipLaunchKernelGGL((k_kv_join<NS, NS, 512>), dim3((uint32_t)rows), dim3(512), 0, hs, a);
+    else hipLaunchKernelGGL((k_kv_join<NS, NS, 128>), dim3((uint32_t)rows), dim3(128), 0, hs, a);
     return launch_status();
 }
 
 // Workgroups that all heads' parts come to, about.
-static int64_t wanted_groups() { return 2 * (int64_t)cu_count(); }
+static int64_t wanted_groups(int64_t D) { return (kv_steps(D) == 8 ? 3 : 2) * (int64_t)cu_count(); }
 // bytes of a part of a request: sums and values of all heads
 static int64_t part_bytes(int64_t units, int64_t D) { return units * KA_COLUMNS * (8 + 4 * 32 * kv_steps(D)); }
 // and of the plan that lies before them
@@ -524,7 +543,7 @@ extern "C" size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H,
 {
     if (!valid_attention(B, Hq, H, D) || B == 0) return 0;
     const int64_t units = H * ((Hq / H + KA_COLUMNS - 1) / KA_COLUMNS);
-    return (size_t)(plan_bytes(B) + (wanted_groups() / units + 2 + B) * part_bytes(units, D));
+    return (size_t)(plan_bytes(B) + (wanted_groups(D) / units + 2 + B) * part_bytes(units, D));
 }
 
 extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* table,
@@ -552,7 +571,7 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
     const int64_t units = H * a.tiles;
     // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.
     const int64_t bytes = (int64_t)(workspace_bytes < (size_t)1 << 50 ? workspace_bytes : (size_t)1 << 50) - plan_bytes(B);
-    const int64_t room = bytes / part_bytes(units, D) - B - 2, want = wanted_groups() / units, wanted = room < want ? room : want;
+    const int64_t room = bytes / part_bytes(units, D) - B - 2, want = wanted_groups(D) / units, wanted = room < want ? room : want;
     const bool join = wanted > 1 && W * page > (int64_t)KA_ONE * KV_BLOCK;
     a.division = {lens, (int)B, (int)(W * page), (int)(window < INT32_MAX ? window : 0), join ? 1.0f / (float)wanted : 0.0f};
     a.items = (int)(join ? wanted + 2 + B : B);
