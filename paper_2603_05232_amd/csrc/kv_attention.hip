@@ -42,7 +42,7 @@ __device__ inline int ka_per(const KaDivision& d, const KaSpan& mine)
     for (int b0 = 64; b0 < d.B; b0 += 64) sum += (float)ka_span(d, b0 + lane).blocks;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);      // the same order in every wavefront
-    const float n = sum * d.share;
+    const float n = fminf(sum * d.share, 0x1p30f);       // more than any request has
     return n < 8 * KA_WAVES ? KA_WAVES * max(1, (int)(n * (1.0f / KA_WAVES) + 0.999f)) : (int)n + 1;      // whole rounds of the wavefronts, while these are few
 }
 __device__ inline int ka_parts(int blocks, int per) { return blocks <= per ? 1 : (blocks + per - 1) / per; }

@@ -5,7 +5,7 @@ namespace ss {
 
 constexpr int KT_THREADS = 1024;
 constexpr int KT_CAP = 1 << 30;                      // sums stop here, above any number that means something
-constexpr int64_t KT_ONE_LAUNCH = 8192;              // new tokens up to which the plan's workgroup fills in the slots too
+constexpr int64_t KT_ONE_LAUNCH = 4096;              // new tokens up to which the plan's workgroup fills in the slots too
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
 

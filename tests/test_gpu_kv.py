@@ -68,7 +68,7 @@ def test_tables_of_one_launch_and_of_two():
     lens, want, table, pool, left = step_of(rng, 40, 16, 64, "any")
     total = sum(max(0, w - n) for w, n in zip(want, lens))
     assert 4096 < total < 30000
-    for N in (8192, 8193, total, 1 << 20):
+    for N in (4096, 4097, total, 1 << 20):
         check_tables(lens, want, table, pool, left, 64, N)
 
 
@@ -275,6 +275,35 @@ def test_attention_of_many_requests():
     lens = [int(n) for n in rng.integers(0, 90, 300)] + [4000]
     cache = Cache(rng, lens, 2, 64, 32, "bf16")
     q = queries(301, 6, 64, "bf16")
+    cache.check(cache(q), q)
+
+
+def test_attention_of_4096_requests():
+    """As many as there can be, most of them in the last of the pieces in which lengths are read; some are long enough to be divided."""
+    rng = np.random.default_rng(12)
+    lens = [0 if i % 7 else int(n) for i, n in enumerate(rng.integers(1, 70, 4096))]
+    lens[4095], lens[1000], lens[63] = 3000, 2500, 1
+    cache = Cache(rng, lens, 1, 16, 32, "bf16")
+    q = queries(4096, 3, 16, "bf16")
+    got = cache(q)
+    cache.check(got, q)
+    assert bool((got[[i for i, n in enumerate(lens) if n == 0]] == 0).all())
+
+
+@pytest.mark.parametrize("Hq,H", [(96, 1), (200, 4), (1024, 1024), (1024, 2)])
+def test_attention_of_many_heads(Hq, H):
+    cache = Cache(np.random.default_rng(13), [700, 33], H, 16, 32, "fp8")
+    q = queries(2, Hq, 16, "bf16")
+    cache.check(cache(q), q)
+
+
+def test_requests_that_share_pages():
+    """Two requests whose rows of the table begin with the same pages, as after a common prompt."""
+    cache = Cache(np.random.default_rng(14), [1000, 900], 2, 64, 32, "bf16")
+    cache.table[1, :20] = cache.table[0, :20]
+    cache.k, cache.v = (x.copy() for x in (cache.k, cache.v))
+    cache.k[1000:1640], cache.v[1000:1640] = cache.k[:640], cache.v[:640]
+    q = queries(2, 4, 64, "bf16")
     cache.check(cache(q), q)
 
 
