@@ -11,7 +11,6 @@ namespace ss {
 
 constexpr int KA_WAVES = 4;                          // wavefronts of a workgroup
 constexpr int KA_COLUMNS = 16;                       // query heads of a product
-constexpr int KA_ONE = 16;                           // blocks of a row of the table up to which requests are not divided
 
 typedef uint32_t ka16_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
@@ -97,14 +96,15 @@ struct KaArgs {
     float2* sums;                                    // [item][head of keys][tile][column]: maximum, sum
     float* parts;                                    // the same [.. , 32 NS]: weighted values
     int items;
-    Div by_units, by_blocks;                         // H tiles; blocks of a page
+    Div by_heads, by_round, by_blocks;               // H; 8 tiles; blocks of a page
     KaDivision division;
 };
 
 // wavefronts of a SIMD that registers are kept for
 constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : 2; }
-// DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32)
-template <int DT, int NS, int QP>
+// DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32); ONCE: up to 16 query heads to a head of keys, so that
+// a block is read by one workgroup
+template <int DT, int NS, int QP, bool ONCE>
 __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const KaArgs a)
 {
     constexpr int ES = kv_es(DT), HALF = kv_half_bytes(ES, NS), BLOCK = kv_block_bytes(ES, NS), LOADS = HALF / 1024, NT = 2 * NS, CHUNK = NT < 32 / KA_WAVES ? NT : 32 / KA_WAVES;
@@ -112,7 +112,15 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     __shared__ float4 joined[KA_WAVES][CHUNK][64];
     __shared__ float2 wave_sums[KA_WAVES][KA_COLUMNS];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
-    const int item = quot(blockIdx.x, a.by_units), unit = blockIdx.x - item * a.H * a.tiles, h = unit / a.tiles, tile = unit - h * a.tiles;
+    // Workgroups that read the same blocks follow one another on an XCD, 8 apart, so that its L2 has the blocks for all of them.
+    int at_head = blockIdx.x, tile = 0;
+    if constexpr (!ONCE) {
+        const int round = quot(blockIdx.x, a.by_round), within = blockIdx.x - round * 8 * a.tiles;
+        tile = within >> 3;
+        at_head = round * 8 + (within & 7);
+    }
+    const int item = quot(at_head, a.by_heads), h = at_head - item * a.H, unit = h * a.tiles + tile;
+    if (!ONCE && item >= a.items) return;
 
     // this workgroup's request and its part of it
     int b = -1, part = 0, parts = 1;
@@ -205,9 +213,15 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
         next_valid = id >= 0 && id < a.P;            // no page: nothing to see, whatever is read instead
         from = a.pages + (next_valid ? id : 0) * a.page_bytes + (int64_t)(h * per_page + __builtin_amdgcn_readlane(at_page, i & 63)) * BLOCK;
     };
+    // Blocks that one workgroup reads go past the caches (plain loads: 64 x 16384 ragged 192 us for 171, 256 x 4096 365 for 325); those of more than 16 heads, which several read, do not.
+    auto load16 = [&](const uint8_t* p) {
+        const uint4* const x = reinterpret_cast<const uint4*>(p) + lane;
+        if constexpr (ONCE) return load_once(x);
+        else return *x;
+    };
     auto load_keys = [&]() {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) k[i] = load_once(reinterpret_cast<const uint4*>(from + i * 1024) + lane);
+        for (int i = 0; i < LOADS; ++i) k[i] = load16(from + i * 1024);
         if constexpr (ES == 1) {
             const float4* const scales = reinterpret_cast<const float4*>(from + 2 * HALF) + 2 * j;
             const float4 x = scales[0], y = scales[1];
@@ -216,7 +230,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     };
     auto load_values = [&]() {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) v[i] = load_once(reinterpret_cast<const uint4*>(from + HALF + i * 1024) + lane);
+        for (int i = 0; i < LOADS; ++i) v[i] = load16(from + HALF + i * 1024);
         if constexpr (ES == 1) {
             const float4* const scales = reinterpret_cast<const float4*>(from + 2 * HALF + 4 * KV_BLOCK) + 2 * j;
             const float4 x = scales[0], y = scales[1];
@@ -454,7 +468,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
     const int slice = blockIdx.x % (NS / SLICE), index = blockIdx.x / (NS / SLICE), heads = a.H * a.G, b = index / heads;
     const int2 plan = a.plan[b];
     const int parts = plan.y;
-    if (parts < 2) return;
+    if (parts < 2 || plan.x < 0 || parts > a.items - plan.x) return;      // (the last two only if lengths are changed while they are read)
     const int head = index - b * heads, h = head / a.G, column = head - h * a.G;
     const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = plan.x * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
     const int at_row = threadIdx.x / LANES, at = threadIdx.x - at_row * LANES, column0 = slice * 32 * SLICE;      // its first value
@@ -513,8 +527,9 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
 
 template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool fp32, bool join, int64_t groups, int64_t rows, hipStream_t hs)
 {
-    if (fp32) hipLaunchKernelGGL((k_kv_attend<DT, NS, 2>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
-    else hipLaunchKernelGGL((k_kv_attend<DT, NS, 1>), dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a);
+    auto attend = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(64 * KA_WAVES), 0, hs, a); };
+    if (a.tiles == 1) fp32 ? attend(k_kv_attend<DT, NS, 2, true>) : attend(k_kv_attend<DT, NS, 1, true>);
+    else fp32 ? attend(k_kv_attend<DT, NS, 2, false>) : attend(k_kv_attend<DT, NS, 1, false>);
     if (!join) return launch_status();
     if (launch_status() != SS_OK) return SS_ERR_HIP;
     if (rows * NS <= cu_count()) hipLaunchKernelGGL((k_kv_join<NS, 1, 512>), dim3((uint32_t)(rows * NS)), dim3(512), 0, hs, a);
@@ -525,6 +540,12 @@ template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool f
 
 // Workgroups that all heads' parts come to, about.
 static int64_t wanted_groups(int64_t D) { return (kv_steps(D) == 8 ? 3 : 2) * (int64_t)cu_count(); }
+// Blocks of a row of the table up to which requests are not divided, by the workgroups that they are without.  A division costs the second launch, 4 us; what it saves is that a compute unit draws some
+// 60 GB/s at most.  Not divided | divided, us a pass:
+//   up to 1 for each compute unit   1 x 512 (8 heads of 128) 7.3, 1 x 576 | 10;   8 x 500 9.1, 8 x 576 | 13.1;   1 x 1024 12.3 | 11.9;   1 x 1536 16.9 | 11.9;   8 x 2048 24.8 | 18.3
+//   up to 4                         40 x 1024 33.0 | 34.6;   64 x 1024 44 .. 47 | 49;   64 x 2048 82.8 | 85.5, lengths up to 2048 34.6 | 31.1;   40 x 2048 62.7 | 59.3
+//   more                            200 x up to 1024 52.3 | 57.1;   256 x up to 2048 (4 heads) 64.8 | 68.1;   256 x up to 4096 120 | 112
+static int64_t undivided_blocks(int64_t groups) { return groups <= cu_count() ? 16 : groups <= 4 * cu_count() ? 32 : 64; }
 // bytes of a part of a request: sums and values of all heads
 static int64_t part_bytes(int64_t units, int64_t D) { return units * KA_COLUMNS * (8 + 4 * 32 * kv_steps(D)); }
 // and of the plan that lies before them
@@ -543,7 +564,8 @@ extern "C" size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H,
 {
     if (!valid_attention(B, Hq, H, D) || B == 0) return 0;
     const int64_t units = H * ((Hq / H + KA_COLUMNS - 1) / KA_COLUMNS);
-    return (size_t)(plan_bytes(B) + (wanted_groups(D) / units + 2 + B) * part_bytes(units, D));
+    const int64_t wanted = wanted_groups(D) / units;
+    return wanted > 1 ? (size_t)(plan_bytes(B) + (wanted + 2 + B) * part_bytes(units, D)) : 0;
 }
 
 extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* table,
@@ -572,15 +594,16 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
     // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.
     const int64_t bytes = (int64_t)(workspace_bytes < (size_t)1 << 50 ? workspace_bytes : (size_t)1 << 50) - plan_bytes(B);
     const int64_t room = bytes / part_bytes(units, D) - B - 2, want = wanted_groups(D) / units, wanted = room < want ? room : want;
-    const bool join = wanted > 1 && W * page > (int64_t)KA_ONE * KV_BLOCK;
+    const bool join = wanted > 1 && W * page > undivided_blocks(B * units) * KV_BLOCK;
     a.division = {lens, (int)B, (int)(W * page), (int)(window < INT32_MAX ? window : 0), join ? 1.0f / (float)wanted : 0.0f};
     a.items = (int)(join ? wanted + 2 + B : B);
     a.plan = join ? static_cast<int2*>(workspace) : nullptr;
     a.sums = join ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan_bytes(B)) : nullptr;
     a.parts = join ? reinterpret_cast<float*>(a.sums + a.items * units * KA_COLUMNS) : nullptr;
-    a.by_units = make_div(units);
+    a.by_heads = make_div(H);
+    a.by_round = make_div(8 * a.tiles);
     a.by_blocks = make_div(page / KV_BLOCK);
-    const int64_t groups = a.items * units, rows = B * Hq;
+    const int64_t heads = a.items * H, groups = a.tiles == 1 ? heads : (heads + 7) / 8 * 8 * a.tiles, rows = B * Hq;
     if (!mx4_grid_fits(groups, 64 * KA_WAVES) || !mx4_grid_fits(rows, 128)) return SS_ERR_SHAPE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const bool fp32 = in_dtype == SS_IN_F32;
