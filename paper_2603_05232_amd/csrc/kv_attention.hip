@@ -4,6 +4,15 @@
 //
 // One pass with a running maximum and sum for each head.  A request's blocks of 32 tokens are divided over workgroups, and a workgroup's over its wavefronts; what these hold (maximum,
 // sum, weighted values) is joined in LDS, and what workgroups hold by a second kernel through the caller's workspace.
+//
+// Bound by HBM: each key and value is read once for all query heads of its head (a product has room for 16), 4 D operations a byte pair on matrix cores that could do fifty times that.  A block's products and
+// softmax take some 2500 cycles of a wavefront, so that what counts is bytes under way: a block and a half for each of twelve wavefronts of a compute unit, 16 KB a block of 128 channels.  Medians of a
+// trace: 256 requests of 4096 tokens, 4 heads of 128, bf16 319 us, 6.7 TB/s; 64 of 16384 down to 256 166 (6.3), the same in fp8 92 (5.9); one of 131072 tokens 44.5 (6.0) and 4.6 for the join.  The
+// counters show the cache's bytes read once (2150 MB of 2150).  One physical placement of the pages or another makes up to 15 % (the same call 203 and 234 us).  Requests below some 1000 tokens are bound by
+// the waits at the start (lengths, table, keys, one after the other: 4.7 us for one token) and by what a compute unit draws by itself, 60 GB/s.
+//
+// Tried and left: equal shares of all requests' blocks, a workgroup passing from one request to the next (ragged batches the same, few short requests 30 % slower: the waits follow one another); eight
+// wavefronts a workgroup; the table's first pages asked for beside the lengths (no gain); up to eight times as many parts (join 4 -> 10 us, the stream as it is).
 #include "kv_common.h"
 #include "quant_common.h"
 
@@ -17,7 +26,8 @@ typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t ka16f_t __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- how the blocks are divided ----
-// Lengths are known on the device alone, so every workgroup works the division out for itself: a few loads and sums over the requests.
+// Lengths are known on the device alone, so every workgroup works the division out for itself: a few loads and sums over the requests.  A replayed graph therefore follows lengths that grow, and no
+// workgroup is launched for tokens that the table has room for and no request has.
 struct KaDivision {
     const int32_t* lens;
     int B, most, window;                             // requests; tokens that a row of the table has room for; 0: no window
@@ -100,7 +110,7 @@ struct KaArgs {
     KaDivision division;
 };
 
-// wavefronts of a SIMD that registers are kept for
+// Wavefronts of a SIMD that registers are kept for.  128 channels in fp8 with three of them 92 us for 108 with two (64 requests up to 16384); 256 channels in int8 with two 126 for 146 with one.
 constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : 2; }
 // DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32); ONCE: up to 16 query heads to a head of keys, so that
 // a block is read by one workgroup
@@ -456,6 +466,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 
 // Joins the parts of a request that was divided: a workgroup for each query head of each request, or for each 32 values of it, which leaves where it was not.  SLICE: steps of 32 values of a workgroup,
 // whose rows are 8 lanes wide each.
+// Bound by the launch and three waits, plan, parts and sums, results: 4.0 .. 4.7 us in a trace where nothing is left to join too.  All rows are asked for before their weights are known; one after the
+// other 256 parts of a head took 18 us.  Slices of 32 values for few heads of many parts: 512 parts of 16 heads of 256 6 us for 15 by whole rows.
 constexpr int KJ_EACH = 8;                           // rows that a thread asks for ahead of their weights
 template <int NS, int SLICE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
@@ -538,7 +550,8 @@ template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool f
     return launch_status();
 }
 
-// Workgroups that all heads' parts come to, about.
+// Workgroups that all heads' parts come to, about.  256 channels, where two of a compute unit run at once, 3 | 2 for each: 22 requests of 7079 tokens, 8 heads, 234 | 261 us; 14 of 20177, 4 heads, int8
+// 116 | 123.  128 channels: one request of 131072 tokens 50.9 | 48.9, 64 up to 16384 174 | 170.
 static int64_t wanted_groups(int64_t D) { return (kv_steps(D) == 8 ? 3 : 2) * (int64_t)cu_count(); }
 // Blocks of a row of the table up to which requests are not divided, by the workgroups that they are without.  A division costs the second launch, 4 us; what it saves is that a compute unit draws some
 // 60 GB/s at most.  Not divided | divided, us a pass:

@@ -4,8 +4,10 @@
 namespace ss {
 
 constexpr int KT_THREADS = 1024;
-constexpr int KT_CAP = 1 << 30;                      // sums stop here, above any number that means something
-constexpr int64_t KT_ONE_LAUNCH = 4096;              // new tokens up to which the plan's workgroup fills in the slots too
+constexpr int KT_CAP = (1 << 30) - 1;                // sums stop here, above any number that means something; two of them are still a number of 32 bits
+// New tokens up to which the plan's workgroup fills in the slots too.  One launch | two, us a call: 64 requests, 2048 tokens 6.5 | 8.1, 4096 8.2 | 8.1 .. 8.8, 8192 11.8 | 8.6; one request, 4096 5.4 | 8.4,
+// 8192 6.6 | 8.7; 512 requests, 4096 9.1 | 9.3.
+constexpr int64_t KT_ONE_LAUNCH = 4096;
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
 
@@ -60,7 +62,8 @@ __device__ inline void kt_fill(const int32_t* start, const KtPlan& plan, int i, 
     slots[i] = id >= 0 && id < P ? id * page + row : -1;
 }
 
-// One workgroup.  The requests' numbers are few; bound by the launch and its waits.  Every input is read before the barrier behind which outputs are written, so new_lens may be
+// One workgroup: the requests' numbers are few.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with sums by shuffles through LDS), 256 of a busy
+// step with 65000 new tokens 5.8 and 3.8 for the slots.  Every input is read before the barrier behind which outputs are written, so new_lens may be
 // lens and new_left may be left.
 template <bool WHOLE>
 __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, const int32_t* want, int B, int32_t* table, int64_t ldt, int W, int page, Div by_page, int32_t* pool, int P,
@@ -68,7 +71,7 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
                                                         int32_t* __restrict__ offsets, KtPlan* __restrict__ out)
 {
     __shared__ KtPlan plan;
-    __shared__ int part[2 * (int)(KV_MAX_REQUESTS / KT_THREADS)][3][KT_THREADS / 64];
+    __shared__ int part[2 * (int)(KV_MAX_REQUESTS / KT_THREADS)][2][KT_THREADS / 64];
     __shared__ int taken;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, most = W * page;
     const int free_before = min(max(*left, 0), P);

@@ -81,6 +81,22 @@ def test_tables_of_one_long_request_and_of_lists_that_mean_nothing():
     check_tables([0, 0], [1, 40], np.zeros((2, 2)), np.array([5, -1, 1 << 30, 0]), 4, 32, 50)         # pages that there are not: slots -1
 
 
+def test_tables_of_sums_beyond_32_bits():
+    """Every request wants as many rows as a call can have, so that their sum is 2^31 and more: all but one, which wants none, are left out, and that one keeps its page."""
+    B, W, page, N = 3000, 32769, 32, 1 << 20
+    table = torch.arange(B, dtype=torch.int32, device=DEV)[:, None].repeat(1, W)
+    before = table.clone()
+    lens, want = torch.ones((B,), dtype=torch.int32, device=DEV), torch.full((B,), W * page, dtype=torch.int32, device=DEV)
+    want[B - 1] = 1
+    pool = torch.arange(1 << 22, dtype=torch.int32, device=DEV)
+    got = binding.kv_tables(lens, want, table, pool, i32([1 << 22]), page, N)
+    assert torch.equal(got[0], lens) and got[1].tolist() == [1 << 22] and bool((got[2] == -1).all()) and got[3].tolist() == [0] + [N] * B
+    assert torch.equal(table, before)
+    want[1], want[B - 1] = 3, 0                                    # one that gives a page back; one that is small, but behind a row too many
+    got = binding.kv_tables(lens, want, table, pool, i32([1000]), page, N)
+    assert got[0].tolist() == [1] * (B - 1) + [0] and got[1].tolist() == [1001] and pool[1000].item() == B - 1 and bool((got[2] == -1).all())
+
+
 def test_tables_in_place_and_again():
     """new_lens and new_left may be lens and left; the same call on the same lengths gives the same."""
     rng = np.random.default_rng(4)
@@ -333,6 +349,14 @@ def test_attention_with_strides_and_a_scale(dtype):
     cache.check(got, q, scale=0.7)
     assert bool((out[:, :, 0] == 7).all()) and bool((out[:, :, 1 + D:] == 7).all())
     assert torch.equal(got, cache(q.contiguous(), scale=0.7))
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "i8"])
+def test_attention_of_a_scale_below_and_at_zero(dtype, scale):
+    cache = Cache(np.random.default_rng(15), [600, 40], 2, 64, 32, dtype)
+    q = queries(2, 4, 64, "bf16")
+    cache.check(cache(q, scale=scale), q, scale=float(np.float32(scale)))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "i8", "fp8"])
