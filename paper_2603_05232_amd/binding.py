@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 import sysconfig
 import types
@@ -680,7 +681,7 @@ def kv_attention(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lens
         out = q.new_empty((B, Hq, D), dtype=torch.bfloat16)
     assert out.shape == (B, Hq, D) and out.dtype == torch.bfloat16
     code = load().kv_attention(q.data_ptr(), _in_code(q), *_kv_heads(q, q), at, P, page, DTYPE_CODE[dtype], table.data_ptr(), _row_stride(table, q), table.shape[1],
-                               _dense_i32(lens, "lens", q), B, Hq, heads, D, D ** -0.5 if scale is None else scale, window, out.data_ptr(), *_kv_heads(out, q),
+                               _dense_i32(lens, "lens", q), B, Hq, heads, D, 1 / math.sqrt(D) if scale is None else scale, window, out.data_ptr(), *_kv_heads(out, q),
                                *_workspace(workspace, q), _stream())
     if code:
         _check(code, "kv_attention")
