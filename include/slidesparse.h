@@ -291,7 +291,7 @@ int64_t kv_page_bytes(int64_t H, int64_t page, int64_t D, ss_dtype dtype);      
  *   new_lens[B], new_left[1]   what is so after the call; these may be lens and left
  * A growing request is left out (its length and table row stay, its rows get -1) if it needs more than W pages, if its rows pass N, or if it needs new pages and these, with those that growing requests before it
  * need, are more than the free ones.  Negative lengths count as 0, lens beyond W page as that, left outside 0 .. P as the nearest; a page outside 0 .. P - 1 gives slots -1.
- * table, pool: read and written.  workspace: kv_tables_workspace_bytes(B, N) bytes (0 for up to 4096 rows), 16-byte aligned, SS_ERR_WORKSPACE if there is less. */
+ * table, pool: read and written.  workspace: kv_tables_workspace_bytes(B, N) bytes (0 for up to 2048 rows), 16-byte aligned, SS_ERR_WORKSPACE if there is less. */
 size_t kv_tables_workspace_bytes(int64_t B, int64_t N);
 ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t B, int32_t* table, int64_t ldt, int64_t W, int64_t page, int32_t* pool, int64_t P,
                     const int32_t* left, int64_t N, int32_t* new_lens, int32_t* new_left, int32_t* slots, int32_t* offsets, void* workspace,

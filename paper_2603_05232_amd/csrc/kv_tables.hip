@@ -5,9 +5,9 @@ namespace ss {
 
 constexpr int KT_THREADS = 1024;
 constexpr int KT_CAP = (1 << 30) - 1;                // sums stop here, above any number that means something; two of them are still a number of 32 bits
-// New tokens up to which the plan's workgroup fills in the slots too.  One launch | two, us a call: 64 requests, 2048 tokens 6.5 | 8.1, 4096 8.2 | 8.1 .. 8.8, 8192 11.8 | 8.6; one request, 4096 5.4 | 8.4,
-// 8192 6.6 | 8.7; 512 requests, 4096 9.1 | 9.3.
-constexpr int64_t KT_ONE_LAUNCH = 4096;
+// New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 | 8.4, 2048 6.5 | 6.1 | 8.7,
+// 4096 8.2 | 6.1 | 8.8, 32768 32 | 6.3 | 8.8; one request, 4096 5.4 | 5.5 | 8.6, 32768 17 | 5.5 | 8.6; 512 requests, 4096 9.1 | 6.3 | 9.5.
+constexpr int64_t KT_ONE_LAUNCH = 2048;
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
 
@@ -30,54 +30,67 @@ template <int NUM> __device__ inline void block_scan(int (&v)[NUM], int (*part)[
     }
 }
 
-// What filling in needs of each request.
-struct KtPlan {
-    int32_t start[KV_MAX_REQUESTS + 1];              // its first new token's row
-    int32_t len[KV_MAX_REQUESTS];                    // its length before
-    int32_t first[KV_MAX_REQUESTS];                  // pages taken by requests before it; -1: it gets no slots
+// What filling in needs of each of up to MAX requests.
+template <int MAX> struct KtPlan {
+    int32_t start[MAX + 1];                          // its first new token's row
+    int32_t len[MAX];                                // its length before
+    int32_t first[MAX];                              // pages taken by requests before it; -1: it gets no slots
     int32_t pages;                                   // free pages, those that were given back among them
 };
+constexpr int KT_MAX = (int)KV_MAX_REQUESTS;
 
-// Row i: the request that it belongs to, its position there, its page.  A new page is entered in the table by the row that begins it.
-__device__ inline void kt_fill(const int32_t* start, const KtPlan& plan, int i, int B, int32_t* __restrict__ table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P,
+// the last of 0 .. n - 1 at which a list that does not fall is at most x; 0 if there is none
+__device__ inline int kt_search(const int32_t* list, int n, int x)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (list[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Row i: the request that it belongs to, its position there, its page.  A new page is entered in the table by the row that begins it.  page_at(k): entry k of the stack.
+template <int MAX, typename F>
+__device__ inline void kt_fill(const int32_t* start, const KtPlan<MAX>& plan, int i, int B, int32_t* __restrict__ table, int64_t ldt, int page, Div by_page, F page_at, int P,
                                int32_t* __restrict__ slots)
 {
     if (i >= start[B]) { slots[i] = -1; return; }
-    int lo = 0, hi = B;                              // the last request that begins at or before i
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= i) lo = mid;
-        else hi = mid;
-    }
-    const int first = plan.first[lo];
+    const int b = kt_search(start, B, i), first = plan.first[b];
     if (first < 0) { slots[i] = -1; return; }
-    const int len = plan.len[lo], at = len + (i - start[lo]), column = quot(at, by_page), row = at - column * page, have = quot(len + page - 1, by_page);
-    int32_t* const cell = table + lo * ldt + column;
+    const int len = plan.len[b], at = len + (i - start[b]), column = quot(at, by_page), row = at - column * page, have = quot(len + page - 1, by_page);
+    int32_t* const cell = table + b * ldt + column;
     int id;
     if (column >= have) {
         const int k = plan.pages - 1 - (first + column - have);      // from the top of the stack
-        id = k >= 0 && k < P ? pool[k] : -1;
+        id = k >= 0 && k < P ? page_at(k) : -1;
         if (row == 0) *cell = id;
     } else id = *cell;
     slots[i] = id >= 0 && id < P ? id * page + row : -1;
 }
 
-// One workgroup: the requests' numbers are few.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with sums by shuffles through LDS), 256 of a busy
-// step with 65000 new tokens 5.8 and 3.8 for the slots.  Every input is read before the barrier behind which outputs are written, so new_lens may be
-// lens and new_left may be left.
-template <bool WHOLE>
+// The requests' numbers are few: one workgroup.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with sums by shuffles through LDS).  Every input
+// is read before the barrier behind which outputs are written, so new_lens may be lens and new_left may be left.  With many rows, either
+//   KT_EVERY   every workgroup works the plan out, the first one writes it, each fills in its rows; pages that this call gives back are taken from the table, not from the stack that another workgroup
+//              is writing.  Where new_lens and new_left are memory of their own, for up to 1024 requests.
+//   KT_PLAN    the plan goes through memory to a second launch.
+constexpr int KT_WHOLE = 0, KT_EVERY = 1, KT_PLAN = 2;
+template <int MODE>
 __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, const int32_t* want, int B, int32_t* table, int64_t ldt, int W, int page, Div by_page, int32_t* pool, int P,
                                                         const int32_t* left, int N, int32_t* new_lens, int32_t* new_left, int32_t* __restrict__ slots,
-                                                        int32_t* __restrict__ offsets, KtPlan* __restrict__ out)
+                                                        int32_t* __restrict__ offsets, KtPlan<KT_MAX>* __restrict__ out)
 {
-    __shared__ KtPlan plan;
-    __shared__ int part[2 * (int)(KV_MAX_REQUESTS / KT_THREADS)][2][KT_THREADS / 64];
+    constexpr int MAX = MODE == KT_EVERY ? KT_THREADS : KT_MAX, PER = MAX / KT_THREADS;
+    __shared__ KtPlan<MAX> plan;
+    __shared__ int part[2 * PER][2][KT_THREADS / 64];
     __shared__ int taken;
+    __shared__ int32_t back_from[MODE == KT_EVERY ? MAX : 1], needs[MODE == KT_EVERY ? MAX : 1];      // pages given back by requests before; pages that are kept
+    const bool writes = MODE != KT_EVERY || blockIdx.x == 0;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, most = W * page;
     const int free_before = min(max(*left, 0), P);
     if (threadIdx.x == 0) taken = 0;
     int rows = 0, pages = 0, back = 0;               // sums of the requests before
-    constexpr int PER = (int)KV_MAX_REQUESTS / KT_THREADS;
     int wanted[PER], upto[PER];                      // the thread's requests: length wanted (-1: not possible); pages that are taken up to this one, if it takes any
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
@@ -102,11 +115,12 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
             plan.start[b] = min(end - min(grow, N + 1), N);
             plan.len[b] = l;
             plan.first[b] = up - more;
+            if constexpr (MODE == KT_EVERY) { back_from[b] = given - fewer; needs[b] = need; }
         }
         upto[q] = more > 0 ? up : 0;
         wanted[q] = possible || w <= l ? w : -1;
         // pages given back: sixteen lanes to a request that has any, four of them at a time
-        for (uint64_t has = __ballot(fewer > 0); has;) {
+        for (uint64_t has = writes ? __ballot(fewer > 0) : 0; has;) {
             int at = -1;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
@@ -130,29 +144,40 @@ __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, con
         const bool served = wanted[q] >= 0 && upto[q] <= all_pages;
         if (!served) plan.first[b] = -1;
         else if (upto[q] > 0) atomicMax(&taken, upto[q]);            // whole numbers: the order does not matter
-        new_lens[b] = served ? wanted[q] : plan.len[b];
-        offsets[b] = plan.start[b];
+        if (writes) {
+            new_lens[b] = served ? wanted[q] : plan.len[b];
+            offsets[b] = plan.start[b];
+        }
     }
     __syncthreads();
-    if (threadIdx.x == 0) { offsets[B] = plan.start[B]; *new_left = all_pages - taken; }
-    if constexpr (WHOLE) {
-        for (int i = threadIdx.x; i < N; i += KT_THREADS) kt_fill(plan.start, plan, i, B, table, ldt, page, by_page, pool, P, slots);
-    } else {
+    if (writes && threadIdx.x == 0) { offsets[B] = plan.start[B]; *new_left = all_pages - taken; }
+    if constexpr (MODE == KT_PLAN) {
         for (int b = threadIdx.x; b <= B; b += KT_THREADS) out->start[b] = plan.start[b];
         for (int b = threadIdx.x; b < B; b += KT_THREADS) { out->len[b] = plan.len[b]; out->first[b] = plan.first[b]; }
         if (threadIdx.x == 0) out->pages = plan.pages;
+    } else {
+        auto page_at = [&](int k) -> int32_t {
+            if constexpr (MODE == KT_EVERY) {
+                if (k >= free_before) {
+                    const int b = kt_search(back_from, B, k - free_before);
+                    return table[b * ldt + needs[b] + (k - free_before - back_from[b])];
+                }
+            }
+            return pool[k];
+        };
+        for (int i = blockIdx.x * KT_THREADS + threadIdx.x; i < N; i += gridDim.x * KT_THREADS) kt_fill(plan.start, plan, i, B, table, ldt, page, by_page, page_at, P, slots);
     }
 }
 
-// The same by as many workgroups as the rows fill, for which the plan went through memory.
-__global__ __launch_bounds__(256) void k_kv_slots(const KtPlan* __restrict__ plan, int B, int32_t* table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P, int N,
+// Slots by as many workgroups as the rows fill, for which the plan went through memory.
+__global__ __launch_bounds__(256) void k_kv_slots(const KtPlan<KT_MAX>* __restrict__ plan, int B, int32_t* table, int64_t ldt, int page, Div by_page, const int32_t* __restrict__ pool, int P, int N,
                                                   int32_t* __restrict__ slots)
 {
-    __shared__ int32_t start[KV_MAX_REQUESTS + 1];
+    __shared__ int32_t start[KT_MAX + 1];
     for (int b = threadIdx.x; b <= B; b += 256) start[b] = plan->start[b];
     __syncthreads();
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < N) kt_fill(start, *plan, i, B, table, ldt, page, by_page, pool, P, slots);
+    if (i < N) kt_fill(start, *plan, i, B, table, ldt, page, by_page, [=](int k) { return pool[k]; }, P, slots);
 }
 
 }  // namespace ss
@@ -161,7 +186,7 @@ using namespace ss;
 
 static bool valid_tables(int64_t B, int64_t N) { return B >= 0 && B <= KV_MAX_REQUESTS && N >= 0 && N <= KV_MAX_TOKENS; }
 
-extern "C" size_t kv_tables_workspace_bytes(int64_t B, int64_t N) { return valid_tables(B, N) && N > KT_ONE_LAUNCH ? sizeof(KtPlan) : 0; }
+extern "C" size_t kv_tables_workspace_bytes(int64_t B, int64_t N) { return valid_tables(B, N) && N > KT_ONE_LAUNCH ? sizeof(KtPlan<KT_MAX>) : 0; }
 
 extern "C" ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t B, int32_t* table, int64_t ldt, int64_t W, int64_t page, int32_t* pool, int64_t P, const int32_t* left,
                                int64_t N, int32_t* new_lens, int32_t* new_left, int32_t* slots, int32_t* offsets, void* workspace, size_t workspace_bytes, void* stream)
@@ -174,13 +199,14 @@ extern "C" ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t
     if (((uintptr_t)workspace & 15) || workspace_bytes < need) return SS_ERR_WORKSPACE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const Div by_page = make_div(page);
-    KtPlan* const plan = static_cast<KtPlan*>(workspace);
-    auto args = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(1), dim3(KT_THREADS), 0, hs, lens, want, (int)B, table, ldt, (int)W, (int)page, by_page, pool, (int)P, left, (int)N, new_lens, new_left, slots, offsets, plan);
+    KtPlan<KT_MAX>* const plan = static_cast<KtPlan<KT_MAX>*>(workspace);
+    auto launch = [&](auto kernel, int64_t groups) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(KT_THREADS), 0, hs, lens, want, (int)B, table, ldt, (int)W, (int)page, by_page, pool, (int)P, left, (int)N, new_lens, new_left, slots, offsets, plan);
         return launch_status();
     };
-    if (need == 0) return args(k_kv_plan<true>);
-    if (args(k_kv_plan<false>) != SS_OK) return SS_ERR_HIP;
+    if (need == 0) return launch(k_kv_plan<KT_WHOLE>, 1);
+    if (B <= KT_THREADS && new_lens != lens && new_left != left) return launch(k_kv_plan<KT_EVERY>, (N + KT_THREADS - 1) / KT_THREADS);
+    if (launch(k_kv_plan<KT_PLAN>, 1) != SS_OK) return SS_ERR_HIP;
     hipLaunchKernelGGL(k_kv_slots, dim3((uint32_t)((N + 255) / 256)), dim3(256), 0, hs, plan, (int)B, table, ldt, (int)page, by_page, pool, (int)P, (int)N, slots);
     return launch_status();
 }

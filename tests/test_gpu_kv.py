@@ -63,12 +63,28 @@ def test_tables(B, W, page, kind):
     check_tables(lens, want, table, pool, left, page, total // 2)                                     # rows for half of them
 
 
+def test_tables_whose_new_pages_were_just_given_back():
+    """No free page but those of requests that end or shrink, in the same call, with more rows than one workgroup fills in."""
+    rng = np.random.default_rng(21)
+    B, W, page = 200, 12, 64
+    lens = [int(n) for n in rng.integers(1, W * page + 1, B)]
+    want = [int(rng.choice([0, n // 2, n])) if b % 2 else min(n + int(rng.integers(0, 200)), W * page) for b, n in enumerate(lens)]
+    counts = [-(-n // page) for n in lens]
+    order, table, at = rng.permutation(sum(counts)), np.full((B, W), -1), 0
+    for b, n in enumerate(counts):
+        table[b, :n] = order[at:at + n]
+        at += n
+    N = sum(max(0, w - n) for w, n in zip(want, lens))
+    assert N > 4096 and sum(-(-w // page) for w in want) <= sum(counts)
+    check_tables(lens, want, table, np.zeros(sum(counts)), 0, page, N)
+
+
 def test_tables_of_one_launch_and_of_two():
     rng = np.random.default_rng(9)
     lens, want, table, pool, left = step_of(rng, 40, 16, 64, "any")
     total = sum(max(0, w - n) for w, n in zip(want, lens))
     assert 4096 < total < 30000
-    for N in (4096, 4097, total, 1 << 20):
+    for N in (2048, 2049, total, 1 << 20):
         check_tables(lens, want, table, pool, left, 64, N)
 
 
@@ -97,10 +113,11 @@ def test_tables_of_sums_beyond_32_bits():
     assert got[0].tolist() == [1] * (B - 1) + [0] and got[1].tolist() == [1001] and pool[1000].item() == B - 1 and bool((got[2] == -1).all())
 
 
-def test_tables_in_place_and_again():
+@pytest.mark.parametrize("B,W", [(30, 6), (30, 40), (1024, 9)])
+def test_tables_in_place_and_again(B, W):
     """new_lens and new_left may be lens and left; the same call on the same lengths gives the same."""
     rng = np.random.default_rng(4)
-    lens, want, table, pool, left = step_of(rng, 30, 6, 32, "any")
+    lens, want, table, pool, left = step_of(rng, B, W, 32, "any")
     N = sum(max(0, w - n) for w, n in zip(want, lens)) + 1
     ref = ko.tables(lens, want, table, 32, pool, left, N)
     a = dict(lens=i32(lens), left=i32([left]), table=i32(table), pool=i32(pool))
@@ -464,7 +481,7 @@ def test_calls_through_the_module_and_without_it(monkeypatch):
         pool, left = torch.arange(52, 152, dtype=torch.int32, device=DEV), i32([60])
         pages = torch.zeros((200, binding.kv_page_bytes(2, 64, 64, "i8")), dtype=torch.uint8, device=DEV)
         a = binding.kv_tables(lens, want, table, pool, left, 64, 100)
-        b = binding.kv_tables(lens.clone(), want, table.clone(), pool.clone(), left.clone(), 64, 9000, new_left=left)
+        b = binding.kv_tables(lens.clone(), want, table.clone(), pool.clone(), left.clone(), 64, 9000, new_left=left.clone())
         binding.kv_write(x, x.flip(0), a[2][:92], pages, 64, "i8")
         ws = torch.empty((binding.kv_attention_workspace_bytes(4, 4, 2, 64),), dtype=torch.uint8, device=DEV)
         return [*a, *b, table, pool, left, pages, *binding.kv_read(pages, a[2], 2, 64, 64, "i8"), *binding.kv_read(pages, a[2], 2, 64, 64, "i8", torch.float32),

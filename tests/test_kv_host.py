@@ -24,7 +24,7 @@ def test_sizes():
     assert [size(*a) for a in ((0, 32, 64, "bf16"), (1025, 32, 64, "bf16"), (1, 48, 64, "bf16"), (1, 0, 64, "bf16"), (1, 4128, 64, "bf16"), (1, 32, 0, "bf16"), (1, 32, 257, "bf16"))] == [-1] * 7
     assert binding.load().kv_page_bytes(1, 32, 64, 9) == -1
     w = binding.kv_tables_workspace_bytes
-    assert w(64, 4096) == 0 and w(64, 4097) > 0 and w(4097, 9000) == 0 and w(64, (1 << 20) + 1) == 0
+    assert w(64, 2048) == 0 and w(64, 2049) > 0 and w(4097, 9000) == 0 and w(64, (1 << 20) + 1) == 0
     a = binding.kv_attention_workspace_bytes
     assert a(1, 32, 8, 128) > 0 and a(1, 33, 8, 128) == 0 and a(1, 4, 8, 128) == 0 and a(4097, 8, 8, 128) == 0 and a(1, 8, 8, 257) == 0 and a(0, 8, 8, 64) == 0
     assert a(64, 32, 8, 128) > a(1, 32, 8, 128)
