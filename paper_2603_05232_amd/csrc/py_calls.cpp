@@ -503,8 +503,13 @@ PyObject* py_kv_read(PyObject*, PyObject* const* a, Py_ssize_t n)
     {
         Unlocked u;
         const auto out = pages.options().dtype(type == SS_IN_F32 ? at::kFloat : at::kBFloat16);
-        if (a[7] == Py_None) K = at::empty({N, H, D}, out);
-        if (a[8] == Py_None) V = at::empty({N, H, D}, a[7] == Py_None ? out : THPVariable_Unpack(a[7]).options());
+        if (a[7] == Py_None && a[8] == Py_None) {     // one allocation, both from a 16-byte line on
+            const int64_t n = (N * H * D + 7) & ~(int64_t)7;
+            const at::Tensor both = at::empty({2 * n}, out);
+            K = part(both, 0, {N, H, D}, both.scalar_type());
+            V = part(both, n, {N, H, D}, both.scalar_type());
+        } else if (a[7] == Py_None) K = at::empty({N, H, D}, out);
+        else if (a[8] == Py_None) V = at::empty({N, H, D}, THPVariable_Unpack(a[7]).options());
         const at::Tensor &k = K.defined() ? K : THPVariable_Unpack(a[7]), &v = V.defined() ? V : THPVariable_Unpack(a[8]);
         st = head_rows(k, pages) && head_rows(v, pages) && float_or_bf16(k) && v.scalar_type() == k.scalar_type() && k.size(0) == N && k.size(1) == H && k.size(2) == D && v.sizes() == k.sizes()
                  ? kv.read(pages.data_ptr(), pages.size(0), page, t.code, ints(slots), N, H, D, in_code(k), k.data_ptr(), token_stride(k), head_stride(k), v.data_ptr(), token_stride(v), head_stride(v),

@@ -222,6 +222,17 @@ def test_values_that_are_no_numbers_and_tiny_ones(dtype):
     assert np.array_equal(k.cpu().numpy(), ko.held(x.cpu().numpy(), dtype), equal_nan=True) and np.array_equal(v.cpu().numpy(), ko.held(x.flip(0).cpu().numpy(), dtype), equal_nan=True)
 
 
+def test_no_tokens_and_no_requests():
+    pages = empty_pages(2, 3, 32, 40, "i8")
+    none = torch.zeros((0, 3, 40), device=DEV)
+    binding.kv_write(none, none, i32([]), pages, 32, "i8")
+    for given in ({}, dict(K=none.clone()), dict(V=none.clone())):
+        k, v = binding.kv_read(pages, i32([]), 3, 40, 32, "i8", torch.float32, **given)
+        assert k.shape == v.shape == (0, 3, 40) and k.dtype == v.dtype == torch.float32
+    out = binding.kv_attention(torch.zeros((0, 6, 40), device=DEV), pages, torch.zeros((0, 2), dtype=torch.int32, device=DEV), i32([]), 3, 32, "i8")
+    assert out.shape == (0, 6, 40) and bool((pages == 0).all())
+
+
 # ---- attention ----
 
 class Cache:

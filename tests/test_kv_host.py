@@ -111,3 +111,22 @@ def test_oracle_of_attention():
     e[0, 2] = d
     want = 0.5 * ((p * k[seen, 0][:, 2]) @ v[seen, 0] - (p @ k[seen, 0][:, 2]) * (p @ v[seen, 0]))
     assert np.allclose((f(q + e) - f(q - e)) / (2 * d), want, atol=1e-7)
+
+
+def test_every_call_of_a_cache_has_a_workspace_of_its_own(monkeypatch):
+    """Calls that are under way at once, on streams or in captured graphs, share no memory."""
+    import types
+
+    import torch
+
+    from paper_2603_05232_amd import kv_cache
+    given = []
+    monkeypatch.setattr(kv_cache, "binding", types.SimpleNamespace(kv_page_bytes=lambda *a: 64, kv_attention_workspace_bytes=lambda B, Hq, H, D: 1000,
+                                                                   kv_attention=lambda *a, workspace=None, **kw: given.append(workspace)))
+    cache = kv_cache.PagedCache("cpu", 3, 5, 2, 2, 16)
+    assert cache.pool.tolist() == [4, 3, 2, 1, 0] and cache.left.tolist() == [5] and cache.lens.tolist() == [0, 0, 0]
+    for _ in range(3):
+        cache.attend(torch.zeros((3, 4, 16)))
+    spans = [(w.data_ptr(), w.data_ptr() + w.numel()) for w in given]
+    assert all(w.dtype == torch.uint8 and w.numel() >= 1000 for w in given) and all(a[1] <= b[0] or b[1] <= a[0] for i, a in enumerate(spans) for b in spans[:i])
+    assert not any(w is v for w in given for v in vars(cache).values())
