@@ -274,23 +274,27 @@ ss_status expert_combine(const void* Y, int64_t R, int64_t O, int64_t ldy, const
 /* ---- A paged cache of keys and values, for decoding --------------------------------------------------------------------------------
  * Beyond the paper: what a transformer block needs around the linear layers to decode one token of each of B requests.
  *
- * Pages.  A page holds `page` tokens (a multiple of 32, up to 4096) of H heads (1 .. 1024) of D values (1 .. 256) each, keys and values, kv_page_bytes() bytes in a layout of
- * this library (ordered for the matrix instruction's operands; written by kv_write, read back by kv_read).  `pages` is P of them one after the other, 16-byte aligned.  Slot id * page + r is row
- * r of page id; P page < 2^31.  table[B,W] (int32, row stride ldt) names the pages of each request in order: column i holds the page of its tokens i page .. i page + page - 1.
- * dtype is what the cache holds: SS_BF16 and SS_FP16 keep values rounded to nearest even; SS_I8 and SS_FP8_E4M3 keep, of each token and head, codes clamp(rne(x r)) with
- * a = max|x|, Qmax = 127 or 448 and r = Qmax * (1 / a) in fp32, and a scale a / Qmax (a below 2^-100: scale 1, codes 0; an infinity or a NaN among the values: a scale that is a NaN).
- * Limits: B <= 4096 requests, N <= 2^20 rows of new tokens a call, and the threads of a launch in 32 bits as above.  Nothing in the device arrays (lengths, tables, slots, lists) can lead a kernel out
- * of bounds: what each call does with an entry that means nothing is said there. */
+ * Pages.  A page holds `page` tokens (a multiple of 32, up to 4096) of H heads (1 .. 1024) of D values (1 .. 256) each, keys and values, kv_page_bytes() bytes in a
+ * layout of this library (ordered for the matrix instruction's operands; written by kv_write, read back by kv_read).  `pages` is P of them one after the other, 16-byte
+ * aligned.  Slot id * page + r is row r of page id; P page < 2^31.  table[B,W] (int32, row stride ldt) names the pages of each request in order: column i holds the
+ * page of its tokens i page .. i page + page - 1.
+ * dtype is what the cache holds: SS_BF16 and SS_FP16 keep values rounded to nearest even; SS_I8 and SS_FP8_E4M3 keep, of each token and head, codes clamp(rne(x r))
+ * with a = max|x|, Qmax = 127 or 448 and r = Qmax * (1 / a) in fp32, and a scale a / Qmax (a below 2^-100: scale 1, codes 0; an infinity or a NaN among the values: a
+ * scale that is a NaN).
+ * Limits: B <= 4096 requests, N <= 2^20 rows of new tokens a call, and the threads of a launch in 32 bits as above.  Nothing in the device arrays (lengths, tables,
+ * slots, lists) can lead a kernel out of bounds: what each call does with an entry that means nothing is said there. */
 int64_t kv_page_bytes(int64_t H, int64_t page, int64_t D, ss_dtype dtype);      /* -1 on a bad argument */
 
 /* Pages for requests whose lengths change from lens[B] to want[B] tokens, and slots for their new tokens.
  *   free pages   the stack pool[0 .. left - 1] (pool has room for P entries).  Requests that shrink give back the pages that they no longer reach (in the order of requests, then of columns:
- *                pool[left], pool[left + 1], ..); then requests that grow take pages from the top, in the same order, and their table rows get them.  Other entries stay as they are.
+ *                pool[left], pool[left + 1], ..); then requests that grow take pages from the top, in the same order, and their table rows get them.  Other entries stay
+ *                as they are.  Nothing counts the requests that name a page: one in the rows of several is given back by each of them that no longer reaches it.
  *   rows         the new tokens of all requests one after the other: those of request b are rows offsets[b] .. offsets[b + 1] - 1 (offsets[B + 1], written; want[b] - lens[b] rows, or none)
  *   slots[N]     of each row; -1 behind offsets[B] (a padded batch) and for requests that are left out
  *   new_lens[B], new_left[1]   what is so after the call; these may be lens and left
- * A growing request is left out (its length and table row stay, its rows get -1) if it needs more than W pages, if its rows pass N, or if it needs new pages and these, with those that growing requests before it
- * need, are more than the free ones.  Negative lengths count as 0, lens beyond W page as that, left outside 0 .. P as the nearest; a page outside 0 .. P - 1 gives slots -1.
+ * A growing request is left out (its length and table row stay, its rows get -1) if it needs more than W pages, if its rows pass N, or if it needs new pages and these,
+ * with those that growing requests before it need, are more than the free ones.  Negative lengths count as 0, lens beyond W page as that, left outside 0 .. P as the
+ * nearest; a page outside 0 .. P - 1 gives slots -1.
  * table, pool: read and written.  workspace: kv_tables_workspace_bytes(B, N) bytes (0 for up to 2048 rows), 16-byte aligned, SS_ERR_WORKSPACE if there is less. */
 size_t kv_tables_workspace_bytes(int64_t B, int64_t N);
 ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t B, int32_t* table, int64_t ldt, int64_t W, int64_t page, int32_t* pool, int64_t P,
@@ -307,11 +311,12 @@ ss_status kv_read(const void* pages, int64_t P, int64_t page, ss_dtype dtype, co
                   void* K, int64_t ldk, int64_t hk, void* V, int64_t ldv, int64_t hv, void* stream);
 
 /* out[b,i] = bf16(sum of p_t v_t / sum of p_t), p_t = exp(scale q[b,i] . k_t), over the cached tokens t of request b, head i / (Hq / H): t < lens[b], and t >= lens[b] - window where
- * window > 0.  Q[B,Hq,D] fp32 or bf16 (requests ldq, heads hq elements apart), out[B,Hq,D] bf16 (ldo, ho).  Hq is a multiple of H, at most 1024.  Scores, sums of probabilities and weighted
- * values in fp32, keys and values as the cache holds them; queries of 32 bits as two pieces of the cache's 16-bit type (SS_FP16: half, else bf16: 16 bits in all).  No token to see: zeros, also where all scores are minus infinity.  Lengths are
- * moved into 0 .. W page; tokens of a page outside 0 .. P - 1 are not seen.  What lies in a page behind a request's tokens does not matter, NaNs included.
- * workspace: as for slide_sparse_gemm_ws, kv_attention_workspace_bytes() bytes let long requests be divided over the chip (the division follows the lengths on the device); without it each head of a request
- * is one workgroup's.  Every call with the same arguments gives the same bits. */
+ * window > 0.  Q[B,Hq,D] fp32 or bf16 (requests ldq, heads hq elements apart), out[B,Hq,D] bf16 (ldo, ho).  Hq is a multiple of H, at most 1024.  Scores, sums of
+ * probabilities and weighted values in fp32, keys and values as the cache holds them; queries of 32 bits as two pieces of the cache's 16-bit type (SS_FP16: half, else
+ * bf16: 16 bits in all).  No token to see: zeros, also where all scores are minus infinity.  Lengths are moved into 0 .. W page; tokens of a page outside 0 .. P - 1
+ * are not seen.  What lies in a page behind a request's tokens does not matter, NaNs included.
+ * workspace: as for slide_sparse_gemm_ws, kv_attention_workspace_bytes() bytes let long requests be divided over the chip (the division follows the lengths on the
+ * device); without it each head of a request is one workgroup's.  Every call with the same arguments gives the same bits. */
 size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H, int64_t D);
 ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype,
                        const int32_t* table, int64_t ldt, int64_t W, const int32_t* lens, int64_t B, int64_t Hq, int64_t H, int64_t D, float scale,

@@ -2,17 +2,19 @@
 //
 //   out[b, head] = sum over t of p_t v_t / sum over t of p_t,   p_t = exp(scale q . k_t - m),   t in [max(0, len - window), len)
 //
-// One pass with a running maximum and sum for each head.  A request's blocks of 32 tokens are divided over workgroups, and a workgroup's over its wavefronts; what these hold (maximum,
-// sum, weighted values) is joined in LDS, and what workgroups hold by a second kernel through the caller's workspace.
+// One pass with a running maximum and sum for each head.  A request's blocks of 32 tokens are divided over workgroups, and a workgroup's over its wavefronts; what
+// these hold (maximum, sum, weighted values) is joined in LDS, and what workgroups hold by a second kernel through the caller's workspace.
 //
-// Bound by HBM: each key and value is read once for all query heads of its head (a product has room for 16), 4 D operations a byte pair on matrix cores that could do fifty times that.  A block's products and
-// softmax take some 2500 cycles of a wavefront, so that what counts is bytes under way: a block and a half for each of twelve wavefronts of a compute unit, 16 KB a block of 128 channels.  Medians of a
-// trace: 256 requests of 4096 tokens, 4 heads of 128, bf16 319 us, 6.7 TB/s; 64 of 16384 down to 256 166 (6.3), the same in fp8 92 (5.9); one of 131072 tokens 44.5 (6.0) and 4.6 for the join.  The
-// counters show the cache's bytes read once (2150 MB of 2150).  One physical placement of the pages or another makes up to 15 % (the same call 203 and 234 us).  Requests below some 1000 tokens are bound by
-// the waits at the start (lengths, table, keys, one after the other: 4.7 us for one token) and by what a compute unit draws by itself, 60 GB/s.
+// Bound by HBM: each key and value is read once for all query heads of its head (a product has room for 16), 4 D operations a byte pair on matrix cores that could do
+// fifty times that.  A block's products and softmax take some 2500 cycles of a wavefront, so that what counts is bytes under way: a block and a half for each of twelve
+// wavefronts of a compute unit, 16 KB a block of 128 channels.  Medians of a trace: 256 requests of 4096 tokens, 4 heads of 128, bf16 319 us, 6.7 TB/s; 64 of 16384
+// down to 256 166 (6.3), the same in fp8 92 (5.9); one of 131072 tokens 44.5 (6.0) and 4.6 for the join.  The counters show the cache's bytes read once (2150 MB of
+// 2150).  One physical placement of the pages or another makes up to 15 % (the same call 203 and 234 us).  Requests below some 1000 tokens are bound by the waits at
+// the start (lengths, table, keys, one after the other: 4.7 us for one token) and by what a compute unit draws by itself, 60 GB/s.
 //
-// Tried and left: equal shares of all requests' blocks, a workgroup passing from one request to the next (ragged batches the same, few short requests 30 % slower: the waits follow one another); eight
-// wavefronts a workgroup; the table's first pages asked for beside the lengths (no gain); up to eight times as many parts (join 4 -> 10 us, the stream as it is).
+// Tried and left: equal shares of all requests' blocks, a workgroup passing from one request to the next (ragged batches the same, few short requests 30 % slower: the
+// waits follow one another); eight wavefronts a workgroup; the table's first pages asked for beside the lengths (no gain); up to eight times as many parts (join 4 ->
+// 10 us, the stream as it is).
 #include "kv_common.h"
 #include "quant_common.h"
 
@@ -26,8 +28,8 @@ typedef uint32_t ka8_t __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t ka16f_t __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- how the blocks are divided ----
-// Lengths are known on the device alone, so every workgroup works the division out for itself: a few loads and sums over the requests.  A replayed graph therefore follows lengths that grow, and no
-// workgroup is launched for tokens that the table has room for and no request has.
+// Lengths are known on the device alone, so every workgroup works the division out for itself: a few loads and sums over the requests.  A replayed graph therefore
+// follows lengths that grow, and no workgroup is launched for tokens that the table has room for and no request has.
 struct KaDivision {
     const int32_t* lens;
     int B, most, window;                             // requests; tokens that a row of the table has room for; 0: no window
@@ -110,10 +112,11 @@ struct KaArgs {
     KaDivision division;
 };
 
-// Wavefronts of a SIMD that registers are kept for.  128 channels in fp8 with three of them 92 us for 108 with two (64 requests up to 16384); 256 channels in int8 with two 126 for 146 with one.
+// Wavefronts of a SIMD that registers are kept for.  128 channels in fp8 with three of them 92 us for 108 with two (64 requests up to 16384); 256 channels in int8 with
+// two 126 for 146 with one.
 constexpr int ka_fit(int ns) { return ns <= 4 ? 3 : 2; }
-// DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32); ONCE: up to 16 query heads to a head of keys, so that
-// a block is read by one workgroup
+// DT: the cache's type; NS: steps of 32 values of a head; QP: pieces that a query value is taken apart into (1: bf16, 2: fp32); ONCE: up to 16 query heads to a head of
+// keys, so that a block is read by one workgroup
 template <int DT, int NS, int QP, bool ONCE>
 __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const KaArgs a)
 {
@@ -160,8 +163,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     if (a.plan && part == 0 && unit == 0 && threadIdx.x == 0) a.plan[b] = make_int2(item, parts);
     const int each = (span.blocks + parts - 1) / parts, lo = span.first + part * each, end = min(lo + each, span.first + span.blocks);
 
-    // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.  Long heads are shared out among the wavefronts, which leave their operands in LDS:
-    // all of them would take the registers that a second wavefront of the SIMD needs.
+    // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.  Long heads are shared out among the wavefronts,
+    // which leave their operands in LDS: all of them would take the registers that a second wavefront of the SIMD needs.
     constexpr bool SHARED = NS > 4;
     constexpr int OWN = SHARED ? (NS + KA_WAVES - 1) / KA_WAVES : NS;
     __shared__ v4i shared_q[SHARED ? QP : 1][SHARED ? NS : 1][64];
@@ -205,8 +208,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     }
     const int per_page = a.page / KV_BLOCK;
     const int32_t* const row = a.table + b * a.ldt;
-    // This wavefront's blocks are first, first + KA_WAVES, ..: lane i holds the page of the i-th of 64 of them.  The keys of the next block are asked for when those of this one have
-    // been multiplied, the values likewise, into the same registers: a block is always under way.
+    // This wavefront's blocks are first, first + KA_WAVES, ..: lane i holds the page of the i-th of 64 of them.  The keys of the next block are asked for when those of
+    // this one have been multiplied, the values likewise, into the same registers: a block is always under way.
     const int first = lo + wave, blocks = first < end ? (end - first + KA_WAVES - 1) / KA_WAVES : 0;
     int ids = 0, at_page = 0;                        // at_page: this lane's block of its page
     bool valid = false, next_valid = false;
@@ -223,7 +226,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
         next_valid = id >= 0 && id < a.P;            // no page: nothing to see, whatever is read instead
         from = a.pages + (next_valid ? id : 0) * a.page_bytes + (int64_t)(h * per_page + __builtin_amdgcn_readlane(at_page, i & 63)) * BLOCK;
     };
-    // Blocks that one workgroup reads go past the caches (plain loads: 64 x 16384 ragged 192 us for 171, 256 x 4096 365 for 325); those of more than 16 heads, which several read, do not.
+    // Blocks that one workgroup reads go past the caches (plain loads: 64 x 16384 ragged 192 us for 171, 256 x 4096 365 for 325); those of more than 16 heads, which
+    // several read, do not.
     auto load16 = [&](const uint8_t* p) {
         const uint4* const x = reinterpret_cast<const uint4*>(p) + lane;
         if constexpr (ONCE) return load_once(x);
@@ -464,10 +468,10 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     }
 }
 
-// Joins the parts of a request that was divided: a workgroup for each query head of each request, or for each 32 values of it, which leaves where it was not.  SLICE: steps of 32 values of a workgroup,
-// whose rows are 8 lanes wide each.
-// Bound by the launch and three waits, plan, parts and sums, results: 4.0 .. 4.7 us in a trace where nothing is left to join too.  All rows are asked for before their weights are known; one after the
-// other 256 parts of a head took 18 us.  Slices of 32 values for few heads of many parts: 512 parts of 16 heads of 256 6 us for 15 by whole rows.
+// Joins the parts of a request that was divided: a workgroup for each query head of each request, or for each 32 values of it, which leaves where it was not.  SLICE:
+// steps of 32 values of a workgroup, whose rows are 8 lanes wide each.  Bound by the launch and three waits, plan, parts and sums, results: 4.0 .. 4.7 us in a trace
+// where nothing is left to join too.  All rows are asked for before their weights are known; one after the other 256 parts of a head took 18 us.  Slices of 32 values
+// for few heads of many parts: 512 parts of 16 heads of 256 6 us for 15 by whole rows.
 constexpr int KJ_EACH = 8;                           // rows that a thread asks for ahead of their weights
 template <int NS, int SLICE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
@@ -550,11 +554,11 @@ template <int DT, int NS> static ss_status launch_attend(const KaArgs& a, bool f
     return launch_status();
 }
 
-// Workgroups that all heads' parts come to, about.  256 channels, where two of a compute unit run at once, 3 | 2 for each: 22 requests of 7079 tokens, 8 heads, 234 | 261 us; 14 of 20177, 4 heads, int8
-// 116 | 123.  128 channels: one request of 131072 tokens 50.9 | 48.9, 64 up to 16384 174 | 170.
+// Workgroups that all heads' parts come to, about.  256 channels, where two of a compute unit run at once, 3 | 2 for each: 22 requests of 7079 tokens, 8 heads, 234 |
+// 261 us; 14 of 20177, 4 heads, int8 116 | 123.  128 channels: one request of 131072 tokens 50.9 | 48.9, 64 up to 16384 174 | 170.
 static int64_t wanted_groups(int64_t D) { return (kv_steps(D) == 8 ? 3 : 2) * (int64_t)cu_count(); }
-// Blocks of a row of the table up to which requests are not divided, by the workgroups that they are without.  A division costs the second launch, 4 us; what it saves is that a compute unit draws some
-// 60 GB/s at most.  Not divided | divided, us a pass:
+// Blocks of a row of the table up to which requests are not divided, by the workgroups that they are without.  A division costs the second launch, 4 us; what it saves
+// is that a compute unit draws some 60 GB/s at most.  Not divided | divided, us a pass:
 //   up to 1 for each compute unit   1 x 512 (8 heads of 128) 7.3, 1 x 576 | 10;   8 x 500 9.1, 8 x 576 | 13.1;   1 x 1024 12.3 | 11.9;   1 x 1536 16.9 | 11.9;   8 x 2048 24.8 | 18.3
 //   up to 4                         40 x 1024 33.0 | 34.6;   64 x 1024 44 .. 47 | 49;   64 x 2048 82.8 | 85.5, lengths up to 2048 34.6 | 31.1;   40 x 2048 62.7 | 59.3
 //   more                            200 x up to 1024 52.3 | 57.1;   256 x up to 2048 (4 heads) 64.8 | 68.1;   256 x up to 4096 120 | 112

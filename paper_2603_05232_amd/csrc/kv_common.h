@@ -1,7 +1,8 @@
 // A paged cache of keys and values: its layout, and what its kernels share.
 //
-// A page holds `page` tokens (a multiple of 32) of every head, head by head, in blocks of 32 tokens.  A block is what one step of the attention reads: the keys and the values of
-// 32 tokens as operands of the 16x16x32 instruction, so that every load of a wavefront is one run of 1024 bytes, 16 to a lane.  D is completed to kv_steps(D) 32 values.
+// A page holds `page` tokens (a multiple of 32) of every head, head by head, in blocks of 32 tokens.  A block is what one step of the attention reads: the keys and the
+// values of 32 tokens as operands of the 16x16x32 instruction, so that every load of a wavefront is one run of 1024 bytes, 16 to a lane.  D is completed to kv_steps(D)
+// 32 values.
 //
 // Scores are K Q^T, 16 tokens x 16 heads in two products t = 0, 1: lane (r, j) = (l & 15, l >> 4) holds 8 values 32 s + 8 j .. + 7 of token row r, and gets the scores of rows
 // 4 j .. 4 j + 3 of head r.  Row r of product t is token 8 (r >> 2) + 4 t + (r & 3), so a lane's eight scores are those of tokens 8 j .. 8 j + 7: just what it has to

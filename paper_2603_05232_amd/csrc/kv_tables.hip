@@ -5,8 +5,8 @@ namespace ss {
 
 constexpr int KT_THREADS = 1024;
 constexpr int KT_CAP = (1 << 30) - 1;                // sums stop here, above any number that means something; two of them are still a number of 32 bits
-// New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 | 8.4, 2048 6.5 | 6.1 | 8.7,
-// 4096 8.2 | 6.1 | 8.8, 32768 32 | 6.3 | 8.8; one request, 4096 5.4 | 5.5 | 8.6, 32768 17 | 5.5 | 8.6; 512 requests, 4096 9.1 | 6.3 | 9.5.
+// New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 |
+// 8.4, 2048 6.5 | 6.1 | 8.7, 4096 8.2 | 6.1 | 8.8, 32768 32 | 6.3 | 8.8; one request, 4096 5.4 | 5.5 | 8.6, 32768 17 | 5.5 | 8.6; 512 requests, 4096 9.1 | 6.3 | 9.5.
 constexpr int64_t KT_ONE_LAUNCH = 2048;
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
@@ -70,10 +70,11 @@ __device__ inline void kt_fill(const int32_t* start, const KtPlan<MAX>& plan, in
     slots[i] = id >= 0 && id < P ? id * page + row : -1;
 }
 
-// The requests' numbers are few: one workgroup.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with sums by shuffles through LDS).  Every input
-// is read before the barrier behind which outputs are written, so new_lens may be lens and new_left may be left.  With many rows, either
-//   KT_EVERY   every workgroup works the plan out, the first one writes it, each fills in its rows; pages that this call gives back are taken from the table, not from the stack that another workgroup
-//              is writing.  Where new_lens and new_left are memory of their own, for up to 1024 requests.
+// The requests' numbers are few: one workgroup.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with
+// sums by shuffles through LDS).  Every input is read before the barrier behind which outputs are written, so new_lens may be lens and new_left may be left.  With many
+// rows, either
+//   KT_EVERY   every workgroup works the plan out, the first one writes it, each fills in its rows; pages that this call gives back are taken from the table, not from
+//              the stack that another workgroup is writing.  Where new_lens and new_left are memory of their own, for up to 1024 requests.
 //   KT_PLAN    the plan goes through memory to a second launch.
 constexpr int KT_WHOLE = 0, KT_EVERY = 1, KT_PLAN = 2;
 template <int MODE>

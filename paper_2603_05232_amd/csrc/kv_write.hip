@@ -1,7 +1,8 @@
 // kv_write, kv_read: keys and values of tokens into the pages of a cache, quantised on the way, and out of them again.
 //
-// Bound by HBM where there are many tokens, 8192 tokens of 8 heads of 128, bf16 to fp8: 10.4 us (33.9 MB read, 17.3 written, 4.9 TB/s) and back 9.9 us, and by three waits one after the other (slots, rows, stores;
-// 2.8 us) where there are few.  Values by single elements throughout took 17 us: a store of one byte for each channel of a token.
+// Bound by HBM where there are many tokens, 8192 tokens of 8 heads of 128, bf16 to fp8: 10.4 us (33.9 MB read, 17.3 written, 4.9 TB/s) and back 9.9 us, and by three
+// waits one after the other (slots, rows, stores; 2.8 us) where there are few.  Values by single elements throughout took 17 us: a store of one byte for each channel
+// of a token.
 #include "kv_common.h"
 #include "quant_common.h"
 
@@ -13,8 +14,8 @@ constexpr int KW_WAVES = 4;                          // wavefronts of a workgrou
 typedef uint32_t kv16_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t kv16f_t __attribute__((ext_vector_type(4), aligned(4)));
 
-// Piece c of a row of D values, 8 c .. 8 c + 7, as it lies in memory; zeros behind the row.  Whole pieces are asked for first, all of them, and what is left of a row afterwards: a branch between two
-// loads makes the second wait for the first.
+// Piece c of a row of D values, 8 c .. 8 c + 7, as it lies in memory; zeros behind the row.  Whole pieces are asked for first, all of them, and what is left of a row
+// afterwards: a branch between two loads makes the second wait for the first.
 template <typename T> struct KvPiece { uint32_t w[2 * sizeof(T)]; };
 __device__ inline void kv_get_whole(const uint16_t* p, int c, int D, KvPiece<uint16_t>& x)
 {
@@ -140,8 +141,8 @@ template <int DT> __device__ inline void kv_values8(uint4 v, float s, float (&f)
     }
 }
 
-// Scale and its inverse from the largest magnitude's bits.  Magnitudes below 2^-100 count as zero, so that the inverse is finite; an infinity or a NaN makes the scale a NaN, and
-// with it every product.
+// Scale and its inverse from the largest magnitude's bits.  Magnitudes below 2^-100 count as zero, so that the inverse is finite; an infinity or a NaN makes the scale
+// a NaN, and with it every product.
 __device__ inline void kv_scale(uint32_t largest, float qmax, float& scale, float& inverse)
 {
     const float a = __uint_as_float(largest);
@@ -158,8 +159,8 @@ __device__ inline int64_t kv_block_of(int slot, int h, int H, int page, Div by_p
     return id * page_bytes + (int64_t)(h * (page / KV_BLOCK) + row / KV_BLOCK) * block_bytes;
 }
 
-// Which of a wavefront's eight tokens base .. base + 7 lie in a whole group: eight tokens side by side whose slots are consecutive from a multiple of 8 on, so that they are all that the
-// cache holds of these eight slots.  Lane l holds the slot of token base - 8 + l, l < 24; the group's first token may lie before or behind base.
+// Which of a wavefront's eight tokens base .. base + 7 lie in a whole group: eight tokens side by side whose slots are consecutive from a multiple of 8 on, so that
+// they are all that the cache holds of these eight slots.  Lane l holds the slot of token base - 8 + l, l < 24; the group's first token may lie before or behind base.
 struct KwGroups {
     int slot;                                        // of token base + (lane >> 3); -1: none
     bool grouped;                                    // whether that one lies in a whole group
@@ -198,9 +199,9 @@ __device__ inline void kw_wave_sync()                // what the wavefront's lan
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// A wavefront takes eight tokens of one head: lane (i, c) = (l >> 3, l & 7) the pieces of 8 values c, c + 8, .. of token i.  First the whole group that begins among its tokens, if any, then
-// those that lie in none.  Keys are stored by pieces.  Of values a whole group's eight tokens are turned in LDS, so that a lane stores the eight tokens of a channel at once; others are stored
-// by single elements.  CH: pieces of a lane.
+// A wavefront takes eight tokens of one head: lane (i, c) = (l >> 3, l & 7) the pieces of 8 values c, c + 8, .. of token i.  First the whole group that begins among
+// its tokens, if any, then those that lie in none.  Keys are stored by pieces.  Of values a whole group's eight tokens are turned in LDS, so that a lane stores the
+// eight tokens of a channel at once; others are stored by single elements.  CH: pieces of a lane.
 template <typename T, int DT, int CH>
 __global__ __launch_bounds__(64 * KW_WAVES) void k_kv_write(const T* __restrict__ K, const T* __restrict__ V, int64_t ldk, int64_t hk, int64_t ldv, int64_t hv, const int32_t* __restrict__ slots,
                                                             int N, int H, int D, int steps, uint8_t* __restrict__ pages, int slots_end, int page, Div by_page, int64_t page_bytes, Div by_heads)
