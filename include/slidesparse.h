@@ -291,7 +291,8 @@ int64_t kv_page_bytes(int64_t H, int64_t page, int64_t D, ss_dtype dtype);      
  *                as they are.  Nothing counts the requests that name a page: one in the rows of several is given back by each of them that no longer reaches it.
  *   rows         the new tokens of all requests one after the other: those of request b are rows offsets[b] .. offsets[b + 1] - 1 (offsets[B + 1], written; want[b] - lens[b] rows, or none)
  *   slots[N]     of each row; -1 behind offsets[B] (a padded batch) and for requests that are left out
- *   new_lens[B], new_left[1]   what is so after the call; these may be lens and left
+ *   new_lens[B], new_left[1]   what is so after the call; these may be lens and left, and otherwise lie in the memory of lens, want and left too.  Beyond that no
+ *                two of the arrays share memory (slots or offsets that do with lens, want, left, new_lens, new_left or one another: SS_ERR_SHAPE)
  * A growing request is left out (its length and table row stay, its rows get -1) if it needs more than W pages, if its rows pass N, or if it needs new pages and these,
  * with those that growing requests before it need, are more than the free ones.  Negative lengths count as 0, lens beyond W page as that, left outside 0 .. P as the
  * nearest; a page outside 0 .. P - 1 gives slots -1.

@@ -36,6 +36,25 @@ inline int64_t kv_bytes_of_page(int64_t H, int64_t page, int64_t D, int dtype) {
 // slots and positions are counted in 32 bits
 inline bool kv_valid_slots(int64_t pages, int64_t page) { return pages >= 1 && pages <= INT32_MAX / page; }
 
+// ---- kv_tables: by how many launches ----
+constexpr int KT_THREADS = 1024;
+// New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 |
+// 8.4, 2048 6.5 | 6.1 | 8.7, 4096 8.2 | 6.1 | 8.8, 32768 32 | 6.3 | 8.8; one request, 4096 5.4 | 5.5 | 8.6, 32768 17 | 5.5 | 8.6; 512 requests, 4096 9.1 | 6.3 | 9.5.
+constexpr int64_t KT_ONE_LAUNCH = 2048;
+constexpr int KT_WHOLE = 0, KT_EVERY = 1, KT_PLAN = 2;      // one workgroup; every workgroup plans; the plan goes through memory to a second launch
+
+// whether lists of n and m numbers of 32 bits have memory in common
+inline bool kv_overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) { return n > 0 && m > 0 && (uintptr_t)a < (uintptr_t)(b + m) && (uintptr_t)b < (uintptr_t)(a + n); }
+
+// Where every workgroup plans, the first one writes new_lens and new_left while others may still read lens, want and left: only if no memory is both.
+inline int kt_route(const int32_t* lens, const int32_t* want, int64_t B, const int32_t* left, int64_t N, const int32_t* new_lens, const int32_t* new_left)
+{
+    if (N <= KT_ONE_LAUNCH) return KT_WHOLE;
+    const bool apart = !kv_overlap(new_lens, B, lens, B) && !kv_overlap(new_lens, B, want, B) && !kv_overlap(new_lens, B, left, 1) && !kv_overlap(new_left, 1, lens, B) &&
+                       !kv_overlap(new_left, 1, want, B) && !kv_overlap(new_left, 1, left, 1);
+    return B <= KT_THREADS && apart ? KT_EVERY : KT_PLAN;
+}
+
 // where 8-value piece c (values 8 c .. 8 c + 7) of a token's key lies in its block, for token tau of the block
 __device__ inline int kv_key_at(int es, int tau, int c)
 {

@@ -3,11 +3,7 @@
 
 namespace ss {
 
-constexpr int KT_THREADS = 1024;
 constexpr int KT_CAP = (1 << 30) - 1;                // sums stop here, above any number that means something; two of them are still a number of 32 bits
-// New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 |
-// 8.4, 2048 6.5 | 6.1 | 8.7, 4096 8.2 | 6.1 | 8.8, 32768 32 | 6.3 | 8.8; one request, 4096 5.4 | 5.5 | 8.6, 32768 17 | 5.5 | 8.6; 512 requests, 4096 9.1 | 6.3 | 9.5.
-constexpr int64_t KT_ONE_LAUNCH = 2048;
 
 __device__ inline int cap_add(int a, int b) { return min(a + b, KT_CAP); }
 
@@ -71,12 +67,11 @@ __device__ inline void kt_fill(const int32_t* start, const KtPlan<MAX>& plan, in
 }
 
 // The requests' numbers are few: one workgroup.  Bound by the launch and its waits, lengths and sums and slots: 64 requests of one token more 3.5 us in a trace (4.8 with
-// sums by shuffles through LDS).  Every input is read before the barrier behind which outputs are written, so new_lens may be lens and new_left may be left.  With many
-// rows, either
+// sums by shuffles through LDS).  Every input is read before the barrier behind which outputs are written, so new_lens and new_left may lie in the memory of lens, want
+// and left.  With many rows, either
 //   KT_EVERY   every workgroup works the plan out, the first one writes it, each fills in its rows; pages that this call gives back are taken from the table, not from
-//              the stack that another workgroup is writing.  Where new_lens and new_left are memory of their own, for up to 1024 requests.
+//              the stack that another workgroup is writing.  Where new_lens and new_left are memory of their own (kt_route), for up to 1024 requests.
 //   KT_PLAN    the plan goes through memory to a second launch.
-constexpr int KT_WHOLE = 0, KT_EVERY = 1, KT_PLAN = 2;
 template <int MODE>
 __global__ __launch_bounds__(KT_THREADS) void k_kv_plan(const int32_t* lens, const int32_t* want, int B, int32_t* table, int64_t ldt, int W, int page, Div by_page, int32_t* pool, int P,
                                                         const int32_t* left, int N, int32_t* new_lens, int32_t* new_left, int32_t* __restrict__ slots,
@@ -198,6 +193,10 @@ extern "C" ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t
     const size_t need = kv_tables_workspace_bytes(B, N);
     if (need > 0 && !workspace) return SS_ERR_NULL;
     if (((uintptr_t)workspace & 15) || workspace_bytes < need) return SS_ERR_WORKSPACE;
+    auto meets = [&](const int32_t* list, int64_t n) {
+        return kv_overlap(list, n, lens, B) || kv_overlap(list, n, want, B) || kv_overlap(list, n, left, 1) || kv_overlap(list, n, new_lens, B) || kv_overlap(list, n, new_left, 1);
+    };
+    if (meets(slots, N) || meets(offsets, B + 1) || kv_overlap(slots, N, offsets, B + 1) || kv_overlap(new_lens, B, new_left, 1)) return SS_ERR_SHAPE;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const Div by_page = make_div(page);
     KtPlan<KT_MAX>* const plan = static_cast<KtPlan<KT_MAX>*>(workspace);
@@ -205,8 +204,9 @@ extern "C" ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t
         hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(KT_THREADS), 0, hs, lens, want, (int)B, table, ldt, (int)W, (int)page, by_page, pool, (int)P, left, (int)N, new_lens, new_left, slots, offsets, plan);
         return launch_status();
     };
-    if (need == 0) return launch(k_kv_plan<KT_WHOLE>, 1);
-    if (B <= KT_THREADS && new_lens != lens && new_left != left) return launch(k_kv_plan<KT_EVERY>, (N + KT_THREADS - 1) / KT_THREADS);
+    const int route = kt_route(lens, want, B, left, N, new_lens, new_left);
+    if (route == KT_WHOLE) return launch(k_kv_plan<KT_WHOLE>, 1);
+    if (route == KT_EVERY) return launch(k_kv_plan<KT_EVERY>, (N + KT_THREADS - 1) / KT_THREADS);
     if (launch(k_kv_plan<KT_PLAN>, 1) != SS_OK) return SS_ERR_HIP;
     hipLaunchKernelGGL(k_kv_slots, dim3((uint32_t)((N + 255) / 256)), dim3(256), 0, hs, plan, (int)B, table, ldt, (int)page, by_page, pool, (int)P, (int)N, slots);
     return launch_status();
