@@ -435,8 +435,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     }
     const int64_t place = ((int64_t)item * a.H * a.tiles + unit) * KA_COLUMNS + r;
     if (parts > 1 && wave == 0 && j == 0 && there) a.sums[place] = make_float2(all_top, all_sum);
-    // nothing seen: zeros
-    const float inverse = parts > 1 ? 1.0f : all_sum == 0.0f ? 0.0f : 1.0f / all_sum;
+    const bool none = all_sum == 0.0f;               // nothing seen, or scores of minus infinity alone: zeros, though 0 times a value may be no number
+    const float inverse = parts > 1 || none ? 1.0f : 1.0f / all_sum;
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += CHUNK) {
         if (n0 > 0) __syncthreads();
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
             if (parts > 1) *reinterpret_cast<float4*>(a.parts + place * (32 * NS) + d) = make_float4(v[0], v[1], v[2], v[3]);
             else if (d < a.D) {
                 uint16_t* const to = a.out + b * a.ldo + (int64_t)(h * a.G + column) * a.ho + d;
-                const uint32_t w0 = pack_bf16x2(v[0] * inverse, v[1] * inverse), w1 = pack_bf16x2(v[2] * inverse, v[3] * inverse);
+                const uint32_t w0 = none ? 0 : pack_bf16x2(v[0] * inverse, v[1] * inverse), w1 = none ? 0 : pack_bf16x2(v[2] * inverse, v[3] * inverse);
                 if (d + 4 <= a.D) *reinterpret_cast<ka8_t*>(to) = ka8_t{w0, w1};
                 else {
 #pragma unroll
@@ -531,13 +531,14 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
     sum = row_sums[0];
 #pragma unroll
     for (int r = 1; r < ROWS; ++r) sum += row_sums[r];
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const bool none = sum == 0.0f;                   // as above
+    const float inverse = none ? 1.0f : 1.0f / sum;
     const float* const rows = reinterpret_cast<const float*>(acc);
     for (int d = threadIdx.x; d < 32 * SLICE && column0 + d < a.D; d += THREADS) {
         float x = 0.0f;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) x += rows[r * 32 * SLICE + d];
-        a.out[b * a.ldo + head * a.ho + column0 + d] = (uint16_t)pack_bf16x2(x * inverse, 0.0f);
+        a.out[b * a.ldo + head * a.ho + column0 + d] = none ? 0 : (uint16_t)pack_bf16x2(x * inverse, 0.0f);
     }
 }
 
