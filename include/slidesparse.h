@@ -307,7 +307,8 @@ ss_status kv_tables(const int32_t* lens, const int32_t* want, int64_t B, int32_t
 ss_status kv_write(const void* K, int64_t ldk, int64_t hk, const void* V, int64_t ldv, int64_t hv, ss_act_dtype in_dtype, int64_t N, int64_t H, int64_t D,
                    const int32_t* slots, void* pages, int64_t P, int64_t page, ss_dtype dtype, void* stream);
 
-/* What the pages hold of N slots, as fp32 or bf16 (codes of 8 bits: code times scale in fp32, then rounded); a slot outside gives zeros. */
+/* What the pages hold of N slots, as fp32 or bf16 (codes of 8 bits: code times scale in fp32, then rounded); a slot outside gives zeros.
+ * Rows of results (here and of kv_attention) that overlap: SS_ERR_SHAPE. */
 ss_status kv_read(const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* slots, int64_t N, int64_t H, int64_t D, ss_act_dtype out_dtype,
                   void* K, int64_t ldk, int64_t hk, void* V, int64_t ldv, int64_t hv, void* stream);
 

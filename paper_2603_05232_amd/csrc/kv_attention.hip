@@ -597,6 +597,7 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
         return SS_ERR_SHAPE;
     if (B == 0) return SS_OK;
     if (!Q || !pages || !table || !lens || !out || (!workspace && workspace_bytes > 0)) return SS_ERR_NULL;
+    if (!kv_rows_apart(B, ldo, Hq, ho, D)) return SS_ERR_SHAPE;
     if (((uintptr_t)Q & (in_dtype == SS_IN_F32 ? 3 : 1)) || ((uintptr_t)out & 1) || (((uintptr_t)table | (uintptr_t)lens) & 3) || ((uintptr_t)pages & 15)) return SS_ERR_SHAPE;
     if ((uintptr_t)workspace & 15) return SS_ERR_WORKSPACE;
     const int ns = kv_steps(D);

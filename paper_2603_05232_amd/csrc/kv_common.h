@@ -36,6 +36,18 @@ inline int64_t kv_bytes_of_page(int64_t H, int64_t page, int64_t D, int dtype) {
 // slots and positions are counted in 32 bits
 inline bool kv_valid_slots(int64_t pages, int64_t page) { return pages >= 1 && pages <= INT32_MAX / page; }
 
+// Whether N x H rows of D elements, ld and hs elements apart, have none in common: results that do are refused.
+inline bool kv_rows_apart(int64_t N, int64_t ld, int64_t H, int64_t hs, int64_t D)
+{
+    if (N < 2 || H < 2) return (N < 2 || ld >= D) && (H < 2 || hs >= D);
+    if (ld < D || hs < D) return false;
+    if (ld >= (H - 1) * hs + D || hs >= (N - 1) * ld + D) return true;      // heads within tokens, or tokens within heads
+    for (int64_t h = 1; h < H; ++h)                  // h heads on and n tokens back
+        for (int64_t n = h * hs / ld, last = n + 1; n <= last; ++n)
+            if (n >= 1 && n < N && h * hs - n * ld < D && n * ld - h * hs < D) return false;
+    return true;
+}
+
 // ---- kv_tables: by how many launches ----
 constexpr int KT_THREADS = 1024;
 // New tokens up to which the plan's workgroup fills in the slots too.  One workgroup | every one plans | two launches, us a call: 64 requests, 1024 tokens 5.6 | 6.0 |

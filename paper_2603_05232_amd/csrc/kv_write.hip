@@ -413,6 +413,7 @@ extern "C" ss_status kv_read(const void* pages, int64_t P, int64_t page, ss_dtyp
     if (N < 0 || N > KV_MAX_TOKENS || !kv_valid_page(H, page, D, dtype) || !kv_valid_slots(P, page) || !valid_strides(ldk, hk) || !valid_strides(ldv, hv)) return SS_ERR_SHAPE;
     if (N == 0) return SS_OK;
     if (!K || !V || !slots || !pages) return SS_ERR_NULL;
+    if (K == V || !kv_rows_apart(N, ldk, H, hk, D) || !kv_rows_apart(N, ldv, H, hv, D)) return SS_ERR_SHAPE;
     if ((((uintptr_t)K | (uintptr_t)V) & (out_dtype == SS_IN_F32 ? 3 : 1)) || ((uintptr_t)slots & 3) || ((uintptr_t)pages & 15)) return SS_ERR_SHAPE;
     const int64_t groups = (N + KW_WAVES * 8 - 1) / (KW_WAVES * 8) * H;
     if (!mx4_grid_fits(groups, 64 * KW_WAVES)) return SS_ERR_SHAPE;
