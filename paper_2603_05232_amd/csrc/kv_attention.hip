@@ -258,7 +258,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     }
     // as operands
     frag q[SHARED ? 1 : QP][SHARED ? 1 : NS];
-    float back = a.scale;                            // of a score
+    float back = a.scale, up = 1.0f;                 // of a score; half: what it is multiplied by first, so that 0 times an infinite product never comes up
     {
         float f[OWN][8];
 #pragma unroll
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[u][e] = __uint_as_float(QP == 2 ? raw[u][e * (QP - 1)] : e & 1 ? raw[u][e >> 1] & 0xFFFF0000u : raw[u][e >> 1] << 16);
         if constexpr (DT == SS_FP16) {
-            // half has 5 bits of exponent: a head's values are brought below 1 by a power of two, which its scores get back
+            // half has 5 bits of exponent: a head's values are brought to 1 by a power of two, from any size, which its scores get back
             float most = 0.0f;
 #pragma unroll
             for (int u = 0; u < OWN; ++u)
@@ -280,13 +280,13 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 #pragma unroll
                 for (int w = 0; w < KA_WAVES; ++w) most = fmaxf(most, wave_sums[w][r].x);
             }
-            const int x = most > 0x1p-100f && most < INFINITY ? min((int)(__float_as_uint(most) >> 23) - 126, 126) : 0;      // most < 2^x, or 4 times that
+            const int x = most > 0.0f && most < INFINITY ? min((int)(__float_as_uint(most) >> 23) - 126, 126) : 0;      // most < 2^x, or 4 times that
             const float down = __uint_as_float((uint32_t)(127 - x) << 23);
 #pragma unroll
             for (int u = 0; u < OWN; ++u)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[u][e] *= down;
-            back *= __uint_as_float((uint32_t)(127 + x) << 23);
+            (x > 0 ? up : back) *= __uint_as_float((uint32_t)(127 + x) << 23);
         }
 #pragma unroll
         for (int u = 0; u < OWN; ++u)
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
             }
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ES == 1 ? back * ks[e] : back);
+        for (int e = 0; e < 8; ++e) x[e] = (DT == SS_FP16 ? s[e >> 2][e & 3] * up : s[e >> 2][e & 3]) * (ES == 1 ? back * ks[e] : back);
         if (step + 1 < blocks) {
             go_to(step + 1);
             load_keys();

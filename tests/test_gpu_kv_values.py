@@ -35,3 +35,25 @@ def test_scores_of_minus_infinity_over_values_that_are_no_numbers(dtype, D):
         got = cache(q, ws=ws)
         assert bool((got[:3] == 0).all())
         assert bool(got[3].isfinite().all()) and bool((got[3] != 0).any())
+
+
+@pytest.mark.parametrize("source", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 200])
+@pytest.mark.parametrize("size", [1e-40, 1e-36, 1e-31, 1e36])
+def test_queries_of_any_size_over_a_cache_in_half(size, D, source):
+    """The scores are brought back by the scale, as far as there is one."""
+    cache = Cache(np.random.default_rng(7), [100, 3], 1, D, 32, "fp16", size=0.1)
+    q = queries(2, 3, D, source, size=size)
+    scale = min(0.5 / size, 1e38)
+    cache.check(cache(q, scale=scale), q, scale=float(np.float32(scale)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "i8", "fp8"])
+@pytest.mark.parametrize("size,scale", [(2.0 ** 100, 2.0 ** 28), (2.0 ** 120, -2.0 ** 126), (1.0, 2.0 ** 127)])
+def test_keys_of_zeros_under_large_queries_and_scales(size, scale, dtype):
+    """Every score is zero, however large what multiplies it: the mean of the values."""
+    cache = Cache(np.random.default_rng(8), [100, 3, 700], 2, 64, 32, dtype)
+    rewrite(cache, torch.zeros_like(cache.K), cache.V)
+    cache.k = np.zeros_like(cache.k)
+    q = queries(3, 4, 64, "bf16", size=size)
+    cache.check(cache(q, scale=scale), q, scale=scale)
