@@ -592,7 +592,8 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
 {
     if ((in_dtype != SS_IN_F32 && in_dtype != SS_IN_BF16) || !valid_dtype(dtype)) return SS_ERR_DTYPE;
     constexpr int64_t FAR = (int64_t)1 << 40;
-    if (!valid_attention(B, Hq, H, D) || !kv_valid_page(H, page, D, dtype) || !kv_valid_slots(P, page) || W < 1 || W > INT32_MAX / page - 1 || ldt < W || window < 0 || !(scale - scale == 0.0f) ||
+    const float scale2 = scale * 1.44269504088896340736f;      // of scores to the base 2
+    if (!valid_attention(B, Hq, H, D) || !kv_valid_page(H, page, D, dtype) || !kv_valid_slots(P, page) || W < 1 || W > INT32_MAX / page - 1 || ldt < W || window < 0 || !(scale2 - scale2 == 0.0f) ||
         ldq < 0 || ldq > FAR || hq < 0 || hq > FAR || ldo < 0 || ldo > FAR || ho < 0 || ho > FAR || ldt > FAR)
         return SS_ERR_SHAPE;
     if (B == 0) return SS_OK;
@@ -607,7 +608,7 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
     a.page_bytes = kv_bytes_of_page(H, page, D, dtype);
     a.table = table; a.ldt = ldt;
     a.H = (int)H; a.G = (int)(Hq / H); a.tiles = (a.G + KA_COLUMNS - 1) / KA_COLUMNS; a.D = (int)D; a.page = (int)page; a.P = (int)P;
-    a.scale = scale * 1.44269504088896340736f;
+    a.scale = scale2;
     a.out = static_cast<uint16_t*>(out); a.ldo = ldo; a.ho = ho;
     const int64_t units = H * a.tiles;
     // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.

@@ -130,3 +130,10 @@ def test_every_call_of_a_cache_has_a_workspace_of_its_own(monkeypatch):
     spans = [(w.data_ptr(), w.data_ptr() + w.numel()) for w in given]
     assert all(w.dtype == torch.uint8 and w.numel() >= 1000 for w in given) and all(a[1] <= b[0] or b[1] <= a[0] for i, a in enumerate(spans) for b in spans[:i])
     assert not any(w is v for w in given for v in vars(cache).values())
+
+
+def test_scales_that_are_infinite_in_powers_of_two_are_refused(lib):
+    """Scores are taken to the base 2: times 1.4427."""
+    def a(scale):
+        return lib.kv_attention(ONE, 1, 512, 64, ONE, 10, 64, 2, ONE, 4, 4, ONE, 2, 8, 4, 64, scale, 0, ONE, 512, 64, None, 0, None)
+    assert a(3e38) == a(-3e38) == a(2.4e38) == 3
