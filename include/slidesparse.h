@@ -315,7 +315,8 @@ ss_status kv_read(const void* pages, int64_t P, int64_t page, ss_dtype dtype, co
 /* out[b,i] = bf16(sum of p_t v_t / sum of p_t), p_t = exp(scale q[b,i] . k_t), over the cached tokens t of request b, head i / (Hq / H): t < lens[b], and t >= lens[b] - window where
  * window > 0.  Q[B,Hq,D] fp32 or bf16 (requests ldq, heads hq elements apart), out[B,Hq,D] bf16 (ldo, ho).  Hq is a multiple of H, at most 1024.  Scores, sums of
  * probabilities and weighted values in fp32, keys and values as the cache holds them; queries of 32 bits as two pieces of the cache's 16-bit type (SS_FP16: half, else
- * bf16: 16 bits in all).  scale and scale log2(e) are finite (SS_ERR_SHAPE).
+ * bf16: 16 bits in all).  Over a cache of 8 bits a query multiplies codes, and the key's scale their sum, which has to stay in fp32's range.  scale and scale log2(e)
+ * are finite (SS_ERR_SHAPE).
  * No token to see: zeros, also where all scores are minus infinity.  Lengths are moved into 0 .. W page; tokens of a page outside 0 .. P - 1
  * are not seen.  What lies in a page behind a request's tokens does not matter, NaNs included.
  * workspace: as for slide_sparse_gemm_ws, kv_attention_workspace_bytes() bytes let long requests be divided over the chip (the division follows the lengths on the

@@ -295,7 +295,9 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
                 v4i w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t both = ka_pack(f[u][2 * e], f[u][2 * e + 1], Ka<DT>());
+                    // a finite number above bf16's largest gets that one for its first piece, not infinity
+                    auto within = [](float x) { return QP == 2 && DT != SS_FP16 && fabsf(x) < INFINITY ? fminf(fmaxf(x, -0x1.FEp127f), 0x1.FEp127f) : x; };
+                    const uint32_t both = ka_pack(within(f[u][2 * e]), within(f[u][2 * e + 1]), Ka<DT>());
                     w[e] = (int)both;
                     if (p + 1 < QP) {                // what the piece left out; of an infinity nothing
                         typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;

@@ -57,3 +57,21 @@ def test_keys_of_zeros_under_large_queries_and_scales(size, scale, dtype):
     cache.k = np.zeros_like(cache.k)
     q = queries(3, 4, 64, "bf16", size=size)
     cache.check(cache(q, scale=scale), q, scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "i8", "fp8"])
+def test_queries_of_32_bits_that_bf16_would_round_to_infinity(dtype, D):
+    """Nearest to the largest numbers of 32 bits is no number of bf16: over keys of zeros, and over small ones."""
+    cache = Cache(np.random.default_rng(9), [100, 3], 1, D, 32, dtype)
+    K = torch.zeros_like(cache.K)
+    if dtype == "bf16":                                            # products with codes of 8 bits are infinite, and half has no numbers as small
+        K[:, :, 5] = 1e-30 * torch.randn(K.shape[:2], generator=torch.Generator().manual_seed(1))
+    rewrite(cache, K, cache.V)
+    cache.k = K.double().numpy()
+    q = queries(2, 3, D, "fp32")
+    q[:, 0, 5], q[:, 1, 5] = 3.4e38, -3.4028234e38
+    cache.check(cache(q, scale=1e-8), q, scale=float(np.float32(1e-8)))
+    q[0, 2, 7], q[1, 2, 7] = float("inf"), float("nan")            # these are not
+    got = cache(q, scale=1e-8)
+    assert bool(got[:, 2].isnan().all()) and bool(got[:, :2].isfinite().all())
