@@ -74,6 +74,16 @@ template <> struct Ka<SS_FP8_E4M3> : Ka<SS_BF16> {};
 __device__ inline uint32_t ka_pack(float a, float b, Ka<SS_BF16>) { return pack_bf16x2(a, b); }
 __device__ inline uint32_t ka_pack(float a, float b, Ka<SS_FP16>) { return f32_to_f16_bits(a) | (uint32_t)f32_to_f16_bits(b) << 16; }
 
+// First pieces of two numbers that are taken apart: below each of them and nearer to zero, so that what is left has the number's sign and is zero for zero alone.  Both
+// pieces then multiply an infinity to the same one.  What is left is at most a unit u of the first piece's last place; as the second one it is off by 2^-9 u (half
+// 2^-12 u), 2^-16 of the number (2^-22).  Above bf16's largest number the first piece is that one.
+__device__ inline uint32_t ka_toward_zero(float x) { return __float_as_uint(x) - (x != 0.0f ? 1u : 0u); }
+__device__ inline uint32_t ka_pack_below(float a, float b, Ka<SS_BF16>) { return __builtin_amdgcn_perm(ka_toward_zero(b), ka_toward_zero(a), 0x07060302u); }
+__device__ inline uint32_t ka_pack_below(float a, float b, Ka<SS_FP16>)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(ka_toward_zero(a)), __uint_as_float(ka_toward_zero(b))));
+}
+
 // eight codes of 8 bits as bf16, which holds them exactly
 template <int DT> __device__ inline v8bf ka_widen(uint32_t lo, uint32_t hi)
 {
@@ -295,19 +305,14 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
                 v4i w;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    // a finite number above bf16's largest gets that one for its first piece, not infinity
-                    auto within = [](float x) { return QP == 2 && DT != SS_FP16 && fabsf(x) < INFINITY ? fminf(fmaxf(x, -0x1.FEp127f), 0x1.FEp127f) : x; };
-                    const uint32_t both = ka_pack(within(f[u][2 * e]), within(f[u][2 * e + 1]), Ka<DT>());
+                    const uint32_t both = p + 1 < QP ? ka_pack_below(f[u][2 * e], f[u][2 * e + 1], Ka<DT>()) : ka_pack(f[u][2 * e], f[u][2 * e + 1], Ka<DT>());
                     w[e] = (int)both;
-                    if (p + 1 < QP) {                // what the piece left out; of an infinity nothing
+                    if (p + 1 < QP) {                // what the piece left out
                         typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
                         typedef half_t two_t __attribute__((ext_vector_type(2)));
                         const two_t t = __builtin_bit_cast(two_t, both);
-#pragma unroll
-                        for (int o = 0; o < 2; ++o) {
-                            float& x = f[u][2 * e + o];
-                            x = fabsf(x) < INFINITY ? x - (float)t[o] : 0.0f;
-                        }
+                        f[u][2 * e] -= (float)t[0];
+                        f[u][2 * e + 1] -= (float)t[1];
                     }
                 }
                 if constexpr (!SHARED) q[p][u] = __builtin_bit_cast(frag, w);

@@ -75,3 +75,22 @@ def test_queries_of_32_bits_that_bf16_would_round_to_infinity(dtype, D):
     q[0, 2, 7], q[1, 2, 7] = float("inf"), float("nan")            # these are not
     got = cache(q, scale=1e-8)
     assert bool(got[:, 2].isnan().all()) and bool(got[:, :2].isfinite().all())
+
+
+@pytest.mark.parametrize("D", [64, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_keys_of_minus_infinity_under_queries_of_32_bits(dtype, D):
+    """Scores of minus infinity, whatever pieces a query is multiplied in: one that a piece holds whole, one whose first piece is above it, one below."""
+    lens = [40, 700, 33]
+    cache = Cache(np.random.default_rng(10), lens, 1, D, 32, dtype, source="fp32")
+    K = cache.K.clone()
+    gone = torch.zeros(sum(lens), dtype=torch.bool)
+    gone[[0, 7, 39, 41, 300, 739]] = True
+    gone[740:] = True                                              # all of the last one's
+    K[gone, 0, 0] = float("-inf")
+    rewrite(cache, K, cache.V)
+    q = queries(3, 3, D, "fp32")
+    q[:, :, 0] = torch.tensor([1.0, 1.0 + 2.0 ** -7 - 2.0 ** -12, 1.0 + 2.0 ** -12], device=DEV)
+    cache.k[gone.numpy(), 0, 0] = 0.0                              # not seen by the oracle
+    starts = cache.starts
+    cache.check(cache(q), q, seen=lambda b, t: ~gone.numpy()[starts[b] + t])
