@@ -382,7 +382,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[n] *= less;
-        // The probabilities as operands.  bf16 alone would cost as much again as the rounding of the result, so what it leaves out is multiplied as well.
+        // The probabilities as operands.  bf16 alone would cost as much again as the rounding of the result, so what it leaves out is multiplied as well.  Codes of 8 bits
+        // are no infinities: the nearest first piece leaves less.
         constexpr int PP = DT == SS_FP16 ? 1 : 2;
         frag p[PP];
 #pragma unroll
@@ -390,10 +391,13 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
             v4i w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                w[e] = (int)ka_pack(y[2 * e], y[2 * e + 1], Ka<DT>());
+                w[e] = (int)(ES == 2 && i + 1 < PP ? ka_pack_below(y[2 * e], y[2 * e + 1], Ka<DT>()) : ka_pack(y[2 * e], y[2 * e + 1], Ka<DT>()));
                 if (i + 1 < PP) {
-                    y[2 * e] -= __uint_as_float((uint32_t)w[e] << 16);
-                    y[2 * e + 1] -= __uint_as_float((uint32_t)w[e] & 0xFFFF0000u);
+                    typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
+                    typedef half_t two_t __attribute__((ext_vector_type(2)));
+                    const two_t t = __builtin_bit_cast(two_t, (uint32_t)w[e]);
+                    y[2 * e] -= (float)t[0];
+                    y[2 * e + 1] -= (float)t[1];
                 }
             }
             p[i] = __builtin_bit_cast(frag, w);

@@ -94,3 +94,29 @@ def test_keys_of_minus_infinity_under_queries_of_32_bits(dtype, D):
     cache.k[gone.numpy(), 0, 0] = 0.0                              # not seen by the oracle
     starts = cache.starts
     cache.check(cache(q), q, seen=lambda b, t: ~gone.numpy()[starts[b] + t])
+
+
+@pytest.mark.parametrize("D", [64, 200])
+@pytest.mark.parametrize("source", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_values_of_infinity(dtype, source, D):
+    """An infinity among the values that are seen makes its channel that infinity, two of them a NaN, and no other channel anything."""
+    lens = [1, 40, 3000]
+    cache = Cache(np.random.default_rng(11), lens, 1, D, 32, dtype)
+    inf = float("inf")
+    V = cache.V.clone()
+    V[0, 0, 3], V[5, 0, 9], V[30, 0, D - 1], V[100, 0, 20], V[101, 0, 20], V[2900, 0, 21], V[2901, 0, 21] = inf, -inf, inf, inf, -inf, inf, inf
+    rewrite(cache, cache.K, V)
+    q = queries(3, 3, D, source, size=0.3)
+    for ws in (True, False):
+        got = cache(q, ws=ws)
+        assert bool((got[0, :, 3] == inf).all()) and bool((got[1, :, 9] == -inf).all()) and bool((got[1, :, D - 1] == inf).all())
+        assert bool(got[2, :, 20].isnan().all()) and bool((got[2, :, 21] == inf).all())
+        odd = torch.zeros((3, D), dtype=torch.bool, device=DEV)
+        odd[0, 3] = odd[1, 9] = odd[1, D - 1] = odd[2, 20] = odd[2, 21] = True
+        assert bool(got.isfinite().eq(~odd[:, None]).all())
+        plain = Cache.__new__(Cache)
+        vars(plain).update(vars(cache))
+        rewrite(plain, cache.K, cache.V)
+        cache.check(torch.where(odd[:, None], plain(q, ws=ws), got), q)
+        rewrite(cache, cache.K, V)
