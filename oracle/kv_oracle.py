@@ -110,8 +110,8 @@ def attention(q, k, v, scale, seen):
 def bound(out, share, sums, spread, floor, D, T, dtype, fp32_q):
     """How far the kernel's bf16 result may be off.  Score: D + 8 roundings of 2^-24 of the sum of magnitudes; a query of 32 bits as two bf16 pieces 2^-16 of it, as two half pieces 2^-22; in
     half, values far below the head's largest 2^-24 of that one; the argument of the exponential 4 roundings of its size; e^delta - 1 counts twice (numerator and denominator).
-    Probabilities 2^-16 (two bf16 pieces) or 2^-11 (half), exponential, scales and weights of parts 2^-20 in all; sums over T tokens T + 64 roundings of 2^-24.  The result 2^-8 of itself."""
+    Probabilities 2^-16 (two bf16 pieces) or 2^-22 (two half pieces), exponential, scales and weights of parts 2^-20 in all; sums over T tokens T + 64 roundings of 2^-24.  The result 2^-8 of itself."""
     half = dtype == "fp16"
     delta = sums * ((D + 8) * 2.0 ** -24 + ((2.0 ** -22 if half else 2.0 ** -16) if fp32_q else 0.0)) + (2.0 ** -24 * floor if half else 0.0) + 4 * spread * 1.4427 * 2.0 ** -24
-    rel = 2 * np.expm1(delta) + (2.0 ** -11 if half else 2.0 ** -16) + 2.0 ** -20 + (T + 64) * 2.0 ** -24
+    rel = 2 * np.expm1(delta) + (2.0 ** -22 if half else 2.0 ** -16) + 2.0 ** -20 + (T + 64) * 2.0 ** -24
     return 2.0 ** -8 * np.abs(out) + share * rel[:, None] + 1e-37

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv_oracle as ko
 from paper_2603_05232_amd import binding
 from test_gpu_kv import DEV, Cache, i32, queries
 
@@ -120,3 +121,31 @@ def test_values_of_infinity(dtype, source, D):
         rewrite(plain, cache.K, cache.V)
         cache.check(torch.where(odd[:, None], plain(q, ws=ws), got), q)
         rewrite(cache, cache.K, V)
+
+
+@pytest.mark.parametrize("source", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_probabilities_where_values_cancel(dtype, source):
+    """Two groups of tokens, of one probability each, whose values nearly cancel: a probability that is rounded stands out.  Two pieces of a probability are within
+    2^-16 of it (bf16: 2^-9 of a unit of 2^-7) or 2^-22 (half: 2^-12 of 2^-10); of the rest as oracle.kv_oracle.bound counts it."""
+    rng = np.random.default_rng(12)
+    few = rng.integers(2, 8, 40)
+    many = few + rng.integers(1, 8, 40)
+    lens = [int(n) for n in few + many]
+    cache = Cache(rng, lens, 1, 32, 32, dtype)
+    K, V = torch.zeros_like(cache.K), torch.ones_like(cache.V)
+    for b, (n, m) in enumerate(zip(few, many)):
+        rows = slice(cache.starts[b] + int(n), cache.starts[b + 1])
+        K[rows, 0, 0] = float(np.log(n / m))                       # their probability, about n / m of the others'
+        V[rows] = -1.0
+    rewrite(cache, K, V)
+    q = torch.zeros((40, 3, 32), device=DEV)
+    q[:, :, 0] = torch.tensor([1.0, 1.0078125, 0.9921875])
+    got = cache(q.bfloat16() if source == "bf16" else q, scale=1.0).double().cpu().numpy()
+    k, v = ko.held(K.float().numpy(), dtype), ko.held(V.float().numpy(), dtype)
+    for b in range(40):
+        rows = slice(cache.starts[b], cache.starts[b + 1])
+        out, share, sums, spread, floor = ko.attention(q[b].double().cpu().numpy(), k[rows], v[rows], 1.0, np.ones(lens[b], bool))
+        delta = sums * (32 + 8) * 2.0 ** -24 + 4 * spread * 1.4427 * 2.0 ** -24
+        rel = 2 * np.expm1(delta) + 2.0 ** (-16 if dtype == "bf16" else -22) + 2.0 ** -20 + (lens[b] + 64) * 2.0 ** -24
+        assert (np.abs(got[b] - out) <= 2.0 ** -8 * np.abs(out) + share * rel[:, None]).all(), b
