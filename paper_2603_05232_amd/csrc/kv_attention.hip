@@ -114,10 +114,10 @@ struct KaArgs {
     int H, G, tiles, D, page, P;                     // heads of keys, query heads to each, products that take
     float scale;                                     // of the scores, times log2(e)
     uint16_t* out; int64_t ldo, ho;
-    int2* plan;                                      // of each request: its first item, its parts (if requests are divided)
-    float2* sums;                                    // [item][head of keys][tile][column]: maximum, sum
+    int2* plan;                                      // of each request: the place of its first part, its parts (if requests are divided)
+    float2* sums;                                    // [place][head of keys][tile][column]: maximum, sum
     float* parts;                                    // the same [.. , 32 NS]: weighted values
-    int items;
+    int items, places;                               // parts of all requests; those of the requests that are in several
     Div by_heads, by_round, by_blocks;               // H; 8 tiles; blocks of a page
     KaDivision division;
 };
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     if (!ONCE && item >= a.items) return;
 
     // this workgroup's request and its part of it
-    int b = -1, part = 0, parts = 1;
+    int b = -1, part = 0, parts = 1, place = 0;      // a part's place among those of requests that are divided: the others take none
     KaSpan span = {0, 0, 0, 0};
     if (!a.plan) {
         b = item;
@@ -154,23 +154,25 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
     } else {
         const KaSpan mine = ka_span(a.division, lane);   // of the first 64 requests, which mostly are all
         const int per = ka_per(a.division, mine);
-        for (int b0 = 0, before = 0; b0 < a.division.B; b0 += 64) {
+        for (int b0 = 0, before = 0, whole = 0; b0 < a.division.B; b0 += 64) {
             const KaSpan s = b0 == 0 ? mine : ka_span(a.division, b0 + lane);
             const int n = b0 + lane < a.division.B ? ka_parts(s.blocks, per) : 0, upto = before + wave_scan_add(n);
-            const uint64_t has = __ballot(upto > item);
+            const uint64_t has = __ballot(upto > item), single = __ballot(n == 1);
             if (has) {
                 const int at = __ffsll((unsigned long long)has) - 1;
                 b = b0 + at;
                 parts = __builtin_amdgcn_readlane(n, at);
                 part = item - (__builtin_amdgcn_readlane(upto, at) - parts);
+                place = item - whole - __popcll(single & (((uint64_t)1 << at) - 1));
                 span = {__builtin_amdgcn_readlane(s.first, at), __builtin_amdgcn_readlane(s.blocks, at), __builtin_amdgcn_readlane(s.len, at), __builtin_amdgcn_readlane(s.from, at)};
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
+            whole += __popcll(single);
         }
     }
-    if (b < 0) return;
-    if (a.plan && part == 0 && unit == 0 && threadIdx.x == 0) a.plan[b] = make_int2(item, parts);
+    if (b < 0 || (parts > 1 && place >= a.places)) return;      // (the latter only if lengths are changed while they are read)
+    if (a.plan && part == 0 && unit == 0 && threadIdx.x == 0) a.plan[b] = make_int2(place, parts);
     const int each = (span.blocks + parts - 1) / parts, lo = span.first + part * each, end = min(lo + each, span.first + span.blocks);
 
     // The queries' loads: lane (r, j) gets values 32 s + 8 j .. + 7 of head r, four words of two or eight of one.  Long heads are shared out among the wavefronts,
@@ -445,8 +447,8 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
         weight[w] = s.x == all_top ? 1.0f : __builtin_amdgcn_exp2f(s.x - all_top);      // both may be minus infinity
         all_sum += s.y * weight[w];
     }
-    const int64_t place = ((int64_t)item * a.H * a.tiles + unit) * KA_COLUMNS + r;
-    if (parts > 1 && wave == 0 && j == 0 && there) a.sums[place] = make_float2(all_top, all_sum);
+    const int64_t row_at = ((int64_t)place * a.H * a.tiles + unit) * KA_COLUMNS + r;
+    if (parts > 1 && wave == 0 && j == 0 && there) a.sums[row_at] = make_float2(all_top, all_sum);
     const bool none = all_sum == 0.0f;               // nothing seen, or scores of minus infinity alone: zeros, though 0 times a value may be no number
     const float inverse = parts > 1 || none ? 1.0f : 1.0f / all_sum;
 #pragma unroll
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
             }
             const int d = 16 * (n0 + n) + 4 * j;
             if (!there) continue;
-            if (parts > 1) *reinterpret_cast<float4*>(a.parts + place * (32 * NS) + d) = make_float4(v[0], v[1], v[2], v[3]);
+            if (parts > 1) *reinterpret_cast<float4*>(a.parts + row_at * (32 * NS) + d) = make_float4(v[0], v[1], v[2], v[3]);
             else if (d < a.D) {
                 uint16_t* const to = a.out + b * a.ldo + (int64_t)(h * a.G + column) * a.ho + d;
                 const uint32_t w0 = none ? 0 : pack_bf16x2(v[0] * inverse, v[1] * inverse), w1 = none ? 0 : pack_bf16x2(v[2] * inverse, v[3] * inverse);
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_join(const KaArgs a)
     const int slice = blockIdx.x % (NS / SLICE), index = blockIdx.x / (NS / SLICE), heads = a.H * a.G, b = index / heads;
     const int2 plan = a.plan[b];
     const int parts = plan.y;
-    if (parts < 2 || plan.x < 0 || parts > a.items - plan.x) return;      // (the last two only if lengths are changed while they are read)
+    if (parts < 2 || plan.x < 0 || parts > a.places - plan.x) return;      // (the last two only if lengths are changed while they are read)
     const int head = index - b * heads, h = head / a.G, column = head - h * a.G;
     const int64_t step = (int64_t)a.H * a.tiles * KA_COLUMNS, first = plan.x * step + (h * a.tiles + column / KA_COLUMNS) * KA_COLUMNS + column % KA_COLUMNS;
     const int at_row = threadIdx.x / LANES, at = threadIdx.x - at_row * LANES, column0 = slice * 32 * SLICE;      // its first value
@@ -578,6 +580,9 @@ static int64_t wanted_groups(int64_t D) { return (kv_steps(D) == 8 ? 3 : 2) * (i
 static int64_t undivided_blocks(int64_t groups) { return groups <= cu_count() ? 16 : groups <= 4 * cu_count() ? 32 : 64; }
 // bytes of a part of a request: sums and values of all heads
 static int64_t part_bytes(int64_t units, int64_t D) { return units * KA_COLUMNS * (8 + 4 * 32 * kv_steps(D)); }
+// Parts of requests that are in several, for so many workgroups: such a request has more blocks than one of these takes, so that there are no more such requests than
+// workgroups, and one part each beyond what the blocks come to.  The rest covers the roundings of a share.
+static int64_t places_for(int64_t wanted, int64_t B) { return wanted + (B < wanted ? B : wanted) + 2; }
 // and of the plan that lies before them
 static int64_t plan_bytes(int64_t B) { return (8 * B + 15) & ~(int64_t)15; }
 
@@ -595,7 +600,7 @@ extern "C" size_t kv_attention_workspace_bytes(int64_t B, int64_t Hq, int64_t H,
     if (!valid_attention(B, Hq, H, D) || B == 0) return 0;
     const int64_t units = H * ((Hq / H + KA_COLUMNS - 1) / KA_COLUMNS);
     const int64_t wanted = wanted_groups(D) / units;
-    return wanted > 1 ? (size_t)(plan_bytes(B) + (wanted + 2 + B) * part_bytes(units, D)) : 0;
+    return wanted > 1 ? (size_t)(plan_bytes(B) + places_for(wanted, B) * part_bytes(units, D)) : 0;
 }
 
 extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t ldq, int64_t hq, const void* pages, int64_t P, int64_t page, ss_dtype dtype, const int32_t* table,
@@ -625,13 +630,14 @@ extern "C" ss_status kv_attention(const void* Q, ss_act_dtype in_dtype, int64_t 
     const int64_t units = H * a.tiles;
     // Parts of all requests together: sum of blocks / per + one for each request.  None where no request can be long enough, or the workspace has no room.
     const int64_t bytes = (int64_t)(workspace_bytes < (size_t)1 << 50 ? workspace_bytes : (size_t)1 << 50) - plan_bytes(B);
-    const int64_t room = bytes / part_bytes(units, D) - B - 2, want = wanted_groups(D) / units, wanted = room < want ? room : want;
+    const int64_t places = bytes / part_bytes(units, D) - 2, room = places - B > places / 2 ? places - B : places / 2, want = wanted_groups(D) / units, wanted = room < want ? room : want;
     const bool join = wanted > 1 && W * page > undivided_blocks(B * units) * KV_BLOCK;
     a.division = {lens, (int)B, (int)(W * page), (int)(window < INT32_MAX ? window : 0), join ? 1.0f / (float)wanted : 0.0f};
     a.items = (int)(join ? wanted + 2 + B : B);
+    a.places = (int)(join ? places_for(wanted, B) : 0);
     a.plan = join ? static_cast<int2*>(workspace) : nullptr;
     a.sums = join ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan_bytes(B)) : nullptr;
-    a.parts = join ? reinterpret_cast<float*>(a.sums + a.items * units * KA_COLUMNS) : nullptr;
+    a.parts = join ? reinterpret_cast<float*>(a.sums + a.places * units * KA_COLUMNS) : nullptr;
     a.by_heads = make_div(H);
     a.by_round = make_div(8 * a.tiles);
     a.by_blocks = make_div(page / KV_BLOCK);
