@@ -149,3 +149,19 @@ def test_probabilities_where_values_cancel(dtype, source):
         delta = sums * (32 + 8) * 2.0 ** -24 + 4 * spread * 1.4427 * 2.0 ** -24
         rel = 2 * np.expm1(delta) + 2.0 ** (-16 if dtype == "bf16" else -22) + 2.0 ** -20 + (lens[b] + 64) * 2.0 ** -24
         assert (np.abs(got[b] - out) <= 2.0 ** -8 * np.abs(out) + share * rel[:, None]).all(), b
+
+
+@pytest.mark.parametrize("source", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype", ["i8", "fp8"])
+def test_rows_of_the_largest_numbers(dtype, source):
+    """Scales whose inverses are below the normal numbers of 32 bits, or nearly."""
+    g = torch.Generator().manual_seed(2)
+    x = torch.rand((64, 2, 48), generator=g) * 2 - 1
+    x[:, :, 7] = 1.0
+    x *= torch.tensor([3.3e38, 8.6e37, 8.4e37, 4.3e37, 2e36, 1e-29, 1.6e-30, 8e-31])[torch.arange(64) % 8][:, None, None]
+    x = x.to(torch.bfloat16 if source == "bf16" else torch.float32)
+    pages = torch.zeros((2, binding.kv_page_bytes(2, 32, 48, dtype)), dtype=torch.uint8, device=DEV)
+    slots = i32(range(64))
+    binding.kv_write(x.to(DEV), x.flip(0).to(DEV), slots, pages, 32, dtype)
+    k, v = binding.kv_read(pages, slots, 2, 48, 32, dtype, torch.float32)
+    assert np.array_equal(k.cpu().numpy(), ko.held(x.float().numpy(), dtype)) and np.array_equal(v.cpu().numpy(), ko.held(x.flip(0).float().numpy(), dtype))
