@@ -557,7 +557,7 @@ def expert_combine(Y: torch.Tensor, slots: torch.Tensor, weights: torch.Tensor, 
 
 # ---- a paged cache of keys and values --------------------------------------------------------------------------------------------
 
-# The stream is the current device's, so the tensors have to be there too.
+# The stream is the current device's, so the tensors have to be there too.  Results that a call makes itself may share one allocation, which lives as long as any of them.
 
 def _current_device() -> int:
     return torch._C._cuda_getDevice()
@@ -594,7 +594,7 @@ def kv_tables_workspace_bytes(B: int, N: int) -> int:
 
 def kv_tables(lens: torch.Tensor, want: torch.Tensor, table: torch.Tensor, pool: torch.Tensor, left: torch.Tensor, page: int, N: int, new_lens=None, new_left=None, workspace=None):
     """Pages for B requests that go from lens[B] to want[B] tokens (int32): table[B,W] and the stack of free pages pool[0 .. left[0] - 1] are brought up to date in place
-    -> (new_lens[B], new_left[1], slots[N], offsets[B + 1]); new_lens may be lens and new_left may be left."""
+    -> (new_lens[B], new_left[1], slots[N], offsets[B + 1]); new_lens may be lens and new_left may be left, or lie in the memory of want."""
     if _kv_calls is None:
         load()
     done = _kv_calls.kv_tables(lens, want, table, pool, left, page, N, new_lens, new_left, workspace)

@@ -94,7 +94,7 @@ class LlamaBlock:
 
     def decode(self, x: torch.Tensor, cache, slots: torch.Tensor, path: str = "fused", timer=None, record=None, window: int = 0):
         """x[B, HIDDEN] bf16, one new token of each request of `cache`, which has made room for it at slots[B] (cache.step()) -> [B, HIDDEN] bf16.  Each token sees its
-        request's cached ones and itself.  record: as above, and "attention": (queries, result)."""
+        request's cached ones and itself (where it found no room, slot -1, the cached ones alone).  record: as above, and "attention": (queries, result)."""
         run = self._run(path, timer, record)
         q, k, v = run("qkv", rms_norm(x)).unflatten(1, (-1, HEAD_DIM)).split([N_Q_HEADS, N_KV_HEADS, N_KV_HEADS], dim=1)
         cache.write(k, v, slots)

@@ -8,7 +8,7 @@
 // Bound by HBM: each key and value is read once for all query heads of its head (a product has room for 16), 4 D operations a byte pair on matrix cores that could do
 // fifty times that.  A block's products and softmax take some 2500 cycles of a wavefront, so that what counts is bytes under way: a block and a half for each of twelve
 // wavefronts of a compute unit, 16 KB a block of 128 channels.  Medians of a trace: 256 requests of 4096 tokens, 4 heads of 128, bf16 319 us, 6.7 TB/s; 64 of 16384
-// down to 256 166 (6.3), the same in fp8 92 (5.9); one of 131072 tokens 44.5 (6.0) and 4.6 for the join.  The counters show the cache's bytes read once (2150 MB of
+// down to 256 167 (6.3), the same in fp8 92 .. 102 (5.9 .. 5.3); one of 131072 tokens 44.5 (6.0) and 4.6 for the join.  The counters show the cache's bytes read once (2150 MB of
 // 2150).  One physical placement of the pages or another makes up to 15 % (the same call 203 and 234 us).  Requests below some 1000 tokens are bound by the waits at
 // the start (lengths, table, keys, one after the other: 4.7 us for one token) and by what a compute unit draws by itself, 60 GB/s.
 //

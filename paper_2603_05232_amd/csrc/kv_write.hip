@@ -1,6 +1,6 @@
 // kv_write, kv_read: keys and values of tokens into the pages of a cache, quantised on the way, and out of them again.
 //
-// Bound by HBM where there are many tokens, 8192 tokens of 8 heads of 128, bf16 to fp8: 10.4 us (33.9 MB read, 17.3 written, 4.9 TB/s) and back 9.9 us, and by three
+// Bound by HBM where there are many tokens, 8192 tokens of 8 heads of 128, bf16 to fp8: 10.4 .. 10.7 us (33.9 MB read, 17.3 written, 4.8 .. 4.9 TB/s) and back 10.2 us, and by three
 // waits one after the other (slots, rows, stores; 2.8 us) where there are few.  Values by single elements throughout took 17 us: a store of one byte for each channel
 // of a token.
 #include "kv_common.h"
