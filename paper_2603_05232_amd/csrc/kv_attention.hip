@@ -83,6 +83,21 @@ __device__ inline uint32_t ka_pack_below(float a, float b, Ka<SS_FP16>)
 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(ka_toward_zero(a)), __uint_as_float(ka_toward_zero(b))));
 }
+// and what they leave of a number: in half no less than its smallest, which would be rounded to zero.  PROBABILITY: not below zero, and of a NaN the first piece is one
+template <int DT, bool PROBABILITY> __device__ inline void ka_leave(float& a, float& b, uint32_t both)
+{
+    typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
+    typedef half_t two_t __attribute__((ext_vector_type(2)));
+    const two_t t = __builtin_bit_cast(two_t, both);
+    auto rest = [](float x, float piece) {
+        const float r = x - piece;
+        if constexpr (DT != SS_FP16) return r;
+        else if constexpr (PROBABILITY) return fmaxf(r, fminf(x, 0x1p-24f));
+        else return r != 0.0f && fabsf(r) < 0x1p-24f ? copysignf(0x1p-24f, r) : r;
+    };
+    a = rest(a, (float)t[0]);
+    b = rest(b, (float)t[1]);
+}
 
 // eight codes of 8 bits as bf16, which holds them exactly
 template <int DT> __device__ inline v8bf ka_widen(uint32_t lo, uint32_t hi)
@@ -278,7 +293,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[u][e] = __uint_as_float(QP == 2 ? raw[u][e * (QP - 1)] : e & 1 ? raw[u][e >> 1] & 0xFFFF0000u : raw[u][e >> 1] << 16);
         if constexpr (DT == SS_FP16) {
-            // half has 5 bits of exponent: a head's values are brought to 1 by a power of two, from any size, which its scores get back
+            // half has 5 bits of exponent: a head's largest value is brought to 2^13 .. 2^14 by a power of two, which its scores get back; the smallest then keep their bits
             float most = 0.0f;
 #pragma unroll
             for (int u = 0; u < OWN; ++u)
@@ -292,7 +307,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 #pragma unroll
                 for (int w = 0; w < KA_WAVES; ++w) most = fmaxf(most, wave_sums[w][r].x);
             }
-            const int x = most > 0.0f && most < INFINITY ? min((int)(__float_as_uint(most) >> 23) - 126, 126) : 0;      // most < 2^x, or 4 times that
+            const int x = most > 0.0f && most < INFINITY ? max((int)(__float_as_uint(most) >> 23) - 140, -126) : 0;      // most < 2^(x + 14)
             const float down = __uint_as_float((uint32_t)(127 - x) << 23);
 #pragma unroll
             for (int u = 0; u < OWN; ++u)
@@ -309,13 +324,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t both = p + 1 < QP ? ka_pack_below(f[u][2 * e], f[u][2 * e + 1], Ka<DT>()) : ka_pack(f[u][2 * e], f[u][2 * e + 1], Ka<DT>());
                     w[e] = (int)both;
-                    if (p + 1 < QP) {                // what the piece left out
-                        typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
-                        typedef half_t two_t __attribute__((ext_vector_type(2)));
-                        const two_t t = __builtin_bit_cast(two_t, both);
-                        f[u][2 * e] -= (float)t[0];
-                        f[u][2 * e + 1] -= (float)t[1];
-                    }
+                    if (p + 1 < QP) ka_leave<DT, false>(f[u][2 * e], f[u][2 * e + 1], both);
                 }
                 if constexpr (!SHARED) q[p][u] = __builtin_bit_cast(frag, w);
                 else if (own(u) < NS) shared_q[p][own(u)][lane] = w;
@@ -395,13 +404,7 @@ __global__ __launch_bounds__(64 * KA_WAVES, ka_fit(NS)) void k_kv_attend(const K
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 w[e] = (int)(ES == 2 && i + 1 < PP ? ka_pack_below(y[2 * e], y[2 * e + 1], Ka<DT>()) : ka_pack(y[2 * e], y[2 * e + 1], Ka<DT>()));
-                if (i + 1 < PP) {
-                    typedef typename std::conditional<DT == SS_FP16, _Float16, __bf16>::type half_t;
-                    typedef half_t two_t __attribute__((ext_vector_type(2)));
-                    const two_t t = __builtin_bit_cast(two_t, (uint32_t)w[e]);
-                    y[2 * e] -= (float)t[0];
-                    y[2 * e + 1] -= (float)t[1];
-                }
+                if (i + 1 < PP) ka_leave<DT, true>(y[2 * e], y[2 * e + 1], (uint32_t)w[e]);
             }
             p[i] = __builtin_bit_cast(frag, w);
         }

@@ -165,3 +165,34 @@ def test_rows_of_the_largest_numbers(dtype, source):
     binding.kv_write(x.to(DEV), x.flip(0).to(DEV), slots, pages, 32, dtype)
     k, v = binding.kv_read(pages, slots, 2, 48, 32, dtype, torch.float32)
     assert np.array_equal(k.cpu().numpy(), ko.held(x.float().numpy(), dtype)) and np.array_equal(v.cpu().numpy(), ko.held(x.flip(0).float().numpy(), dtype))
+
+
+@pytest.mark.parametrize("source", ["bf16", "fp32"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_values_of_infinity_under_any_probability(dtype, source):
+    """Two tokens to a request, the second one less likely by anything down to 2^-36 and of infinite values."""
+    B = 2000
+    cache = Cache(np.random.default_rng(13), [2] * B, 1, 32, 32, dtype)
+    K, V = torch.zeros_like(cache.K), torch.ones_like(cache.V)
+    K[1::2, 0, 0] = -torch.rand((B,), generator=torch.Generator().manual_seed(3)).to(K.dtype) * 25
+    V[1::2, 0, 4], V[1::2, 0, 5] = float("inf"), float("-inf")
+    rewrite(cache, K, V)
+    q = torch.zeros((B, 2, 32), device=DEV)
+    q[:, :, 0] = torch.rand((B, 2), generator=torch.Generator().manual_seed(4)).to(DEV) * 0.1 + 0.9
+    got = cache(q.bfloat16() if source == "bf16" else q, scale=1.0)
+    assert bool((got[:, :, 4] == float("inf")).all()) and bool((got[:, :, 5] == float("-inf")).all()) and bool((got[:, :, :4] == 1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_keys_of_minus_infinity_under_any_query_of_32_bits(dtype):
+    """One of two tokens is not seen for its score, whatever the query's value there, down to 2^-35 of the largest."""
+    B = 2000
+    cache = Cache(np.random.default_rng(14), [2] * B, 1, 32, 32, dtype)
+    K, V = torch.zeros_like(cache.K), torch.ones_like(cache.V)
+    K[1::2, 0, 0], V[1::2] = float("-inf"), 3.0
+    rewrite(cache, K, V)
+    g = torch.Generator().manual_seed(5)
+    q = torch.rand((B, 2, 32), generator=g)
+    q[:, :, 0] = torch.exp2(-torch.randint(0, 35, (B, 2), generator=g).float()) * (1 + torch.randint(0, 3, (B, 2), generator=g) * 2.0 ** -23)
+    q[:, :, 1] = 1.0
+    assert bool((cache(q.to(DEV)) == 1).all())
